@@ -1,0 +1,343 @@
+"""The cases of the feed-forward operators: what a program that trains a gated
+feed-forward block, bounds its gradients and serves it with 4-bit weights has
+the library do.
+
+Kinds:
+
+  ffn_train   h = act(x Wg^T) * (x Wu^T), then from gh the gradients of x, Wg
+              and Wu; 16-bit tensors.
+  ffn_infer   the forward alone.
+  q4_linear   y = x W^T + b, W in 4-bit E2M1 codes with a scale per group.
+  q4_gated    h = act(x Wg^T) * (x Wu^T) on such weights.
+  clip        the norm over all gradients of a model, and the gradients scaled
+              to at most `max_norm`.
+
+`own` chooses between the library's kernels and a plain form in fp32.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+_T = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+_SIZE = {"f16": 2, "bf16": 2, "f32": 4}
+_ACTS = ("silu", "gelu", "relu")
+
+
+# ---------------------------------------------------------------------------
+# cases
+# ---------------------------------------------------------------------------
+
+def _ffn(name, kind, m, k, f, dtype, act, wide=0):
+    return dict(name=name, kind=kind, m=m, k=k, f=f, dtype=dtype, act=act, wide=wide)
+
+
+def _q4(name, kind, m, k, n, group, dtype, act="silu", bias=False, wide=0):
+    return dict(name=name, kind=kind, m=m, k=k, n=n, group=group, dtype=dtype, act=act, bias=bias, wide=wide)
+
+
+def listed():
+    return [
+        # a block at the ConvNet's first fully connected sizes and batch (8192 features in, 1024 hidden)
+        _ffn("ffn_train_f16_convnet_fc", "ffn_train", 256, 8192, 1024, "f16", "relu"),
+        # an ordinary training step of one block
+        _ffn("ffn_train_bf16_m4096", "ffn_train", 4096, 2048, 8192, "bf16", "silu"),
+        # sizes that fill no tile; rows of an odd hidden size start at any 2-byte address
+        _ffn("ffn_train_f16_ragged", "ffn_train", 1021, 1000, 2731, "f16", "gelu"),
+        # the largest training step: two sequences of 4096 tokens through a wide block
+        _ffn("ffn_train_bf16_m8192", "ffn_train", 8192, 4096, 16384, "bf16", "silu"),
+        # one token through 16-bit weights: bound by reading them
+        _ffn("ffn_infer_f16_m1", "ffn_infer", 1, 2048, 8192, "f16", "silu"),
+        # one token, one square layer: the smallest call, where latency counts
+        _q4("q4_linear_bf16_m1", "q4_linear", 1, 4096, 4096, 64, "bf16"),
+        # one token through the wide block at 4 bits, smallest groups
+        _q4("q4_gated_f16_m1", "q4_gated", 1, 4096, 16384, 32, "f16"),
+        # a few tokens, odd sizes: a group and a tile that end early, rows of a wider tensor
+        _q4("q4_linear_bf16_ragged_m13", "q4_linear", 13, 5001, 4097, 128, "bf16", bias=True, wide=7),
+        # the ConvNet's first fully connected layer at 4 bits for a batch of 64
+        _q4("q4_linear_f16_m64", "q4_linear", 64, 8192, 1024, 64, "f16", bias=True),
+        # a prompt of 512 tokens through the wide block
+        _q4("q4_gated_bf16_m512", "q4_gated", 512, 4096, 16384, 128, "bf16"),
+        # ResNet-18's 62 gradients in fp32
+        dict(name="clip_f32_resnet18", kind="clip", tensors=62, values=11689512, arenas=62, dtype="f32", max_norm=1.0),
+        # a large model's gradients: 290 tensors of very different sizes in one buffer per layer
+        dict(name="clip_bf16_1e9", kind="clip", tensors=290, values=1000000007, arenas=32, dtype="bf16", max_norm=1.0),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(rng, lo, hi):
+    """A size over [lo, hi], spread over its logarithm: a third each multiples of 64, multiples of 8 and any."""
+    v, step = _log(rng, lo, hi), rng.choice((64, 8, 1))
+    return max(step, v // step * step)
+
+
+def draw(rng):
+    kind = rng.choice(["ffn_train", "ffn_train", "ffn_infer", "q4_linear", "q4_linear", "q4_gated", "clip"])
+    dtype = rng.choice(["f16", "bf16"])
+    if kind in ("ffn_train", "ffn_infer"):
+        k, f = _size(rng, 64, 8192), _size(rng, 64, 16384)
+        m = _size(rng, 1, 16384)
+        m = max(1, min(m, int(8192 * 4096 * 16384 / (k * f)), int(8192 * 16384 / f)))
+        c = _ffn("", kind, m, k, f, dtype, rng.choice(_ACTS), rng.choice((0, 0, 8, 5)))
+    elif kind != "clip":
+        k, n = _size(rng, 64, 16384), _size(rng, 16, 16384)
+        m = rng.choice([1, 1, rng.randint(2, 16), _log(rng, 1, 64), _log(rng, 16, 4096)])
+        m = max(1, min(m, int(512 * 4096 * 16384 / (k * n)) + 1))
+        c = _q4("", kind, m, k, n, rng.choice((32, 64, 128)), dtype, rng.choice(_ACTS), rng.random() < 0.5 and kind == "q4_linear",
+                rng.choice((0, 0, 8, 5)))
+    else:
+        t = _log(rng, 1, 600)
+        c = dict(name="", kind=kind, tensors=t, values=max(t, _log(rng, 1000, 500_000_000)), arenas=rng.randint(1, min(t, 60)),
+                 dtype=rng.choice(["f32", "f16", "bf16", "mixed"]), max_norm=rng.choice((1.0, 0.5, 1e6)))
+    del c["name"]
+    return c
+
+
+# ---------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------
+
+def _normal(gen, shape, std, dtype, wide=0):
+    """N(0, std^2) in the type; `wide` > 0: the leading columns of a tensor that has so many more."""
+    t = torch.randn((*shape[:-1], shape[-1] + wide), generator=gen, device=DEV, dtype=torch.float32)
+    return (t * std).to(dtype)[..., :shape[-1]]
+
+
+def _quantize(w, group):
+    """(codes [n][kp / 2], scales [n][kp / group]) of a weight [n][kp] in the documented format: E2M1 codes, code 2i in
+    the low half of byte i; scales are max / 6 in 7 significant bits, kept as bf16."""
+    n, kp = w.shape
+    g = w.view(n, kp // group, group)
+    s = g.abs().amax(-1) / 6.0
+    bits = s.view(torch.int32)
+    s = ((bits + 0xFFFF + ((bits >> 17) & 1)) & ~0x1FFFF).view(torch.float32)
+    mids = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], device=w.device)
+    mag = torch.bucketize((g.abs() / s.clamp_min(1e-38).unsqueeze(-1)), mids)
+    c = (mag + 8 * (g < 0)).to(torch.uint8).view(n, kp)
+    return (c[:, 0::2] | (c[:, 1::2] << 4)).contiguous(), s.to(torch.bfloat16)
+
+
+def _q4_weight(gen, n, k, group):
+    kp = -(-k // group) * group
+    w = torch.randn((n, kp), generator=gen, device=DEV, dtype=torch.float32) * k ** -0.5
+    w[:, k:] = 0.0
+    return _quantize(w, group)
+
+
+def _sizes(case):
+    """The number of values of each gradient: half of them small (norms, biases), the others share the rest unevenly."""
+    rng = random.Random(case["tensors"] * 1000003 + case["values"])
+    t, left = case["tensors"], case["values"]
+    small = [rng.randint(1, 1024) if i % 2 else 0 for i in range(t)]
+    if sum(small) >= left:
+        small = [0] * t
+    part = [0.0 if s else math.exp(rng.uniform(0.0, 3.0)) for s in small]
+    left -= sum(small)
+    got = [s or max(1, int(left * p / sum(part)) - 1) for s, p in zip(small, part)]
+    got[0] += case["values"] - sum(got) if case["values"] > sum(got) else 0
+    return got
+
+
+def _arenas(case):
+    """For each buffer its type and its gradients' (offset, values)."""
+    sizes, a = _sizes(case), case["arenas"]
+    kinds = ["f32", "bf16", "f16"] if case["dtype"] == "mixed" else [case["dtype"]]
+    return [(kinds[i % len(kinds)], sizes[i * len(sizes) // a:(i + 1) * len(sizes) // a]) for i in range(a)]
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    s = dict(case)
+    if case["kind"] in ("ffn_train", "ffn_infer"):
+        t, m, k, f = _T[case["dtype"]], case["m"], case["k"], case["f"]
+        s["x"] = _normal(gen, (m, k), 1.0, t, case["wide"])
+        s["w_gate"] = _normal(gen, (f, k), k ** -0.5, t)
+        s["w_up"] = _normal(gen, (f, k), k ** -0.5, t)
+        if case["kind"] == "ffn_train":
+            s["gh"] = _normal(gen, (m, f), 0.05, t)
+    elif case["kind"] != "clip":
+        t, m, k, n = _T[case["dtype"]], case["m"], case["k"], case["n"]
+        s["x"] = _normal(gen, (m, k), 1.0, t, case["wide"])
+        s["w"] = _q4_weight(gen, n, k, case["group"])
+        if case["kind"] == "q4_gated":
+            s["w_up"] = _q4_weight(gen, n, k, case["group"])
+        s["b"] = _normal(gen, (n,), 0.1, torch.float32) if case["bias"] else None
+    else:
+        s["grads"], s["out"], s["flat"] = [], [], []
+        for kind, sizes in _arenas(case):
+            # a gradient's scale differs from buffer to buffer
+            g = _normal(gen, (sum(sizes),), math.exp(-1.0 - len(s["flat"]) % 7), _T[kind])
+            o = torch.empty_like(g)
+            s["grads"] += torch.split(g, sizes)
+            s["out"] += torch.split(o, sizes)
+            s["flat"].append(o)
+    return s
+
+
+# ---------------------------------------------------------------------------
+# the plain forms, in fp32
+# ---------------------------------------------------------------------------
+
+def _act(g, act):
+    if act == "silu":
+        return g / (1.0 + torch.exp(-g))
+    if act == "gelu":
+        return 0.5 * g * (1.0 + torch.erf(g * 0.5 ** 0.5))
+    return g.clamp_min(0.0)
+
+
+def _act_grad(g, act):
+    if act == "silu":
+        p = 1.0 / (1.0 + torch.exp(-g))
+        return p * (1.0 + g * (1.0 - p))
+    if act == "gelu":
+        return 0.5 * (1.0 + torch.erf(g * 0.5 ** 0.5)) + g * torch.exp(-0.5 * g * g) * (2.0 * math.pi) ** -0.5
+    return (g > 0).to(g.dtype)
+
+
+def _plain_ffn(s):
+    t = s["x"].dtype
+    x, wg, wu = s["x"].float(), s["w_gate"].float(), s["w_up"].float()
+    g, u = x @ wg.t(), x @ wu.t()
+    a = _act(g, s["act"])
+    h = (a * u).to(t)
+    if s["kind"] == "ffn_infer":
+        return h
+    gh = s["gh"].float()
+    dg, du = gh * u * _act_grad(g, s["act"]), gh * a
+    return h, (dg @ wg + du @ wu).to(t), (dg.t() @ x).to(t), (du.t() @ x).to(t)
+
+
+_LEVELS = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0]
+
+
+def _plain_weight(w, k):
+    codes, scales = w
+    lut = torch.tensor(_LEVELS, device=codes.device)
+    v = lut[torch.stack((codes & 15, codes >> 4), -1).flatten(1).int()]
+    return (v * scales.float().repeat_interleave(v.shape[1] // scales.shape[1], 1))[:, :k]
+
+
+def _plain_q4(s):
+    x, k = s["x"].float(), s["k"]
+    y = x @ _plain_weight(s["w"], k).t()
+    if s["kind"] == "q4_gated":
+        y = _act(y, s["act"]) * (x @ _plain_weight(s["w_up"], k).t())
+    elif s["b"] is not None:
+        y = y + s["b"]
+    return y.to(s["x"].dtype)
+
+
+def _plain_clip(s):
+    norm = torch.stack([g.float().square().sum() for g in s["grads"]]).sum().sqrt()
+    c = torch.where(norm > s["max_norm"], s["max_norm"] / norm, torch.ones_like(norm))
+    [o.copy_(g.float() * c) for o, g in zip(s["out"], s["grads"])]
+    return norm, s["flat"]
+
+
+# ---------------------------------------------------------------------------
+# one pass
+# ---------------------------------------------------------------------------
+
+def _own(s):
+    import paper_2003_04296_amd as q
+
+    if s["kind"] == "clip":
+        return q.aqe_clip_grads(s["grads"], s["max_norm"], out=s["out"]), s["flat"]
+    act = {"silu": q.ACT_SILU, "gelu": q.ACT_GELU, "relu": q.ACT_RELU}[s["act"]]
+    if s["kind"] == "ffn_infer":
+        return q.ffn_forward(s["x"], s["w_gate"], s["w_up"], act)[0]
+    if s["kind"] == "ffn_train":
+        h, pre = q.ffn_forward(s["x"], s["w_gate"], s["w_up"], act, keep_pre=True)
+        return (h, *q.ffn_backward(s["x"], s["w_gate"], s["w_up"], pre, s["gh"], act))
+    if s["kind"] == "q4_gated":
+        return q.q4_gated(s["x"], *s["w"], *s["w_up"], act)
+    return q.q4_linear(s["x"], *s["w"], bias=s["b"])
+
+
+def run(state):
+    if own:
+        return _own(state)
+    return {"clip": _plain_clip, "q4_linear": _plain_q4, "q4_gated": _plain_q4}.get(state["kind"], _plain_ffn)(state)
+
+
+def work(case):
+    if case["kind"] == "clip":
+        # the gradients are read, and written scaled; a square, a sum and a product each
+        return {"bytes": sum(2 * _SIZE[t] * sum(n) for t, n in _arenas(case)), "flops": 3 * case["values"]}
+    m, k = case["m"], case["k"]
+    if case["kind"] in ("q4_linear", "q4_gated"):
+        n, two = case["n"], 2 if case["kind"] == "q4_gated" else 1
+        kp = -(-k // case["group"]) * case["group"]
+        w = n * (kp // 2 + 2 * (kp // case["group"])) * two
+        return {"bytes": w + 2 * m * k + 2 * m * n + (4 * n if case["bias"] else 0), "flops": 2 * m * n * k * two}
+    f = case["f"]
+    if case["kind"] == "ffn_infer":
+        return {"bytes": 2 * (m * k + 2 * f * k + m * f), "flops": 4 * m * k * f}
+    # x, both weights and gh in; h and the gradients of x and both weights out
+    return {"bytes": 2 * (2 * m * k + 4 * f * k + 2 * m * f), "flops": 12 * m * k * f}
+
+
+# ---------------------------------------------------------------------------
+# the definition, in 64 bits
+# ---------------------------------------------------------------------------
+
+def _exact_gate(g, act):
+    """act(g) and its derivative."""
+    if act == "relu":
+        on = (g > 0).double()
+        return g * on, on
+    if act == "silu":
+        p = torch.sigmoid(g)
+        return g * p, p + g * p * (1 - p)
+    cdf = 0.5 * torch.erfc(-g / math.sqrt(2.0))
+    return g * cdf, cdf + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+
+
+def _exact_weight(w, k):
+    codes, scales = (v.to(torch.int32) if v.dtype == torch.uint8 else v.double() for v in w)
+    n, half = codes.shape
+    c = torch.empty((n, 2 * half), dtype=torch.int32, device=codes.device)
+    c[:, 0::2], c[:, 1::2] = codes % 16, codes // 16
+    e, f = (c % 8) // 2, (c % 2).double()
+    mag = torch.where(e == 0, 0.5 * f, (1 + 0.5 * f) * torch.exp2(e.double() - 1))
+    v = torch.where(c >= 8, -mag, mag).view(n, scales.shape[1], -1) * scales.unsqueeze(-1)
+    return v.reshape(n, 2 * half)[:, :k]
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "clip":
+        total = sum(float(g.double().square().sum()) for g in s["grads"])
+        norm = math.sqrt(total)
+        c = case["max_norm"] / norm if norm > case["max_norm"] else 1.0
+        at, flat = 0, []
+        for _, sizes in _arenas(case):
+            flat.append(torch.cat([g.double() * c for g in s["grads"][at:at + len(sizes)]]))
+            at += len(sizes)
+        return torch.tensor(norm, dtype=torch.float64), flat
+    x = s["x"].double()
+    if case["kind"] in ("q4_linear", "q4_gated"):
+        y = torch.mm(x, _exact_weight(s["w"], case["k"]).t().contiguous())
+        if case["kind"] == "q4_gated":
+            return _exact_gate(y, case["act"])[0] * torch.mm(x, _exact_weight(s["w_up"], case["k"]).t().contiguous())
+        return y if s["b"] is None else y + s["b"].double()
+    wg, wu = s["w_gate"].double(), s["w_up"].double()
+    g, u = torch.mm(x, wg.t().contiguous()), torch.mm(x, wu.t().contiguous())
+    a, da = _exact_gate(g, case["act"])
+    if case["kind"] == "ffn_infer":
+        return a * u
+    gh = s["gh"].double()
+    dg, du = gh * u * da, gh * a
+    return (a * u, torch.mm(dg, wg) + torch.mm(du, wu), torch.mm(dg.t().contiguous(), x),
+            torch.mm(du.t().contiguous(), x))

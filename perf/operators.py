@@ -114,12 +114,12 @@ def _normal(gen, shape, std, dtype, wide=0):
 
 def _quantize(w, group):
     """(codes [n][kp / 2], scales [n][kp / group]) of a weight [n][kp] in the documented format: E2M1 codes, code 2i in
-    the low half of byte i; scales are max / 6 in 7 significant bits, kept as bf16."""
+    the low half of byte i; scales are max / 6 in 6 significant bits, kept as bf16."""
     n, kp = w.shape
     g = w.view(n, kp // group, group)
     s = g.abs().amax(-1) / 6.0
     bits = s.view(torch.int32)
-    s = ((bits + 0xFFFF + ((bits >> 17) & 1)) & ~0x1FFFF).view(torch.float32)
+    s = ((bits + 0x1FFFF + ((bits >> 18) & 1)) & ~0x3FFFF).view(torch.float32)
     mids = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], device=w.device)
     mag = torch.bucketize((g.abs() / s.clamp_min(1e-38).unsqueeze(-1)), mids)
     c = (mag + 8 * (g < 0)).to(torch.uint8).view(n, kp)

@@ -290,6 +290,111 @@ int aqe_backward(const float* x, const float* gy, int64_t n, float alpha, float*
 int aqe_sgd_clip(float* w, const float* g, int64_t n, float lr, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Fully connected operators: the gated feed-forward block with its gradients */
+/* and products with 4-bit weights.  Tensors are row-major with unit column   */
+/* stride and a row stride (ld, in elements) of at least the columns; any     */
+/* address a value may have is allowed, 16-byte aligned rows are faster.      */
+/* All sums run in fp32; results are rounded once to the tensors' type.       */
+/* ------------------------------------------------------------------------ */
+typedef enum { QCONV_F32 = 0, QCONV_F16 = 1, QCONV_BF16 = 2 } qconv_dtype;
+
+typedef enum {
+  QCONV_ACT_SILU = 0, /* g / (1 + exp(-g))              */
+  QCONV_ACT_GELU = 1, /* g (1 + erf(g / sqrt(2))) / 2   */
+  QCONV_ACT_RELU = 2  /* max(g, 0), slope 0 at 0        */
+} qconv_act;
+
+typedef struct {
+  int m, k, f;              /* tokens, input features, hidden features           */
+  int dtype;                /* QCONV_F16 or QCONV_BF16: every tensor but pre     */
+  int act;                  /* qconv_act                                         */
+  int64_t ld_x, ld_w, ld_h; /* row strides of x, of both weights, of h and of gh */
+} qconv_ffn_desc;
+
+/* Floats of the `pre` buffer: [m][2][fp] with fp = f rounded up to 8. */
+size_t qconv_ffn_pre_floats(int m, int f);
+
+/* h[m][f] = act(g) * u with g = x w_gate^T, u = x w_up^T; x[m][k],
+ * w_gate[f][k], w_up[f][k].  pre (NULL to leave it out) receives g in
+ * [m][0][0..f) and u in [m][1][0..f) for the backward pass; what lies past f
+ * in a row is not written.  m == 0 launches nothing. */
+int qconv_ffn_forward(const qconv_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, void* h,
+                      float* pre, void* stream);
+
+/* Workspace of qconv_ffn_backward. */
+size_t qconv_ffn_backward_bytes(const qconv_ffn_desc* d);
+
+/* From gh[m][f] (the gradient of h) and the forward's pre:
+ *   dg = gh u act'(g), du = gh act(g), rounded to the tensors' type, then
+ *   gx[m][k] = dg w_gate + du w_up,  gw_gate[f][k] = dg^T x,  gw_up[f][k] = du^T x.
+ * gx, and gw_gate together with gw_up, may be NULL to leave them out; they
+ * are contiguous.  m == 0 gives zero weight gradients.  workspace: 16-byte
+ * aligned, at least qconv_ffn_backward_bytes. */
+int qconv_ffn_backward(const qconv_ffn_desc* d, const void* x, const void* w_gate, const void* w_up,
+                       const float* pre, const void* gh, void* gx, void* gw_gate, void* gw_up, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* 4-bit weights.  A matrix w[n][k] is kept as E2M1 codes and one scale per
+ * `group` (32, 64 or 128) consecutive values of a row:
+ *   codes : bytes [n][kp / 2], kp = k rounded up to the group; the low half of
+ *           byte i holds value 2i.  Bit 3 is the sign, bits 0..2 select the
+ *           magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (the matrix cores' fp4, which
+ *           holds every 1..3-bit level of this library exactly).  Codes past
+ *           k are 0.
+ *   scales: bf16 [n][kp / group];  w = scale * magnitude.
+ * Both buffers are 16-byte aligned.
+ * Packing: scale = max|w| of the group / top, rounded to 6 significant bits
+ * (to nearest, ties to even), so that scale * magnitude is exact in bf16; each
+ * value takes the nearest magnitude of |w| / scale, a tie the smaller one.
+ * top = 6 uses every magnitude; top = 4 maps the levels 0, +-1/4, +-1/2, +-1
+ * of 3-bit weights (and of 1 and 2 bits) to themselves wherever the group
+ * holds a +-1.  A group that holds an inf or NaN gets a NaN scale. */
+size_t qconv_q4_code_bytes(int n, int k, int group);
+size_t qconv_q4_scale_bytes(int n, int k, int group);
+int qconv_q4_pack(const void* w, int dtype, int n, int k, int64_t ld_w, int group, int top, uint8_t* codes,
+                  uint16_t* scales, void* stream);
+
+typedef struct {
+  int m, n, k;        /* tokens, outputs, inputs                  */
+  int group;          /* 32, 64 or 128                            */
+  int dtype;          /* QCONV_F16 or QCONV_BF16: x and y         */
+  int64_t ld_x, ld_y; /* row strides of x and y                   */
+} qconv_q4_desc;
+
+/* Workspace of the two products below (0 where they need none). */
+size_t qconv_q4_workspace_bytes(const qconv_q4_desc* d, int gated);
+
+/* y[m][n] = x[m][k] w^T + bias[n] (fp32, NULL for none); the weights are used
+ * exactly (no rounding of scale * magnitude).  m == 0 launches nothing. */
+int qconv_q4_linear(const qconv_q4_desc* d, const void* x, const uint8_t* codes, const uint16_t* scales,
+                    const float* bias, void* y, void* workspace, size_t workspace_bytes, void* stream);
+
+/* y[m][n] = act(x w_gate^T) * (x w_up^T): the gated block on 4-bit weights. */
+int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_codes, const uint16_t* gate_scales,
+                   const uint8_t* up_codes, const uint16_t* up_scales, int act, void* y, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* The norm over all gradients of a model, and clipping by it                */
+/* ------------------------------------------------------------------------ */
+
+/* grads (host array of `count` device pointers), numel (host), dtypes (host;
+ * qconv_dtype each).  norm (device float) receives sqrt(sum of all squares),
+ * summed in fp64 in an order that the sizes alone fix. count == 0 and tensors
+ * of no values are allowed (a null pointer is, with numel 0). */
+size_t aqe_grad_norm_bytes(int count, const int64_t* numel);
+int aqe_grad_norm(int count, const void* const* grads, const int64_t* numel, const int* dtypes, float* norm,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norm as above, then out_t = c * grad_t with c = max_norm / norm where
+ * norm > max_norm and 1 otherwise (a NaN norm leaves the values as they are;
+ * an infinite one gives c = 0); c is rounded to fp32, the product to the
+ * tensor's type.  out[t] may be grads[t] itself (clipping in place) or a
+ * tensor that overlaps no gradient.  max_norm >= 0. */
+int aqe_clip_grads(int count, const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes,
+                   float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Whole networks (Algorithm 1, inference branch, layer by layer)            */
 /* ------------------------------------------------------------------------ */
 

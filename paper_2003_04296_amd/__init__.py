@@ -19,6 +19,8 @@ ALGO_AUTO, ALGO_BITPLANE, ALGO_MFMA_I8, ALGO_MFMA_FP4, ALGO_MFMA_F16 = 0, 1, 2, 
 EPI_INT32, EPI_SCALE_F32, EPI_BN_F32, EPI_BN_PACK = 0, 1, 2, 3
 EPI_POOL2, EPI_RESIDUAL = 1, 2
 F32_FMAF_CHAIN, F32_MFMA, F32_BF16X6 = 0, 1, 2
+DT_F32, DT_F16, DT_BF16 = 0, 1, 2
+ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
 OP_NAMES = {1: "XNOR", 2: "SHIFT", 3: "XNOR-ADDER", 4: "SHIFT-ADDER", 5: "MAC"}
 
 EXPORTED = (
@@ -31,6 +33,9 @@ EXPORTED = (
     "qnet_layer_kernel",
     "qnet_tensor_info", "qconv_resolve_algo",
     "qconv_kernel_name", "aqe_forward", "aqe_backward", "aqe_sgd_clip",
+    "qconv_ffn_pre_floats", "qconv_ffn_forward", "qconv_ffn_backward_bytes", "qconv_ffn_backward",
+    "qconv_q4_code_bytes", "qconv_q4_scale_bytes", "qconv_q4_pack", "qconv_q4_workspace_bytes", "qconv_q4_linear",
+    "qconv_q4_gated", "aqe_grad_norm_bytes", "aqe_grad_norm", "aqe_clip_grads",
 )
 
 
@@ -50,6 +55,16 @@ class qconv_epilogue(ctypes.Structure):
     _fields_ = [("mode", ctypes.c_int), ("flags", ctypes.c_int), ("scale", ctypes.c_void_p),
                 ("bn_k", ctypes.c_void_p), ("bn_b", ctypes.c_void_p), ("residual", ctypes.c_void_p),
                 ("out_bits", ctypes.c_int), ("out_thresholds", ctypes.c_void_p)]
+
+
+class qconv_ffn_desc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("m", "k", "f", "dtype", "act")] + \
+               [(name, ctypes.c_int64) for name in ("ld_x", "ld_w", "ld_h")]
+
+
+class qconv_q4_desc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("m", "n", "k", "group", "dtype")] + \
+               [(name, ctypes.c_int64) for name in ("ld_x", "ld_y")]
 
 
 _lib = None
@@ -90,6 +105,26 @@ def lib() -> ctypes.CDLL:
     L.aqe_forward.argtypes = [vp, i64, i32, f32, vp, vp, i64, vp, vp]
     L.aqe_backward.argtypes = [vp, vp, i64, f32, vp, vp]
     L.aqe_sgd_clip.argtypes = [vp, vp, i64, f32, vp]
+    ffn, q4 = ctypes.POINTER(qconv_ffn_desc), ctypes.POINTER(qconv_q4_desc)
+    L.qconv_ffn_pre_floats.restype = sz
+    L.qconv_ffn_pre_floats.argtypes = [i32, i32]
+    L.qconv_ffn_forward.argtypes = [ffn] + [vp] * 6
+    L.qconv_ffn_backward_bytes.restype = sz
+    L.qconv_ffn_backward_bytes.argtypes = [ffn]
+    L.qconv_ffn_backward.argtypes = [ffn] + [vp] * 9 + [sz, vp]
+    L.qconv_q4_code_bytes.restype = sz
+    L.qconv_q4_code_bytes.argtypes = [i32] * 3
+    L.qconv_q4_scale_bytes.restype = sz
+    L.qconv_q4_scale_bytes.argtypes = [i32] * 3
+    L.qconv_q4_pack.argtypes = [vp, i32, i32, i32, i64, i32, i32, vp, vp, vp]
+    L.qconv_q4_workspace_bytes.restype = sz
+    L.qconv_q4_workspace_bytes.argtypes = [q4, i32]
+    L.qconv_q4_linear.argtypes = [q4] + [vp] * 6 + [sz, vp]
+    L.qconv_q4_gated.argtypes = [q4] + [vp] * 5 + [i32] + [vp] * 2 + [sz, vp]
+    L.aqe_grad_norm_bytes.restype = sz
+    L.aqe_grad_norm_bytes.argtypes = [i32, vp]
+    L.aqe_grad_norm.argtypes = [i32] + [vp] * 5 + [sz, vp]
+    L.aqe_clip_grads.argtypes = [i32] + [vp] * 4 + [f32, vp, vp, sz, vp]
     L.qnet_create.restype = vp
     L.qnet_create.argtypes = [i32, i32, i32]
     L.qnet_destroy.argtypes = [vp]
@@ -244,6 +279,275 @@ def aqe_sgd_clip(w, g, lr: float, stream=None):
     """In place: w = clip(w - lr g, -1, 1)."""
     _check(lib().aqe_sgd_clip(_ptr(w), _ptr(g), w.numel(), float(lr), _stream(stream)), "aqe_sgd_clip")
     return w
+
+
+# ---------------------------------------------------------------------------
+# Fully connected operators and the gradient norm
+# ---------------------------------------------------------------------------
+
+_dtypes = None
+
+
+def _new(shape, dtype, like, stream):
+    """A new tensor that belongs to the stream the kernels run on (freed memory
+    is handed out again in that stream's order)."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _on_gpu(t, what: str):
+    if not t.is_cuda:
+        raise ValueError(f"{what}: tensors are on the GPU, got one on {t.device}")
+
+
+def _dtype_code(t) -> int:
+    """DT_* of a tensor (-1 for other types)."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+
+        _dtypes = {torch.float32: DT_F32, torch.float16: DT_F16, torch.bfloat16: DT_BF16}
+    return _dtypes.get(t.dtype, -1)
+
+
+def _rows(t, rows, cols, like, what: str) -> int:
+    """Row stride of a matrix [rows][cols] (rows None: any) with unit column
+    stride, of the type and on the device of `like`."""
+    s = t.shape
+    if len(s) != 2 or s[1] != cols or (rows is not None and s[0] != rows):
+        raise ValueError(f"{what}: shape {tuple(s)}, expected ({'m' if rows is None else rows}, {cols})")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError(f"{what}: columns must be contiguous (strides {t.stride()})")
+    if s[0] <= 1:
+        return cols  # no second row
+    if ld < cols:
+        raise ValueError(f"{what}: row stride {ld} is below the {cols} columns")
+    return ld
+
+
+def _workspace(ws, nbytes: int, like, what: str, stream):
+    """The caller's workspace (checked on the C side for its size) or a new one."""
+    if ws is None and nbytes:
+        import torch
+
+        ws = _new(nbytes, torch.uint8, like, stream)
+    if ws is None:
+        return None, 0
+    if ws.device != like.device or not ws.is_contiguous():
+        raise ValueError(f"{what}: the workspace is a contiguous tensor on {like.device}")
+    return ws, ws.numel() * ws.element_size()
+
+
+def _ffn_desc(x, w_gate, w_up, act, h, what):
+    if x.dim() != 2 or w_gate.dim() != 2:
+        raise ValueError(f"{what}: x and the weights are matrices")
+    _on_gpu(x, what)
+    m, k = x.shape
+    f = w_gate.shape[0]
+    ld_w = _rows(w_gate, f, k, x, f"{what} w_gate")
+    if _rows(w_up, f, k, x, f"{what} w_up") != ld_w:
+        raise ValueError(f"{what}: w_gate and w_up have different row strides")
+    return qconv_ffn_desc(m, k, f, _dtype_code(x), act, _rows(x, m, k, x, f"{what} x"), ld_w,
+                          _rows(h, m, f, x, f"{what} h"))
+
+
+def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pre=None, out=None, stream=None):
+    """h = act(x w_gate^T) * (x w_up^T) for 16-bit x [m][k] and weights [f][k]
+    -> (h [m][f], pre).  keep_pre (or a buffer `pre` of a former call) keeps
+    what ffn_backward needs, else pre is None."""
+    import torch
+
+    _on_gpu(x, "ffn_forward")
+    m, f = x.shape[0], w_gate.shape[0]
+    h = _new((m, f), x.dtype, x, stream) if out is None else out
+    d = _ffn_desc(x, w_gate, w_up, act, h, "ffn_forward")
+    if keep_pre and pre is None:
+        pre = _new(lib().qconv_ffn_pre_floats(m, f), torch.float32, x, stream)
+    elif pre is not None:
+        _check_pre(pre, m, f, x, "ffn_forward")
+    _check(lib().qconv_ffn_forward(ctypes.byref(d), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(h), _ptr(pre),
+                                   _stream(stream)), "qconv_ffn_forward")
+    return h, pre
+
+
+def _check_pre(pre, m, f, like, what):
+    import torch
+
+    if pre.dtype != torch.float32 or pre.device != like.device or not pre.is_contiguous() or \
+            pre.numel() < lib().qconv_ffn_pre_floats(m, f):
+        raise ValueError(f"{what}: pre holds at least {lib().qconv_ffn_pre_floats(m, f)} contiguous fp32 values")
+
+
+def ffn_backward(x, w_gate, w_up, pre, gh, act: int = ACT_SILU, need_x: bool = True, need_w: bool = True, out=None,
+                 workspace=None, stream=None):
+    """From gh [m][f] and the forward's pre -> (gx [m][k], gw_gate [f][k],
+    gw_up [f][k]) in x's type; None for what need_x / need_w leave out.  out:
+    contiguous tensors to write instead of new ones."""
+    d = _ffn_desc(x, w_gate, w_up, act, gh, "ffn_backward")
+    m, k, f = d.m, d.k, d.f
+    _check_pre(pre, m, f, x, "ffn_backward")
+    gx, gg, gu = out if out is not None else (None, None, None)
+    shapes = [(m, k), (f, k), (f, k)]
+    for i, (t, need) in enumerate(zip((gx, gg, gu), (need_x, need_w, need_w))):
+        if t is not None and (not t.is_contiguous() or _rows(t, *shapes[i], x, "ffn_backward out") != k):
+            raise ValueError("ffn_backward: out tensors are contiguous")
+    new = lambda t, need, s: (_new(s, x.dtype, x, stream) if t is None else t) if need else None
+    gx, gg, gu = new(gx, need_x, shapes[0]), new(gg, need_w, shapes[1]), new(gu, need_w, shapes[2])
+    ws, nbytes = _workspace(workspace, lib().qconv_ffn_backward_bytes(ctypes.byref(d)), x, "ffn_backward", stream)
+    _check(lib().qconv_ffn_backward(ctypes.byref(d), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(pre), _ptr(gh), _ptr(gx),
+                                    _ptr(gg), _ptr(gu), _ptr(ws), nbytes, _stream(stream)), "qconv_ffn_backward")
+    return gx, gg, gu
+
+
+def q4_pack(w, group: int = 64, top: int = 6, out=None, stream=None):
+    """A matrix [n][k] (fp32 or 16-bit) -> (codes uint8 [n][kp / 2], scales
+    bf16 [n][kp / group]): 4-bit E2M1 codes with a scale per `group` values of
+    a row; top: the magnitude a group's largest value maps to (6, or 4 for
+    weights that sit on the levels of 1..3 bits)."""
+    import torch
+
+    if w.dim() != 2:
+        raise ValueError("q4_pack: w is a matrix")
+    _on_gpu(w, "q4_pack")
+    n, k = w.shape
+    ld = _rows(w, n, k, w, "q4_pack")
+    if out is None:
+        cb, sb = lib().qconv_q4_code_bytes(n, k, group), lib().qconv_q4_scale_bytes(n, k, group)
+        out = (_new((n, cb // n if n else 0), torch.uint8, w, stream),
+               _new((n, sb // (2 * n) if n else 0), torch.bfloat16, w, stream))
+    else:
+        _q4_group(*out, n, k, w.device, "q4_pack", group)
+    codes, scales = out
+    _check(lib().qconv_q4_pack(_ptr(w), _dtype_code(w), n, k, ld, group, top, _ptr(codes), _ptr(scales),
+                               _stream(stream)), "qconv_q4_pack")
+    return codes, scales
+
+
+def _q4_group(codes, scales, n, k, device, what, group=None) -> int:
+    """The group size of packed weights [n][k], their buffers checked against it."""
+    import torch
+
+    if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16 or codes.device != device or \
+            scales.device != device or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError(f"{what}: codes are uint8 and scales bf16, contiguous, on {device}")
+    cs, ss = codes.shape, scales.shape
+    if group is None:
+        group = 2 * cs[1] // ss[1] if len(cs) == 2 and len(ss) == 2 and ss[1] else 0
+    if group not in (32, 64, 128):
+        raise ValueError(f"{what}: groups of {group} values (32, 64 and 128 are supported)")
+    groups = (k + group - 1) // group
+    if tuple(cs) != (n, groups * group // 2) or tuple(ss) != (n, groups):
+        raise ValueError(f"{what}: codes {tuple(cs)} and scales {tuple(ss)} are not those of a ({n}, {k}) weight")
+    return group
+
+
+def _q4_desc(x, codes, scales, out, what, stream):
+
+    if x.dim() != 2 or codes.dim() != 2:
+        raise ValueError(f"{what}: x and codes are matrices")
+    _on_gpu(x, what)
+    m, k = x.shape
+    n = codes.shape[0]
+    y = _new((m, n), x.dtype, x, stream) if out is None else out
+    group = _q4_group(codes, scales, n, k, x.device, what)
+    return qconv_q4_desc(m, n, k, group, _dtype_code(x), _rows(x, m, k, x, f"{what} x"),
+                         _rows(y, m, n, x, f"{what} out")), y
+
+
+def q4_linear(x, codes, scales, bias=None, out=None, workspace=None, stream=None):
+    """y [m][n] = x [m][k] w^T + bias with 4-bit weights (q4_pack); x and y
+    fp16 or bf16, bias fp32 [n]."""
+    import torch
+
+    d, y = _q4_desc(x, codes, scales, out, "q4_linear", stream)
+    if bias is not None and (bias.dtype != torch.float32 or bias.device != x.device or tuple(bias.shape) != (d.n,)
+                             or not bias.is_contiguous()):
+        raise ValueError(f"q4_linear: bias is a contiguous fp32 vector of {d.n} on {x.device}")
+    ws, nbytes = _workspace(workspace, lib().qconv_q4_workspace_bytes(ctypes.byref(d), 0), x, "q4_linear", stream)
+    _check(lib().qconv_q4_linear(ctypes.byref(d), _ptr(x), _ptr(codes), _ptr(scales), _ptr(bias), _ptr(y), _ptr(ws),
+                                 nbytes, _stream(stream)), "qconv_q4_linear")
+    return y
+
+
+def q4_gated(x, gate_codes, gate_scales, up_codes, up_scales, act: int = ACT_SILU, out=None, workspace=None,
+             stream=None):
+    """h [m][n] = act(x w_gate^T) * (x w_up^T) with 4-bit weights."""
+    d, y = _q4_desc(x, gate_codes, gate_scales, out, "q4_gated", stream)
+    if _q4_group(up_codes, up_scales, d.n, d.k, x.device, "q4_gated up") != d.group:
+        raise ValueError("q4_gated: gate and up weights have different groups")
+    ws, nbytes = _workspace(workspace, lib().qconv_q4_workspace_bytes(ctypes.byref(d), 1), x, "q4_gated", stream)
+    _check(lib().qconv_q4_gated(ctypes.byref(d), _ptr(x), _ptr(gate_codes), _ptr(gate_scales), _ptr(up_codes),
+                                _ptr(up_scales), act, _ptr(y), _ptr(ws), nbytes, _stream(stream)), "qconv_q4_gated")
+    return y
+
+
+def _dense(t) -> bool:
+    """Whether a tensor's values fill one range of memory, in any order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for size, stride in sorted(((s, st) for s, st in zip(t.shape, t.stride()) if s != 1), key=lambda v: v[1]):
+        if stride != want:
+            return False
+        want *= size
+    return True
+
+
+def _grad_arrays(grads, what):
+    """(count, pointers, sizes, types) of a list of gradients as C arrays."""
+    n = len(grads)
+    dev = grads[0].device if n else None
+    types = [_dtype_code(g) for g in grads]
+    if n:
+        _on_gpu(grads[0], what)
+    if any(g.device != dev or not _dense(g) for g in grads) or -1 in types:
+        raise ValueError(f"{what}: gradients are dense fp32, fp16 or bf16 tensors on one device")
+    return (n, (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]),
+            (ctypes.c_int64 * n)(*[g.numel() for g in grads]), (ctypes.c_int * n)(*types))
+
+
+def _norm_out(grads, norm, what, stream):
+    import torch
+
+    if norm is None:
+        return _new((), torch.float32, grads[0] if len(grads) else torch.empty(0, device="cuda"), stream)
+    if norm.dtype != torch.float32 or norm.numel() != 1 or (len(grads) and norm.device != grads[0].device):
+        raise ValueError(f"{what}: norm is one fp32 value on the gradients' device")
+    return norm
+
+
+def aqe_grad_norm(grads, norm=None, workspace=None, stream=None):
+    """The 2-norm over all values of a list of gradients, as a device scalar."""
+    n, ptrs, sizes, types = _grad_arrays(grads, "aqe_grad_norm")
+    norm = _norm_out(grads, norm, "aqe_grad_norm", stream)
+    ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, sizes), norm, "aqe_grad_norm", stream)
+    _check(lib().aqe_grad_norm(n, ptrs, sizes, types, _ptr(norm), _ptr(ws), nbytes, _stream(stream)), "aqe_grad_norm")
+    return norm
+
+
+def aqe_clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, stream=None):
+    """Scale a list of gradients so that their joint norm is at most max_norm,
+    in place or into the tensors of `out` (same types and layouts); returns
+    the norm before, as a device scalar."""
+    n, ptrs, sizes, types = _grad_arrays(grads, "aqe_clip_grads")
+    outs = ptrs
+    if out is not None:
+        if len(out) != n or any(o.shape != g.shape or o.stride() != g.stride() or o.dtype != g.dtype or
+                                o.device != g.device for o, g in zip(out, grads)):
+            raise ValueError("aqe_clip_grads: out holds one tensor per gradient, of its shape, strides, type and device")
+        outs = (ctypes.c_void_p * n)(*[o.data_ptr() for o in out])
+    norm = _norm_out(grads, norm, "aqe_clip_grads", stream)
+    ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, sizes), norm, "aqe_clip_grads", stream)
+    _check(lib().aqe_clip_grads(n, ptrs, outs, sizes, types, float(max_norm), _ptr(norm), _ptr(ws), nbytes,
+                                _stream(stream)), "aqe_clip_grads")
+    return norm
 
 
 def fold_bn(gamma, beta, mean, var, eps):

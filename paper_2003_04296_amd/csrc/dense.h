@@ -1,0 +1,105 @@
+// dense.h -- what the fully connected operators share (gated feed-forward
+// block, 4-bit products): 16-bit types, the matrix instruction, activations,
+// loads from any address, and the launchers behind the C ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/qconv.h"
+
+namespace qc {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+
+// The two 16-bit types behind one set of names: the kernels move 16-bit
+// patterns and only the matrix instruction and the conversions know which.
+struct F16 {
+  __device__ __forceinline__ static float up(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
+  __device__ __forceinline__ static uint16_t down(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+  // D[16 rows of a][16 rows of b] += a b^T over 32 products
+  __device__ __forceinline__ static v4f mfma(v4u a, v4u b, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+  // the two E2M1 codes in byte BYTE of w as 16-bit values (exact)
+  template <int BYTE>
+  __device__ __forceinline__ static uint32_t from_e2m1(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, BYTE));
+  }
+};
+struct BF16 {
+  __device__ __forceinline__ static float up(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+  __device__ __forceinline__ static uint16_t down(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+  __device__ __forceinline__ static v4f mfma(v4u a, v4u b, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+  }
+  template <int BYTE>
+  __device__ __forceinline__ static uint32_t from_e2m1(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, BYTE));
+  }
+};
+
+// Eight 16-bit values from any 2-byte address (global loads take them).
+struct __attribute__((packed, aligned(2))) U128 {
+  v4u v;
+};
+__device__ __forceinline__ v4u load8(const uint16_t* p) { return reinterpret_cast<const U128*>(p)->v; }
+
+// The first `n` of eight values at p, +0 for the rest; n <= 0 reads nothing.
+// No byte past p[n - 1] is touched.
+__device__ __forceinline__ v4u load8_first(const uint16_t* p, int n) {
+  if (n >= 8) return load8(p);
+  v4u r = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) r[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+  return r;
+}
+
+// act(g) and act'(g) in fp32.  exp(-g) = inf gives silu 0 and slope 0.
+template <int ACT>
+__device__ __forceinline__ float act_value(float g) {
+  if constexpr (ACT == QCONV_ACT_SILU) return g / (1.0f + expf(-g));
+  if constexpr (ACT == QCONV_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+  return g < 0.0f ? 0.0f : g;  // a NaN stays
+}
+template <int ACT>
+__device__ __forceinline__ float act_slope(float g) {
+  if constexpr (ACT == QCONV_ACT_SILU) {
+    const float p = 1.0f / (1.0f + expf(-g));
+    return p * (1.0f + g * (1.0f - p));
+  }
+  if constexpr (ACT == QCONV_ACT_GELU)
+    return 0.5f * (1.0f + erff(g * 0.70710678118654752f)) + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+  return g > 0.0f ? 1.0f : 0.0f;
+}
+__device__ __forceinline__ float act_value(int act, float g) {
+  return act == QCONV_ACT_SILU ? act_value<QCONV_ACT_SILU>(g)
+                               : act == QCONV_ACT_GELU ? act_value<QCONV_ACT_GELU>(g) : act_value<QCONV_ACT_RELU>(g);
+}
+
+inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+int launch_ffn_forward(const qconv_ffn_desc& d, const void* x, const void* wg, const void* wu, void* h, float* pre,
+                       hipStream_t s);
+size_t ffn_backward_bytes(const qconv_ffn_desc& d);
+int launch_ffn_backward(const qconv_ffn_desc& d, const void* x, const void* wg, const void* wu, const float* pre,
+                        const void* gh, void* gx, void* gwg, void* gwu, void* ws, hipStream_t s);
+
+int launch_q4_pack(const void* w, int dtype, int n, int k, int64_t ld, int group, int top, uint8_t* codes,
+                   uint16_t* scales, hipStream_t s);
+// wu / su NULL: y = x W^T + bias; else the gated form.
+int launch_q4(const qconv_q4_desc& d, const void* x, const uint8_t* w, const uint16_t* sc, const uint8_t* wu,
+              const uint16_t* scu, const float* bias, int act, void* y, hipStream_t s);
+
+size_t grad_norm_bytes(int count, const int64_t* numel);
+int launch_grad_norm(int count, const void* const* grads, const int64_t* numel, const int* dtypes, float* norm,
+                     void* ws, hipStream_t s);
+int launch_clip_grads(int count, const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes,
+                      float max_norm, float* norm, void* ws, hipStream_t s);
+
+}  // namespace qc

@@ -1,0 +1,197 @@
+// q4.hip -- weights of 4 bits with group scales: packing, and the products
+//   y = x W^T + bias,   h = act(x Wg^T) * (x Wu^T)
+// with W = scale * E2M1 magnitude.  The codes become 16-bit operands by the
+// conversion instruction (exact), one matrix instruction sums 32 products of
+// a group, and the fp32 sum of a group is multiplied by its scale, so no
+// weight is ever rounded.
+#include "dense.h"
+
+#include "qconv_internal.h"
+
+namespace qc {
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// packing
+// ---------------------------------------------------------------------------
+
+// fp32 bits rounded to 6 significant bits, to nearest, ties to even.
+__device__ __forceinline__ uint32_t round6(uint32_t b) { return (b + 0x1FFFFu + ((b >> 18) & 1u)) & ~0x3FFFFu; }
+
+// Nearest magnitude's index of r >= 0; a tie takes the smaller.
+__device__ __forceinline__ uint32_t e2m1_index(float r) {
+  return (r > 0.25f) + (r > 0.75f) + (r > 1.25f) + (r > 1.75f) + (r > 2.5f) + (r > 3.5f) + (r > 5.0f);
+}
+
+template <int DT>
+__device__ __forceinline__ float load_value(const void* p, int64_t i) {
+  if constexpr (DT == QCONV_F32) return ((const float*)p)[i];
+  if constexpr (DT == QCONV_F16) return F16::up(((const uint16_t*)p)[i]);
+  return BF16::up(((const uint16_t*)p)[i]);
+}
+
+// Eight values of a group per thread, group / 8 neighbouring lanes a group.
+// Bound by reading w.
+template <int DT>
+__global__ __launch_bounds__(256) void q4_pack_kernel(const void* __restrict__ w, int n, int k, int64_t ld, int group,
+                                                      int kp, float top, uint32_t* __restrict__ codes,
+                                                      uint16_t* __restrict__ scales) {
+  const int per = group / 8;  // 4, 8 or 16 lanes
+  const int64_t units = (int64_t)n * (kp / 8), padded = (units + 255) / 256 * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < padded; i += (int64_t)gridDim.x * 256) {
+    const bool on = i < units;
+    const int64_t row = on ? i / (kp / 8) : 0;
+    const int c = on ? (int)(i % (kp / 8)) * 8 : kp;
+    float v[8], big = 0.0f;
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = c + e < k ? load_value<DT>(w, row * ld + c + e) : 0.0f;
+      big = fmaxf(big, fabsf(v[e]));
+      odd |= !(fabsf(v[e]) < __builtin_inff());
+    }
+    uint32_t bad = odd;
+    for (int d = 1; d < per; d *= 2) {
+      big = fmaxf(big, __shfl_xor(big, d));
+      bad |= __shfl_xor(bad, d);
+    }
+    const float s = __uint_as_float(round6(__float_as_uint(big / top)));
+    uint32_t code = 0;
+    if (s > 0.0f && !bad) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t mag = e2m1_index(fabsf(v[e]) / s);
+        code |= (mag | (v[e] < 0.0f && mag ? 8u : 0u)) << (4 * e);
+      }
+    }
+    if (!on) continue;
+    codes[i] = code;
+    if (c % group == 0) scales[row * (kp / group) + c / group] = bad ? 0x7FC0u : (uint16_t)(__float_as_uint(s) >> 16);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------
+
+struct Q4Args {
+  const uint16_t* x;
+  int64_t ld_x, ld_y;
+  const uint8_t* w[2];
+  const uint16_t* sc[2];
+  const float* bias;
+  uint16_t* y;
+  int m, n, k, kp, act;
+};
+
+// 16 tokens x 16 outputs per block; its four waves take every fourth block of
+// 128 inputs and are joined through LDS.  D of the matrix instruction: lane
+// holds output lane % 16 and tokens (lane / 16) * 4 + 0..3, so one scale per
+// lane serves it.
+template <class T, int GROUP, bool GATED>
+__global__ __launch_bounds__(256) void q4_rows_kernel(Q4Args a) {
+  constexpr int H = GATED ? 2 : 1;
+  __shared__ float part[4][H][256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r = lane & 15, o = lane >> 4;  // tile row, octet of the 32 products
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
+  const bool xin = m0 + r < a.m, win = n0 + r < a.n;
+  const uint16_t* x = a.x + (xin ? (int64_t)(m0 + r) * a.ld_x : 0);
+  const int64_t wrow = win ? n0 + r : 0;
+  v4f acc[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) acc[h] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int g0 = wave * GROUP; g0 < a.kp; g0 += 4 * GROUP) {
+    v4u xf[GROUP / 32];
+#pragma unroll
+    for (int i = 0; i < GROUP / 32; ++i) {
+      const int k = g0 + i * 32 + o * 8;
+      xf[i] = load8_first(x + (xin ? k : 0), xin ? a.k - k : 0);
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < GROUP / 32; ++i) {
+        const uint32_t c = *(const uint32_t*)(a.w[h] + wrow * (a.kp / 2) + (g0 + i * 32 + o * 8) / 2);
+        const v4u wf = {T::template from_e2m1<0>(c), T::template from_e2m1<1>(c), T::template from_e2m1<2>(c),
+                        T::template from_e2m1<3>(c)};
+        sum = T::mfma(xf[i], wf, sum);
+      }
+      const float s = BF16::up(a.sc[h][wrow * (a.kp / GROUP) + g0 / GROUP]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[h][e] = fmaf(s, sum[e], acc[h][e]);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[wave][h][(o * 4 + e) * 16 + r] = acc[h][e];
+  __syncthreads();
+  const int t = threadIdx.x, m = m0 + t / 16, n = n0 + t % 16;
+  if (m >= a.m || n >= a.n) return;
+  float v[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) v[h] = (part[0][h][t] + part[1][h][t]) + (part[2][h][t] + part[3][h][t]);
+  float y;
+  if constexpr (GATED)
+    y = act_value(a.act, v[0]) * v[1];
+  else
+    y = a.bias ? v[0] + a.bias[n] : v[0];
+  a.y[(int64_t)m * a.ld_y + n] = T::down(y);
+}
+
+template <class T, bool GATED>
+int run_rows(const Q4Args& a, int group, hipStream_t s) {
+  const dim3 grid(ceil_div(a.n, 16), ceil_div(a.m, 16));
+  if ((int64_t)grid.x * grid.y >= (1 << 24) || grid.y > 65535) return QCONV_EUNSUPPORTED;
+  if (group == 32)
+    q4_rows_kernel<T, 32, GATED><<<grid, 256, 0, s>>>(a);
+  else if (group == 64)
+    q4_rows_kernel<T, 64, GATED><<<grid, 256, 0, s>>>(a);
+  else
+    q4_rows_kernel<T, 128, GATED><<<grid, 256, 0, s>>>(a);
+  return hip_status();
+}
+
+}  // namespace
+
+int launch_q4_pack(const void* w, int dtype, int n, int k, int64_t ld, int group, int top, uint8_t* codes,
+                   uint16_t* scales, hipStream_t s) {
+  const int kp = (int)round_up(k, group);
+  const int64_t units = (int64_t)n * (kp / 8);
+  const unsigned grid = (unsigned)(units < (1 << 22) ? (units + 255) / 256 : 1 << 14);
+  uint32_t* c = (uint32_t*)codes;
+  if (dtype == QCONV_F32)
+    q4_pack_kernel<QCONV_F32><<<grid, 256, 0, s>>>(w, n, k, ld, group, kp, (float)top, c, scales);
+  else if (dtype == QCONV_F16)
+    q4_pack_kernel<QCONV_F16><<<grid, 256, 0, s>>>(w, n, k, ld, group, kp, (float)top, c, scales);
+  else
+    q4_pack_kernel<QCONV_BF16><<<grid, 256, 0, s>>>(w, n, k, ld, group, kp, (float)top, c, scales);
+  return hip_status();
+}
+
+int launch_q4(const qconv_q4_desc& d, const void* x, const uint8_t* w, const uint16_t* sc, const uint8_t* wu,
+              const uint16_t* scu, const float* bias, int act, void* y, hipStream_t s) {
+  if (d.m == 0) return QCONV_OK;
+  Q4Args a = {};
+  a.x = (const uint16_t*)x;
+  a.ld_x = d.ld_x;
+  a.ld_y = d.ld_y;
+  a.w[0] = w;
+  a.w[1] = wu;
+  a.sc[0] = sc;
+  a.sc[1] = scu;
+  a.bias = bias;
+  a.y = (uint16_t*)y;
+  a.m = d.m;
+  a.n = d.n;
+  a.k = d.k;
+  a.kp = (int)round_up(d.k, d.group);
+  a.act = act;
+  if (d.dtype == QCONV_F16) return wu ? run_rows<F16, true>(a, d.group, s) : run_rows<F16, false>(a, d.group, s);
+  return wu ? run_rows<BF16, true>(a, d.group, s) : run_rows<BF16, false>(a, d.group, s);
+}
+
+}  // namespace qc

@@ -8,7 +8,9 @@ no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
+from array import array
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libqconv.so")
@@ -285,7 +287,21 @@ def aqe_sgd_clip(w, g, lr: float, stream=None):
 # Fully connected operators and the gradient norm
 # ---------------------------------------------------------------------------
 
-_dtypes = None
+class _Dtypes(dict):
+    """torch type -> DT_*, -1 for the types the operators do not take."""
+
+    def __missing__(self, key):
+        import torch
+
+        self.update({torch.float32: DT_F32, torch.float16: DT_F16, torch.bfloat16: DT_BF16})
+        return self.setdefault(key, -1)
+
+
+_dtypes = _Dtypes()
+
+
+def _dtype_code(t) -> int:
+    return _dtypes[t.dtype]
 
 
 def _new(shape, dtype, like, stream):
@@ -302,16 +318,6 @@ def _new(shape, dtype, like, stream):
 def _on_gpu(t, what: str):
     if not t.is_cuda:
         raise ValueError(f"{what}: tensors are on the GPU, got one on {t.device}")
-
-
-def _dtype_code(t) -> int:
-    """DT_* of a tensor (-1 for other types)."""
-    global _dtypes
-    if _dtypes is None:
-        import torch
-
-        _dtypes = {torch.float32: DT_F32, torch.float16: DT_F16, torch.bfloat16: DT_BF16}
-    return _dtypes.get(t.dtype, -1)
 
 
 def _rows(t, rows, cols, like, what: str) -> int:
@@ -501,16 +507,27 @@ def _dense(t) -> bool:
 
 
 def _grad_arrays(grads, what):
-    """(count, pointers, sizes, types) of a list of gradients as C arrays."""
+    """(count, pointers, sizes, types, dense order) of a list of gradients as C
+    arrays.  One pass per property with the tensors' own methods: a model has
+    hundreds of gradients, and a Python loop body costs more than the kernels."""
+    import torch
+
+    T = torch.Tensor
     n = len(grads)
-    dev = grads[0].device if n else None
-    types = [_dtype_code(g) for g in grads]
+    types = list(map(operator.attrgetter("dtype"), grads))
+    codes = array("i", [_dtypes[types[0]]]) * n if n and types.count(types[0]) == n else \
+        array("i", map(_dtypes.__getitem__, types))
     if n:
         _on_gpu(grads[0], what)
-    if any(g.device != dev or not _dense(g) for g in grads) or -1 in types:
+    plain = all(map(T.is_contiguous, grads))
+    if len(set(map(T.get_device, grads))) > 1 or -1 in codes or not (plain or all(map(_dense, grads))):
         raise ValueError(f"{what}: gradients are dense fp32, fp16 or bf16 tensors on one device")
-    return (n, (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]),
-            (ctypes.c_int64 * n)(*[g.numel() for g in grads]), (ctypes.c_int * n)(*types))
+    return n, array("Q", map(T.data_ptr, grads)), array("q", map(T.numel, grads)), codes, plain
+
+
+def _addr(a):
+    """Address of an array.array's values, which its owner keeps alive."""
+    return a.buffer_info()[0]
 
 
 def _norm_out(grads, norm, what, stream):
@@ -525,28 +542,29 @@ def _norm_out(grads, norm, what, stream):
 
 def aqe_grad_norm(grads, norm=None, workspace=None, stream=None):
     """The 2-norm over all values of a list of gradients, as a device scalar."""
-    n, ptrs, sizes, types = _grad_arrays(grads, "aqe_grad_norm")
+    n, ptrs, sizes, types, _ = _grad_arrays(grads, "aqe_grad_norm")
     norm = _norm_out(grads, norm, "aqe_grad_norm", stream)
-    ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, sizes), norm, "aqe_grad_norm", stream)
-    _check(lib().aqe_grad_norm(n, ptrs, sizes, types, _ptr(norm), _ptr(ws), nbytes, _stream(stream)), "aqe_grad_norm")
+    ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, _addr(sizes)), norm, "aqe_grad_norm", stream)
+    _check(lib().aqe_grad_norm(n, _addr(ptrs), _addr(sizes), _addr(types), _ptr(norm), _ptr(ws), nbytes,
+                               _stream(stream)), "aqe_grad_norm")
     return norm
 
 
 def aqe_clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, stream=None):
     """Scale a list of gradients so that their joint norm is at most max_norm,
-    in place or into the tensors of `out` (same types and layouts); returns
+    in place or into the tensors of `out` (same sizes, types and layouts); returns
     the norm before, as a device scalar."""
-    n, ptrs, sizes, types = _grad_arrays(grads, "aqe_clip_grads")
+    n, ptrs, sizes, types, plain = _grad_arrays(grads, "aqe_clip_grads")
     outs = ptrs
     if out is not None:
-        if len(out) != n or any(o.shape != g.shape or o.stride() != g.stride() or o.dtype != g.dtype or
-                                o.device != g.device for o, g in zip(out, grads)):
-            raise ValueError("aqe_clip_grads: out holds one tensor per gradient, of its shape, strides, type and device")
-        outs = (ctypes.c_void_p * n)(*[o.data_ptr() for o in out])
+        m, outs, out_sizes, out_types, out_plain = _grad_arrays(out, "aqe_clip_grads")
+        if m != n or out_sizes != sizes or out_types != types or (n and out[0].device != grads[0].device) or \
+                not (plain and out_plain or all(o.stride() == g.stride() for o, g in zip(out, grads))):
+            raise ValueError("aqe_clip_grads: out holds one tensor per gradient, of its size, layout, type and device")
     norm = _norm_out(grads, norm, "aqe_clip_grads", stream)
-    ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, sizes), norm, "aqe_clip_grads", stream)
-    _check(lib().aqe_clip_grads(n, ptrs, outs, sizes, types, float(max_norm), _ptr(norm), _ptr(ws), nbytes,
-                                _stream(stream)), "aqe_clip_grads")
+    ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, _addr(sizes)), norm, "aqe_clip_grads", stream)
+    _check(lib().aqe_clip_grads(n, _addr(ptrs), _addr(outs), _addr(sizes), _addr(types), float(max_norm), _ptr(norm),
+                                _ptr(ws), nbytes, _stream(stream)), "aqe_clip_grads")
     return norm
 
 

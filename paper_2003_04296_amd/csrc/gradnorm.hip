@@ -30,29 +30,78 @@ struct Table {
 };
 static_assert(sizeof(Table) <= 3900, "kernel arguments");
 
+// Values of a type in 16 bytes, their widening and their rounding.
 template <int DT>
-__device__ __forceinline__ float value_at(const void* p, int64_t i) {
-  if constexpr (DT == QCONV_F32) return ((const float*)p)[i];
-  if constexpr (DT == QCONV_F16) return F16::up(((const uint16_t*)p)[i]);
-  return BF16::up(((const uint16_t*)p)[i]);
-}
+struct Values {
+  static constexpr int N = DT == QCONV_F32 ? 4 : 8, SIZE = DT == QCONV_F32 ? 4 : 2;
+  __device__ __forceinline__ static float one(const char* p, int64_t i) {
+    if constexpr (DT == QCONV_F32) return ((const float*)p)[i];
+    if constexpr (DT == QCONV_F16) return F16::up(((const uint16_t*)p)[i]);
+    return BF16::up(((const uint16_t*)p)[i]);
+  }
+  __device__ __forceinline__ static void put(char* p, int64_t i, float v) {
+    if constexpr (DT == QCONV_F32) ((float*)p)[i] = v;
+    else if constexpr (DT == QCONV_F16) ((uint16_t*)p)[i] = F16::down(v);
+    else ((uint16_t*)p)[i] = BF16::down(v);
+  }
+  __device__ __forceinline__ static void widen(v4u w, float v[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if constexpr (DT == QCONV_F32) v[e] = __uint_as_float(w[e]);
+      else if constexpr (DT == QCONV_F16) v[e] = F16::up((uint16_t)(w[e / 2] >> (16 * (e & 1))));
+      else v[e] = BF16::up((uint16_t)(w[e / 2] >> (16 * (e & 1))));
+    }
+  }
+  __device__ __forceinline__ static v4u narrow(const float v[N]) {
+    v4u w = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if constexpr (DT == QCONV_F32) w[e] = __float_as_uint(v[e]);
+      else if constexpr (DT == QCONV_F16) w[e / 2] |= (uint32_t)F16::down(v[e]) << (16 * (e & 1));
+      else w[e / 2] |= (uint32_t)BF16::down(v[e]) << (16 * (e & 1));
+    }
+    return w;
+  }
+};
+
+// The values [b, e) of a tensor at p in three parts: up to 16-byte alignment,
+// whole 16-byte groups, and the rest.
+struct Parts {
+  int64_t first, groups, rest;  // first value of the groups, their number, first value after them
+};
 template <int DT>
-__device__ __forceinline__ void put_at(void* p, int64_t i, float v) {
-  if constexpr (DT == QCONV_F32) ((float*)p)[i] = v;
-  else if constexpr (DT == QCONV_F16) ((uint16_t*)p)[i] = F16::down(v);
-  else ((uint16_t*)p)[i] = BF16::down(v);
+__device__ __forceinline__ Parts parts_of(const void* p, int64_t b, int64_t e) {
+  typedef Values<DT> V;
+  const int64_t skew = (int64_t)((uintptr_t)p / V::SIZE + b) & (V::N - 1);
+  Parts r;
+  r.first = b + (skew ? V::N - skew : 0);
+  if (r.first > e) r.first = e;
+  r.groups = (e - r.first) / V::N;
+  r.rest = r.first + r.groups * V::N;
+  return r;
 }
 
-// Tensor of a chunk and the chunk's first value.
-__device__ __forceinline__ int find(const Table& t, int chunk, int64_t* start) {
+// A walk over the chunks [from, to) of a launch; blocks take neighbouring
+// runs, so that the tensor of a chunk is found once and then followed.
+struct Run {
+  int from, to;
+};
+__device__ __forceinline__ Run run_of(const Table& t) {
+  return {(int)((int64_t)t.chunks * blockIdx.x / gridDim.x), (int)((int64_t)t.chunks * (blockIdx.x + 1) / gridDim.x)};
+}
+__device__ __forceinline__ int tensor_of(const Table& t, int chunk) {
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
     if (t.last[mid] > chunk) hi = mid;
     else lo = mid + 1;
   }
-  *start = (int64_t)(chunk - (lo ? t.last[lo - 1] : 0)) * CHUNK;
   return lo;
+}
+// The first value of a chunk of tensor i, and the one after its last.
+__device__ __forceinline__ void range_of(const Table& t, int i, int chunk, int64_t* b, int64_t* e) {
+  *b = (int64_t)(chunk - (i ? t.last[i - 1] : 0)) * CHUNK;
+  *e = *b + CHUNK < t.numel[i] ? *b + CHUNK : t.numel[i];
 }
 
 __device__ __forceinline__ double block_sum(double v, double* lds) {
@@ -63,11 +112,35 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+// Groups loaded by a thread before any is used: the loads of a wave have to
+// cover the memory's latency.
+constexpr int AHEAD = 8;
+
 template <int DT>
 __device__ __forceinline__ double squares(const void* p, int64_t b, int64_t e) {
+  typedef Values<DT> V;
+  const Parts r = parts_of<DT>(p, b, e);
+  const v4u* g = (const v4u*)((const char*)p + r.first * V::SIZE);
   double s = 0.0;
-  for (int64_t i = b + threadIdx.x; i < e; i += 256) {
-    const double v = (double)value_at<DT>(p, i);
+  for (int64_t i = threadIdx.x; i < r.groups; i += 256 * AHEAD) {
+    v4u w[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) w[j] = i + j * 256 < r.groups ? g[i + j * 256] : v4u{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      float v[V::N];
+      V::widen(w[j], v);
+#pragma unroll
+      for (int k = 0; k < V::N; ++k) s = fma((double)v[k], (double)v[k], s);
+    }
+  }
+  const int64_t head = b + threadIdx.x, tail = r.rest + threadIdx.x;  // at most 7 values each
+  if (head < r.first) {
+    const double v = (double)V::one((const char*)p, head);
+    s = fma(v, v, s);
+  }
+  if (tail < e) {
+    const double v = (double)V::one((const char*)p, tail);
     s = fma(v, v, s);
   }
   return s;
@@ -75,11 +148,13 @@ __device__ __forceinline__ double squares(const void* p, int64_t b, int64_t e) {
 
 __global__ __launch_bounds__(256) void grad_squares_kernel(Table t, double* parts) {
   __shared__ double lds[4];
+  const Run run = run_of(t);
   double s = 0.0;
-  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    int64_t b;
-    const int i = find(t, c, &b);
-    const int64_t e = b + CHUNK < t.numel[i] ? b + CHUNK : t.numel[i];
+  int i = tensor_of(t, run.from);
+  for (int c = run.from; c < run.to; ++c) {
+    while (c >= t.last[i]) ++i;
+    int64_t b, e;
+    range_of(t, i, c, &b, &e);
     if (t.type[i] == QCONV_F32) s += squares<QCONV_F32>(t.in[i], b, e);
     else if (t.type[i] == QCONV_F16) s += squares<QCONV_F16>(t.in[i], b, e);
     else s += squares<QCONV_BF16>(t.in[i], b, e);
@@ -101,22 +176,56 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double* parts, int
   if (threadIdx.x == 0) *norm = (float)v;
 }
 
+// Sixteen bytes from any address a value may have.
 template <int DT>
-__device__ __forceinline__ void scale(const void* in, void* out, int64_t b, int64_t e, float c) {
-  for (int64_t i = b + threadIdx.x; i < e; i += 256) put_at<DT>(out, i, value_at<DT>(in, i) * c);
+__device__ __forceinline__ v4u load16(const char* p) {
+  struct __attribute__((packed, aligned(Values<DT>::SIZE))) U {
+    v4u v;
+  };
+  return reinterpret_cast<const U*>(p)->v;
 }
 
+// Stores are aligned; loads need not be, where the two tensors start differently.
+template <int DT>
+__device__ __forceinline__ void scale(const void* in, void* out, int64_t b, int64_t e, float c) {
+  typedef Values<DT> V;
+  const Parts r = parts_of<DT>(out, b, e);
+  const char* g = (const char*)in + r.first * V::SIZE;
+  v4u* o = (v4u*)((char*)out + r.first * V::SIZE);
+  for (int64_t i = threadIdx.x; i < r.groups; i += 256 * AHEAD) {
+    v4u w[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      w[j] = i + j * 256 < r.groups ? load16<DT>(g + (i + j * 256) * 16) : v4u{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      float v[V::N];
+      V::widen(w[j], v);
+#pragma unroll
+      for (int k = 0; k < V::N; ++k) v[k] *= c;
+      if (i + j * 256 < r.groups) __builtin_nontemporal_store(V::narrow(v), o + i + j * 256);
+    }
+  }
+  const int64_t head = b + threadIdx.x, tail = r.rest + threadIdx.x;
+  if (head < r.first) V::put((char*)out, head, V::one((const char*)in, head) * c);
+  if (tail < e) V::put((char*)out, tail, V::one((const char*)in, tail) * c);
+}
+
+// Each block walks its run backwards: what the norm's pass read last is what
+// the 256 MB cache still holds.
 __global__ __launch_bounds__(256) void grad_scale_kernel(Table t, const double* parts, int n, float max_norm,
                                                          float* norm) {
   __shared__ double lds[4];
   const double v = norm_of(parts, n, lds);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
   const float c = v > (double)max_norm ? (float)((double)max_norm / v) : 1.0f;
-  for (int k = blockIdx.x; k < t.chunks; k += gridDim.x) {
-    int64_t b;
-    const int i = find(t, k, &b);
+  const Run run = run_of(t);
+  int i = tensor_of(t, run.to - 1);
+  for (int k = run.to - 1; k >= run.from; --k) {
+    while (i > 0 && k < t.last[i - 1]) --i;
     if (c == 1.0f && t.in[i] == t.out[i]) continue;
-    const int64_t e = b + CHUNK < t.numel[i] ? b + CHUNK : t.numel[i];
+    int64_t b, e;
+    range_of(t, i, k, &b, &e);
     if (t.type[i] == QCONV_F32) scale<QCONV_F32>(t.in[i], t.out[i], b, e, c);
     else if (t.type[i] == QCONV_F16) scale<QCONV_F16>(t.in[i], t.out[i], b, e, c);
     else scale<QCONV_BF16>(t.in[i], t.out[i], b, e, c);

@@ -8,7 +8,7 @@
 // forward, dg/du in gx) are read from LDS as 16 bytes per lane, operands whose
 // k runs down their columns ("column form": W in gx, all of gW) through the
 // transposing LDS reads.
-#include "dense.h"
+#include "dense_rows.h"
 
 #include "qconv_internal.h"
 
@@ -352,6 +352,23 @@ int run_slopes(const qconv_ffn_desc& d, const float* pre, const void* gh, int fp
 int launch_ffn_forward(const qconv_ffn_desc& d, const void* x, const void* wg, const void* wu, void* h, float* pre,
                        hipStream_t s) {
   if (d.m == 0) return QCONV_OK;
+  if (d.m <= 64) {
+    RowsArgs r = {};
+    r.x = (const uint16_t*)x;
+    r.ld_x = d.ld_x;
+    r.ld_w = d.ld_w;
+    r.ld_y = d.ld_h;
+    r.w[0] = wg;
+    r.w[1] = wu;
+    r.y = (uint16_t*)h;
+    r.pre = pre;
+    r.ld_pre = (int)round_up(d.f, 8);
+    r.m = d.m;
+    r.n = d.f;
+    r.k = d.k;
+    r.act = d.act;
+    return d.dtype == QCONV_F16 ? run_dense_rows<F16, Dense16, 2>(r, s) : run_dense_rows<BF16, Dense16, 2>(r, s);
+  }
   GemmArgs a = {};
   a.r[0] = {(const uint16_t*)x, d.ld_x};
   a.c[0] = {(const uint16_t*)wg, d.ld_w};

@@ -4,7 +4,7 @@
 // conversion instruction (exact), one matrix instruction sums 32 products of
 // a group, and the fp32 sum of a group is multiplied by its scale, so no
 // weight is ever rounded.
-#include "dense.h"
+#include "dense_rows.h"
 
 #include "qconv_internal.h"
 
@@ -71,88 +71,11 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const void* __restrict__ w
   }
 }
 
-// ---------------------------------------------------------------------------
-// products
-// ---------------------------------------------------------------------------
-
-struct Q4Args {
-  const uint16_t* x;
-  int64_t ld_x, ld_y;
-  const uint8_t* w[2];
-  const uint16_t* sc[2];
-  const float* bias;
-  uint16_t* y;
-  int m, n, k, kp, act;
-};
-
-// 16 tokens x 16 outputs per block; its four waves take every fourth block of
-// 128 inputs and are joined through LDS.  D of the matrix instruction: lane
-// holds output lane % 16 and tokens (lane / 16) * 4 + 0..3, so one scale per
-// lane serves it.
-template <class T, int GROUP, bool GATED>
-__global__ __launch_bounds__(256) void q4_rows_kernel(Q4Args a) {
-  constexpr int H = GATED ? 2 : 1;
-  __shared__ float part[4][H][256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r = lane & 15, o = lane >> 4;  // tile row, octet of the 32 products
-  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
-  const bool xin = m0 + r < a.m, win = n0 + r < a.n;
-  const uint16_t* x = a.x + (xin ? (int64_t)(m0 + r) * a.ld_x : 0);
-  const int64_t wrow = win ? n0 + r : 0;
-  v4f acc[H];
-#pragma unroll
-  for (int h = 0; h < H; ++h) acc[h] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int g0 = wave * GROUP; g0 < a.kp; g0 += 4 * GROUP) {
-    v4u xf[GROUP / 32];
-#pragma unroll
-    for (int i = 0; i < GROUP / 32; ++i) {
-      const int k = g0 + i * 32 + o * 8;
-      xf[i] = load8_first(x + (xin ? k : 0), xin ? a.k - k : 0);
-    }
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int i = 0; i < GROUP / 32; ++i) {
-        const uint32_t c = *(const uint32_t*)(a.w[h] + wrow * (a.kp / 2) + (g0 + i * 32 + o * 8) / 2);
-        const v4u wf = {T::template from_e2m1<0>(c), T::template from_e2m1<1>(c), T::template from_e2m1<2>(c),
-                        T::template from_e2m1<3>(c)};
-        sum = T::mfma(xf[i], wf, sum);
-      }
-      const float s = BF16::up(a.sc[h][wrow * (a.kp / GROUP) + g0 / GROUP]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[h][e] = fmaf(s, sum[e], acc[h][e]);
-    }
-  }
-#pragma unroll
-  for (int h = 0; h < H; ++h)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) part[wave][h][(o * 4 + e) * 16 + r] = acc[h][e];
-  __syncthreads();
-  const int t = threadIdx.x, m = m0 + t / 16, n = n0 + t % 16;
-  if (m >= a.m || n >= a.n) return;
-  float v[H];
-#pragma unroll
-  for (int h = 0; h < H; ++h) v[h] = (part[0][h][t] + part[1][h][t]) + (part[2][h][t] + part[3][h][t]);
-  float y;
-  if constexpr (GATED)
-    y = act_value(a.act, v[0]) * v[1];
-  else
-    y = a.bias ? v[0] + a.bias[n] : v[0];
-  a.y[(int64_t)m * a.ld_y + n] = T::down(y);
-}
-
-template <class T, bool GATED>
-int run_rows(const Q4Args& a, int group, hipStream_t s) {
-  const dim3 grid(ceil_div(a.n, 16), ceil_div(a.m, 16));
-  if ((int64_t)grid.x * grid.y >= (1 << 24) || grid.y > 65535) return QCONV_EUNSUPPORTED;
-  if (group == 32)
-    q4_rows_kernel<T, 32, GATED><<<grid, 256, 0, s>>>(a);
-  else if (group == 64)
-    q4_rows_kernel<T, 64, GATED><<<grid, 256, 0, s>>>(a);
-  else
-    q4_rows_kernel<T, 128, GATED><<<grid, 256, 0, s>>>(a);
-  return hip_status();
+template <class T, int H>
+int run_rows(RowsArgs& a, int group, hipStream_t s) {
+  if (group == 32) return run_dense_rows<T, Q4<32>, H>(a, s);
+  if (group == 64) return run_dense_rows<T, Q4<64>, H>(a, s);
+  return run_dense_rows<T, Q4<128>, H>(a, s);
 }
 
 }  // namespace
@@ -175,7 +98,7 @@ int launch_q4_pack(const void* w, int dtype, int n, int k, int64_t ld, int group
 int launch_q4(const qconv_q4_desc& d, const void* x, const uint8_t* w, const uint16_t* sc, const uint8_t* wu,
               const uint16_t* scu, const float* bias, int act, void* y, hipStream_t s) {
   if (d.m == 0) return QCONV_OK;
-  Q4Args a = {};
+  RowsArgs a = {};
   a.x = (const uint16_t*)x;
   a.ld_x = d.ld_x;
   a.ld_y = d.ld_y;
@@ -190,8 +113,8 @@ int launch_q4(const qconv_q4_desc& d, const void* x, const uint8_t* w, const uin
   a.k = d.k;
   a.kp = (int)round_up(d.k, d.group);
   a.act = act;
-  if (d.dtype == QCONV_F16) return wu ? run_rows<F16, true>(a, d.group, s) : run_rows<F16, false>(a, d.group, s);
-  return wu ? run_rows<BF16, true>(a, d.group, s) : run_rows<BF16, false>(a, d.group, s);
+  if (d.dtype == QCONV_F16) return wu ? run_rows<F16, 2>(a, d.group, s) : run_rows<F16, 1>(a, d.group, s);
+  return wu ? run_rows<BF16, 2>(a, d.group, s) : run_rows<BF16, 1>(a, d.group, s);
 }
 
 }  // namespace qc

@@ -314,12 +314,17 @@ typedef struct {
 /* Floats of the `pre` buffer: [m][2][fp] with fp = f rounded up to 8. */
 size_t qconv_ffn_pre_floats(int m, int f);
 
+/* Workspace of qconv_ffn_forward (0 where it needs none). */
+size_t qconv_ffn_forward_bytes(const qconv_ffn_desc* d);
+
 /* h[m][f] = act(g) * u with g = x w_gate^T, u = x w_up^T; x[m][k],
  * w_gate[f][k], w_up[f][k].  pre (NULL to leave it out) receives g in
  * [m][0][0..f) and u in [m][1][0..f) for the backward pass; what lies past f
- * in a row is not written.  m == 0 launches nothing. */
+ * in a row is not written.  m == 0 launches nothing.  workspace (here and
+ * below): 16-byte aligned, of at least the stated bytes, not kept between
+ * calls. */
 int qconv_ffn_forward(const qconv_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, void* h,
-                      float* pre, void* stream);
+                      float* pre, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Workspace of qconv_ffn_backward. */
 size_t qconv_ffn_backward_bytes(const qconv_ffn_desc* d);
@@ -328,8 +333,7 @@ size_t qconv_ffn_backward_bytes(const qconv_ffn_desc* d);
  *   dg = gh u act'(g), du = gh act(g), rounded to the tensors' type, then
  *   gx[m][k] = dg w_gate + du w_up,  gw_gate[f][k] = dg^T x,  gw_up[f][k] = du^T x.
  * gx, and gw_gate together with gw_up, may be NULL to leave them out; they
- * are contiguous.  m == 0 gives zero weight gradients.  workspace: 16-byte
- * aligned, at least qconv_ffn_backward_bytes. */
+ * are contiguous.  m == 0 gives zero weight gradients. */
 int qconv_ffn_backward(const qconv_ffn_desc* d, const void* x, const void* w_gate, const void* w_up,
                        const float* pre, const void* gh, void* gx, void* gw_gate, void* gw_up, void* workspace,
                        size_t workspace_bytes, void* stream);

@@ -35,7 +35,7 @@ EXPORTED = (
     "qnet_layer_kernel",
     "qnet_tensor_info", "qconv_resolve_algo",
     "qconv_kernel_name", "aqe_forward", "aqe_backward", "aqe_sgd_clip",
-    "qconv_ffn_pre_floats", "qconv_ffn_forward", "qconv_ffn_backward_bytes", "qconv_ffn_backward",
+    "qconv_ffn_pre_floats", "qconv_ffn_forward_bytes", "qconv_ffn_forward", "qconv_ffn_backward_bytes", "qconv_ffn_backward",
     "qconv_q4_code_bytes", "qconv_q4_scale_bytes", "qconv_q4_pack", "qconv_q4_workspace_bytes", "qconv_q4_linear",
     "qconv_q4_gated", "aqe_grad_norm_bytes", "aqe_grad_norm", "aqe_clip_grads",
 )
@@ -110,7 +110,9 @@ def lib() -> ctypes.CDLL:
     ffn, q4 = ctypes.POINTER(qconv_ffn_desc), ctypes.POINTER(qconv_q4_desc)
     L.qconv_ffn_pre_floats.restype = sz
     L.qconv_ffn_pre_floats.argtypes = [i32, i32]
-    L.qconv_ffn_forward.argtypes = [ffn] + [vp] * 6
+    L.qconv_ffn_forward_bytes.restype = sz
+    L.qconv_ffn_forward_bytes.argtypes = [ffn]
+    L.qconv_ffn_forward.argtypes = [ffn] + [vp] * 6 + [sz, vp]
     L.qconv_ffn_backward_bytes.restype = sz
     L.qconv_ffn_backward_bytes.argtypes = [ffn]
     L.qconv_ffn_backward.argtypes = [ffn] + [vp] * 9 + [sz, vp]
@@ -364,7 +366,8 @@ def _ffn_desc(x, w_gate, w_up, act, h, what):
                           _rows(h, m, f, x, f"{what} h"))
 
 
-def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pre=None, out=None, stream=None):
+def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pre=None, out=None,
+                workspace=None, stream=None):
     """h = act(x w_gate^T) * (x w_up^T) for 16-bit x [m][k] and weights [f][k]
     -> (h [m][f], pre).  keep_pre (or a buffer `pre` of a former call) keeps
     what ffn_backward needs, else pre is None."""
@@ -378,8 +381,9 @@ def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pr
         pre = _new(lib().qconv_ffn_pre_floats(m, f), torch.float32, x, stream)
     elif pre is not None:
         _check_pre(pre, m, f, x, "ffn_forward")
-    _check(lib().qconv_ffn_forward(ctypes.byref(d), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(h), _ptr(pre),
-                                   _stream(stream)), "qconv_ffn_forward")
+    ws, nbytes = _workspace(workspace, lib().qconv_ffn_forward_bytes(ctypes.byref(d)), x, "ffn_forward", stream)
+    _check(lib().qconv_ffn_forward(ctypes.byref(d), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(h), _ptr(pre), _ptr(ws),
+                                   nbytes, _stream(stream)), "qconv_ffn_forward")
     return h, pre
 
 

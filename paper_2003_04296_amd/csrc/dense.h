@@ -15,6 +15,8 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 
 // The two 16-bit types behind one set of names: the kernels move 16-bit
 // patterns and only the matrix instruction and the conversions know which.
@@ -30,6 +32,12 @@ struct F16 {
   __device__ __forceinline__ static uint32_t from_e2m1(uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, BYTE));
   }
+  // the same times s
+  template <int BYTE>
+  __device__ __forceinline__ static uint32_t scaled_e2m1(uint32_t w, float s) {
+    const _Float16 h = (_Float16)s;
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, BYTE) * v2h{h, h});
+  }
 };
 struct BF16 {
   __device__ __forceinline__ static float up(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
@@ -40,6 +48,11 @@ struct BF16 {
   template <int BYTE>
   __device__ __forceinline__ static uint32_t from_e2m1(uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, BYTE));
+  }
+  template <int BYTE>
+  __device__ __forceinline__ static uint32_t scaled_e2m1(uint32_t w, float s) {
+    const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, BYTE);
+    return __builtin_bit_cast(uint32_t, v2b{(__bf16)(v[0] * s), (__bf16)(v[1] * s)});
   }
 };
 
@@ -84,17 +97,19 @@ __device__ __forceinline__ float act_value(int act, float g) {
 
 inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
+size_t ffn_forward_bytes(const qconv_ffn_desc& d);
 int launch_ffn_forward(const qconv_ffn_desc& d, const void* x, const void* wg, const void* wu, void* h, float* pre,
-                       hipStream_t s);
+                       void* ws, hipStream_t s);
 size_t ffn_backward_bytes(const qconv_ffn_desc& d);
 int launch_ffn_backward(const qconv_ffn_desc& d, const void* x, const void* wg, const void* wu, const float* pre,
                         const void* gh, void* gx, void* gwg, void* gwu, void* ws, hipStream_t s);
 
 int launch_q4_pack(const void* w, int dtype, int n, int k, int64_t ld, int group, int top, uint8_t* codes,
                    uint16_t* scales, hipStream_t s);
-// wu / su NULL: y = x W^T + bias; else the gated form.
+size_t q4_workspace_bytes(const qconv_q4_desc& d, bool gated);
+// wu / scu NULL: y = x W^T + bias; else the gated form.
 int launch_q4(const qconv_q4_desc& d, const void* x, const uint8_t* w, const uint16_t* sc, const uint8_t* wu,
-              const uint16_t* scu, const float* bias, int act, void* y, hipStream_t s);
+              const uint16_t* scu, const float* bias, int act, void* y, void* ws, hipStream_t s);
 
 size_t grad_norm_bytes(int count, const int64_t* numel);
 int launch_grad_norm(int count, const void* const* grads, const int64_t* numel, const int* dtypes, float* norm,

@@ -53,13 +53,19 @@ size_t qconv_ffn_pre_floats(int m, int f) {
   return (size_t)m * 2 * round_up(f, 8);
 }
 
+size_t qconv_ffn_forward_bytes(const qconv_ffn_desc* d) { return check_ffn(d) ? 0 : ffn_forward_bytes(*d); }
+
 int qconv_ffn_forward(const qconv_ffn_desc* d, const void* x, const void* w_gate, const void* w_up, void* h,
-                      float* pre, void* stream) {
+                      float* pre, void* workspace, size_t workspace_bytes, void* stream) {
   const int rc = check_ffn(d);
   if (rc) return rc;
   if (!w_gate || !w_up || (d->m > 0 && (!x || !h))) return QCONV_EINVAL;
-  if (!at(x, 2) || !at(w_gate, 2) || !at(w_up, 2) || !at(h, 2) || !at(pre, 16)) return QCONV_EINVAL;
-  return launch_ffn_forward(*d, x, w_gate, w_up, h, pre, (hipStream_t)stream);
+  if (!at(x, 2) || !at(w_gate, 2) || !at(w_up, 2) || !at(h, 2) || !at(pre, 16) || !at(workspace, 16))
+    return QCONV_EINVAL;
+  const size_t need = ffn_forward_bytes(*d);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  return launch_ffn_forward(*d, x, w_gate, w_up, h, pre, workspace, (hipStream_t)stream);
 }
 
 size_t qconv_ffn_backward_bytes(const qconv_ffn_desc* d) { return check_ffn(d) ? 0 : ffn_backward_bytes(*d); }
@@ -96,7 +102,9 @@ int qconv_q4_pack(const void* w, int dtype, int n, int k, int64_t ld_w, int grou
   return launch_q4_pack(w, dtype, n, k, ld_w, group, top, codes, scales, (hipStream_t)stream);
 }
 
-size_t qconv_q4_workspace_bytes(const qconv_q4_desc* d, int gated) { return 0; }
+size_t qconv_q4_workspace_bytes(const qconv_q4_desc* d, int gated) {
+  return check_q4(d) ? 0 : q4_workspace_bytes(*d, gated != 0);
+}
 
 int qconv_q4_linear(const qconv_q4_desc* d, const void* x, const uint8_t* codes, const uint16_t* scales,
                     const float* bias, void* y, void* workspace, size_t workspace_bytes, void* stream) {
@@ -105,8 +113,10 @@ int qconv_q4_linear(const qconv_q4_desc* d, const void* x, const uint8_t* codes,
   if (!codes || !scales || (d->m > 0 && (!x || !y)) || !at(x, 2) || !at(y, 2) || !at(bias, 4) || !at(codes, 16) ||
       !at(scales, 16) || !at(workspace, 16))
     return QCONV_EINVAL;
-  if (workspace_bytes < qconv_q4_workspace_bytes(d, 0)) return QCONV_EWORKSPACE;
-  return launch_q4(*d, x, codes, scales, nullptr, nullptr, bias, 0, y, (hipStream_t)stream);
+  const size_t need = q4_workspace_bytes(*d, false);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  return launch_q4(*d, x, codes, scales, nullptr, nullptr, bias, 0, y, workspace, (hipStream_t)stream);
 }
 
 int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_codes, const uint16_t* gate_scales,
@@ -118,8 +128,11 @@ int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_co
       (d->m > 0 && (!x || !y)) || !at(x, 2) || !at(y, 2) || !at(gate_codes, 16) || !at(gate_scales, 16) ||
       !at(up_codes, 16) || !at(up_scales, 16) || !at(workspace, 16))
     return QCONV_EINVAL;
-  if (workspace_bytes < qconv_q4_workspace_bytes(d, 1)) return QCONV_EWORKSPACE;
-  return launch_q4(*d, x, gate_codes, gate_scales, up_codes, up_scales, nullptr, act, y, (hipStream_t)stream);
+  const size_t need = q4_workspace_bytes(*d, true);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  return launch_q4(*d, x, gate_codes, gate_scales, up_codes, up_scales, nullptr, act, y, workspace,
+                   (hipStream_t)stream);
 }
 
 size_t aqe_grad_norm_bytes(int count, const int64_t* numel) {

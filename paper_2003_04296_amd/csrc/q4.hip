@@ -4,6 +4,7 @@
 // conversion instruction (exact), one matrix instruction sums 32 products of
 // a group, and the fp32 sum of a group is multiplied by its scale, so no
 // weight is ever rounded.
+#include "dense_gemm.h"
 #include "dense_rows.h"
 
 #include "qconv_internal.h"
@@ -71,6 +72,87 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const void* __restrict__ w
   }
 }
 
+// For each weight row the power of two that takes its largest finite scale to
+// [1, 2); a wave per row.
+__global__ __launch_bounds__(256) void q4_unit_kernel(const uint16_t* __restrict__ scales, int n, int groups,
+                                                      float* __restrict__ unit) {
+  const int row = blockIdx.x * 4 + threadIdx.x / 64;
+  if (row >= n) return;
+  uint32_t top = 0;  // the largest scale's exponent field
+  for (int g = threadIdx.x & 63; g < groups; g += 64) {
+    const uint32_t e = scales[(int64_t)row * groups + g] >> 7 & 0xFF;
+    if (e < 255 && e > top) top = e;
+  }
+#pragma unroll
+  for (int d = 32; d; d /= 2) {
+    const uint32_t v = __shfl_xor(top, d);
+    if (v > top) top = v;
+  }
+  // 2^(127 - top), kept a normal number
+  if ((threadIdx.x & 63) == 0) unit[row] = __uint_as_float((top < 1 ? 253u : top > 253 ? 1u : 254u - top) << 23);
+}
+
+template <class T, int OUT, int GROUP>
+int run_gemm_q4(GemmArgs& a, int tile, bool aligned, hipStream_t s) {
+  constexpr bool PAIR = OUT == OUT_GATED;
+  if (!aligned)
+    return run_gemm_tiles<T, Stage16<128, 256, 0, false, false, false>, StageQ4<T, 128, 256, GROUP, PAIR>, OUT, 128>(a,
+                                                                                                                    s);
+  if (tile == 256)
+    return run_gemm_tiles<T, Stage16<256, 512, 0, false, true, false>, StageQ4<T, 256, 512, GROUP, PAIR>, OUT, 256>(a, s);
+  return run_gemm_tiles<T, Stage16<128, 256, 0, false, true, false>, StageQ4<T, 128, 256, GROUP, PAIR>, OUT, 128>(a, s);
+}
+
+template <class T, int OUT>
+int run_gemm_q4_group(GemmArgs& a, int group, int tile, bool aligned, hipStream_t s) {
+  if (group == 32) return run_gemm_q4<T, OUT, 32>(a, tile, aligned, s);
+  if (group == 64) return run_gemm_q4<T, OUT, 64>(a, tile, aligned, s);
+  return run_gemm_q4<T, OUT, 128>(a, tile, aligned, s);
+}
+
+constexpr int ROWS_MOST = 64;  // tokens that go through dense_rows.h
+
+GemmPlan plan_q4(const qconv_q4_desc& d, bool gated, bool aligned) {
+  return gemm_plan(d.m, d.n, ceil_div(d.k, KSTEP), 1, gated, aligned);
+}
+size_t unit_bytes(const qconv_q4_desc& d) { return (size_t)round_up(d.n, 4) * 4; }  // of one weight
+
+int launch_gemm(const qconv_q4_desc& d, const void* x, const uint8_t* const w[2], const uint16_t* const sc[2],
+                const float* bias, int act, void* y, void* ws, hipStream_t s) {
+  const bool gated = w[1] != nullptr;
+  GemmArgs a = {};
+  a.r[0] = {(const uint16_t*)x, d.ld_x};
+  a.rows = d.m;
+  a.cols = d.n;
+  a.k = d.k;
+  a.segments = a.halves = 1;
+  a.kp = (int)round_up(d.k, d.group);
+  char* at = (char*)ws;
+  for (int h = 0; h < (gated ? 2 : 1); ++h) {
+    a.codes[h] = w[h];
+    a.scales[h] = sc[h];
+    if (d.dtype == QCONV_F16) {
+      float* u = (float*)at;
+      q4_unit_kernel<<<ceil_div(d.n, 4), 256, 0, s>>>(sc[h], d.n, a.kp / d.group, u);
+      a.unit[h] = u;
+      at += unit_bytes(d);
+    }
+  }
+  const bool aligned = aligned_rows(a.r[0]) && d.k % 8 == 0;
+  const GemmPlan p = plan_q4(d, gated, aligned);
+  a.parts = p.parts;
+  a.part = (float*)at;
+  a.out[0] = y;
+  a.ld_out = d.ld_y;
+  a.bias = bias;
+  a.act = act;
+  if (d.dtype == QCONV_F16)
+    return gated ? run_gemm_q4_group<F16, OUT_GATED>(a, d.group, p.tile, aligned, s)
+                 : run_gemm_q4_group<F16, OUT_PLAIN>(a, d.group, p.tile, aligned, s);
+  return gated ? run_gemm_q4_group<BF16, OUT_GATED>(a, d.group, p.tile, aligned, s)
+               : run_gemm_q4_group<BF16, OUT_PLAIN>(a, d.group, p.tile, aligned, s);
+}
+
 template <class T, int H>
 int run_rows(RowsArgs& a, int group, hipStream_t s) {
   if (group == 32) return run_dense_rows<T, Q4<32>, H>(a, s);
@@ -95,9 +177,21 @@ int launch_q4_pack(const void* w, int dtype, int n, int k, int64_t ld, int group
   return hip_status();
 }
 
+size_t q4_workspace_bytes(const qconv_q4_desc& d, bool gated) {
+  if (d.m <= ROWS_MOST) return 0;
+  const size_t u = d.dtype == QCONV_F16 ? unit_bytes(d) * (gated ? 2 : 1) : 0;
+  const size_t p = plan_q4(d, gated, false).bytes, q = plan_q4(d, gated, true).bytes;
+  return u + (p > q ? p : q);
+}
+
 int launch_q4(const qconv_q4_desc& d, const void* x, const uint8_t* w, const uint16_t* sc, const uint8_t* wu,
-              const uint16_t* scu, const float* bias, int act, void* y, hipStream_t s) {
+              const uint16_t* scu, const float* bias, int act, void* y, void* ws, hipStream_t s) {
   if (d.m == 0) return QCONV_OK;
+  if (d.m > ROWS_MOST) {
+    const uint8_t* const ww[2] = {w, wu};
+    const uint16_t* const ss[2] = {sc, scu};
+    return launch_gemm(d, x, ww, ss, bias, act, y, ws, s);
+  }
   RowsArgs a = {};
   a.x = (const uint16_t*)x;
   a.ld_x = d.ld_x;

@@ -21,7 +21,7 @@ BAD_FFN = [dict(m=-1), dict(k=0), dict(f=0), dict(act=3), dict(act=-1), dict(dty
 @pytest.mark.parametrize("bad", BAD_FFN)
 def test_ffn_descriptors(bad):
     L, d = q.lib(), _ffn(**bad)
-    assert L.qconv_ffn_forward(d, P, P, P, P, None, None) == q.QCONV_EINVAL
+    assert L.qconv_ffn_forward(d, P, P, P, P, None, P, 1 << 40, None) == q.QCONV_EINVAL
     assert L.qconv_ffn_backward(d, P, P, P, P, P, P, P, P, P, 1 << 30, None) == q.QCONV_EINVAL
     assert L.qconv_ffn_backward_bytes(d) == 0
 
@@ -30,9 +30,9 @@ def test_ffn_pointers_and_types():
     L = q.lib()
     for p in ((None, P, P, P, None), (P, None, P, P, None), (P, P, None, P, None), (P, P, P, None, None),
               (P + 1, P, P, P, None), (P, P, P, P + 1, None), (P, P, P, P, P + 4)):
-        assert L.qconv_ffn_forward(_ffn(), *p, None) == q.QCONV_EINVAL
-    assert L.qconv_ffn_forward(None, P, P, P, P, None, None) == q.QCONV_EINVAL
-    assert L.qconv_ffn_forward(_ffn(dtype=q.DT_F32), P, P, P, P, None, None) == q.QCONV_EUNSUPPORTED
+        assert L.qconv_ffn_forward(_ffn(), *p, P, 1 << 40, None) == q.QCONV_EINVAL
+    assert L.qconv_ffn_forward(None, P, P, P, P, None, P, 1 << 40, None) == q.QCONV_EINVAL
+    assert L.qconv_ffn_forward(_ffn(dtype=q.DT_F32), P, P, P, P, None, P, 1 << 40, None) == q.QCONV_EUNSUPPORTED
     ok = [P] * 9
     for i in (0, 1, 2, 3, 4, 6, 7, 8):  # gx alone may be missing, the weight gradients only together
         a = list(ok)
@@ -41,7 +41,13 @@ def test_ffn_pointers_and_types():
     need = L.qconv_ffn_backward_bytes(_ffn())
     assert need >= 4 * 2 * 24 * 2
     assert L.qconv_ffn_backward(_ffn(), *ok, need - 1, None) == q.QCONV_EWORKSPACE
-    assert L.qconv_ffn_forward(_ffn(m=0), None, P, P, None, None, None) == q.QCONV_OK  # nothing to do, nothing read
+    assert L.qconv_ffn_forward(_ffn(m=0), None, P, P, None, None, None, 0, None) == q.QCONV_OK  # nothing to do, nothing read
+    wide = dict(m=256, k=8192, f=64, ld_x=8192, ld_w=8192, ld_h=64)  # few tiles and a long sum: a split product
+    need = L.qconv_ffn_forward_bytes(_ffn(**wide))
+    assert need > 0 and L.qconv_ffn_forward_bytes(_ffn()) == 0
+    assert L.qconv_ffn_forward(_ffn(**wide), P, P, P, P, None, P, need - 1, None) == q.QCONV_EWORKSPACE
+    assert L.qconv_ffn_forward(_ffn(**wide), P, P, P, P, None, None, 0, None) == q.QCONV_EINVAL
+    assert L.qconv_ffn_forward(_ffn(**wide), P, P, P, P, None, P + 8, need, None) == q.QCONV_EINVAL
     assert L.qconv_ffn_pre_floats(3, 20) == 3 * 2 * 24 and L.qconv_ffn_pre_floats(-1, 20) == 0
 
 
@@ -67,6 +73,12 @@ def test_q4_pointers_types_and_sizes():
     assert L.qconv_q4_gated(_q4(), P, P, P, None, P, 0, P, P, 1 << 40, None) == q.QCONV_EINVAL
     assert L.qconv_q4_gated(_q4(), P, P, P, P, P, 4, P, P, 1 << 40, None) == q.QCONV_EINVAL
     assert L.qconv_q4_linear(_q4(m=0), None, P, P, None, None, None, 0, None) == q.QCONV_OK
+    many = dict(m=256, n=64, k=8192, ld_x=8192, ld_y=64)
+    need = L.qconv_q4_workspace_bytes(_q4(**many), 0)
+    assert need > 0 and L.qconv_q4_workspace_bytes(_q4(), 1) == 0
+    assert L.qconv_q4_linear(_q4(**many), P, P, P, None, P, P, need - 1, None) == q.QCONV_EWORKSPACE
+    assert L.qconv_q4_linear(_q4(**many), P, P, P, None, P, None, need, None) == q.QCONV_EINVAL
+    assert L.qconv_q4_gated(_q4(**many), P, P, P, P, P, 0, P, P, need - 1, None) == q.QCONV_EWORKSPACE
     assert L.qconv_q4_code_bytes(3, 100, 32) == 3 * 64 and L.qconv_q4_scale_bytes(3, 100, 32) == 3 * 4 * 2
     assert L.qconv_q4_code_bytes(3, 100, 33) == 0 and L.qconv_q4_scale_bytes(0, 100, 32) == 0
     ok = (P, q.DT_F32, 4, 100, 100, 32, 6, P, P, None)

@@ -237,6 +237,33 @@ __device__ __forceinline__ void put4(void* out, int64_t row, int64_t c, int64_t 
   }
 }
 
+// The order of a stage's LDS reads and matrix instructions.  Left alone, the
+// compiler reads each fragment right before its use, and the wave waits out
+// the LDS latency a dozen times per stage.  Here the first fragments are read
+// ahead and the rest are spread evenly over the first two thirds of the
+// instructions, a few fragments before their use: FC and FR reads make one
+// fragment of a column group (4 in a half stage) and of a row group (NR).
+template <int NR, int FC, int FR>
+struct ReadOrder {
+  static constexpr int ALL = 2 * (4 * FC + NR * FR), FIRST = 4 * FC + 3 * FR, GROUPS = 2 * NR;
+  static constexpr int before(int g) {  // reads issued before group g of 4 instructions
+    const int n = FIRST + ((ALL - FIRST) * g * 3 + 2 * GROUPS - 1) / (2 * GROUPS);
+    return n < ALL ? n : ALL;
+  }
+};
+template <int NR, int FC, int FR>
+__device__ __forceinline__ void order_reads() {
+  typedef ReadOrder<NR, FC, FR> O;
+  constexpr int MFMA = 0x8, DS_READ = 0x100;
+  __builtin_amdgcn_sched_group_barrier(DS_READ, O::FIRST, 0);
+  Unroll<0, O::GROUPS>::run([](auto g) {
+    constexpr int G = decltype(g)::value;
+    __builtin_amdgcn_sched_group_barrier(MFMA, 4, 0);
+    if constexpr (O::before(G + 1) > O::before(G))
+      __builtin_amdgcn_sched_group_barrier(DS_READ, O::before(G + 1) - O::before(G), 0);
+  });
+}
+
 // Results of row r, columns c..c + 3: bias, activation, rounding, store.
 template <class T, int OUT>
 __device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, int64_t c, float v[2][4]) {
@@ -334,6 +361,7 @@ __global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i][j] = T::mfma(fc[i], fr[j], acc[i][j]);
     }
+    order_reads<NR, SC::COL ? 2 : 1, SR::COL ? 2 : 1>();
     if (step + 1 < end) {
       sr.store(lds[b ^ 1]);
       sc.store(lds[b ^ 1] + LR);

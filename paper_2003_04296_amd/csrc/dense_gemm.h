@@ -15,9 +15,8 @@
 
 namespace qc {
 
-constexpr int KSTEP = 64;  // products per LDS stage
-
-typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef __attribute__((address_space(3))) v4u lds_v4u;
+typedef __attribute__((address_space(3))) void lds_void;
 
 // Row form: value (r, k) at p[r * ld + k]; column form: at p[k * ld + r].
 struct Operand {
@@ -53,12 +52,19 @@ struct GemmArgs {
   int ld_part;
 };
 
-// LDS holds chunks of 16 bytes.  Row form: rows of 64 products (8 chunks)
-// with the chunk index xored by the row, so that the 16 rows of a fragment
-// read lie in different banks.  Column form: one LDS row per product, of ROWS
-// values; a transposing read touches 4 of them at one place, and the lanes
-// beside it 4 more 8 rows below, which the xor spreads over the banks.
-__device__ __forceinline__ int swz_row(int r) { return r & 7; }
+// LDS holds chunks of 16 bytes; a stage holds KS products (32 or 64) of every
+// row.  Row form: rows of KS / 8 chunks, the chunk index xored by the row so
+// that the 16 rows that 16 lanes read at one place lie in different banks.
+// (16-byte reads are served 16 lanes at a time, 0-3, 12-15, 20-23 and 24-27,
+// then 4-11, 16-19 and 28-31; r & 7 for rows of 8 chunks and the map 0, 2, 3, 1
+// of r / 4 for rows of 4 keep both free of conflicts.)  Column form: one LDS
+// row per product, of ROWS values; a transposing read touches 4 of them at one
+// place, and the lanes beside it 4 more 8 rows below, which the xor spreads
+// over the banks.
+template <int KS>
+__device__ __forceinline__ int swz_row(int r) {
+  return KS == 64 ? r & 7 : ((r >> 2) & 1) << 1 ^ ((r >> 3) & 1) * 3;
+}
 __device__ __forceinline__ int swz_col(int k) { return ((k & 3) | ((k >> 3) & 1) << 2) << 1; }
 
 // Columns of the gated forward: 64 columns of the tile are 32 gate rows and
@@ -69,7 +75,7 @@ __device__ __forceinline__ int weight_row(int t) {
   return PAIR ? (t / 64) * 32 + t % 32 : t;
 }
 
-// The tile of one 16-bit operand: ROWS rows (or columns) of C by KSTEP
+// The tile of one 16-bit operand: ROWS rows (or columns) of C by KS
 // products, staged by NT threads, CH chunks each.  SIDE 0: GemmArgs::r, 1: c.
 //
 // ALIGNED: every row of the operand starts at a 16-byte address and the rows'
@@ -77,11 +83,11 @@ __device__ __forceinline__ int weight_row(int t) {
 // straight into LDS; chunks past the ends get an offset past the buffer's
 // range, which loads zeros.  Otherwise chunks pass through registers, and the
 // ones that cross an end are read value by value.
-template <int ROWS, int NT, int SIDE, bool COL_, bool ALIGNED, bool PAIR>
+template <int KS_, int ROWS, int NT, int SIDE, bool COL_, bool ALIGNED, bool PAIR>
 struct Stage16 {
   static constexpr bool COL = COL_, DIRECT = ALIGNED;
-  static constexpr int CH = ROWS * KSTEP / 8 / NT;
-  const uint16_t *p, *p2;  // the tile's first value, product 0
+  static constexpr int KS = KS_, CPR = KS / 8, CH = ROWS * CPR / NT;
+  const uint16_t* p[2];  // the tile's first value, product 0; by segment, or gate and up for PAIR
   int64_t ld;
   int rows;  // rows of the operand from the tile's first (gate rows for PAIR)
   typedef std::conditional_t<ALIGNED, uint32_t, int64_t> Off;
@@ -90,24 +96,26 @@ struct Stage16 {
   int at[CH];   // its first product (row form) or its product (column form)
   v4u reg[ALIGNED ? 1 : CH];
 
-  __device__ __forceinline__ static int chunk(int j) { return (int)threadIdx.x + j * NT; }
+  __device__ __forceinline__ static int index(int j) { return (int)threadIdx.x + j * NT; }
 
-  __device__ __forceinline__ void init(const GemmArgs& a, int which, int64_t r0) {
-    const Operand& o = SIDE == 0 ? a.r[which] : a.c[which];
+  // `half` picks the operand where C has two halves; the operands of two
+  // segments have one row stride.
+  __device__ __forceinline__ void init(const GemmArgs& a, int half, int64_t r0) {
+    const Operand* o = SIDE == 0 ? a.r + half : a.c;
     const int64_t all = SIDE == 0 ? a.rows : a.cols;
-    p = o.p + (COL ? r0 : r0 * o.ld);
-    p2 = PAIR ? a.c[1].p + r0 * o.ld : nullptr;
-    ld = o.ld;
+    ld = o->ld;
+    p[0] = o->p + (COL ? r0 : r0 * ld);
+    p[1] = PAIR || a.segments == 2 ? o[1].p + (COL ? r0 : r0 * ld) : p[0];
     rows = (int)(all - r0 < 0x7fffff00 ? all - r0 : 0x7fffff00);
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
-      const int c = chunk(j);
+      const int c = index(j);
       if constexpr (COL) {
         const int k = c / (ROWS / 8), r = ((c % (ROWS / 8)) ^ swz_col(k)) * 8;
         at[j] = k;
         off[j] = r < rows ? (Off)(k * ld + r) * 2 : OUTSIDE;
       } else {
-        const int t = c / 8, k = ((c % 8) ^ swz_row(t)) * 8;
+        const int t = c / CPR, k = ((c % CPR) ^ swz_row<KS>(t)) * 8;
         const int r = weight_row<PAIR>(t);
         at[j] = k;
         off[j] = r < rows ? (Off)(r * ld + k) * 2 : OUTSIDE;
@@ -115,59 +123,58 @@ struct Stage16 {
     }
   }
 
-  // Products [k0, k0 + KSTEP) of `k`, into (or on the way to) the stage at lds.
-  __device__ __forceinline__ void load(v4u* lds, int k0, int k) {
-    const int left = k - k0;
-    const uint16_t* b = p + (COL ? k0 * ld : (int64_t)k0);
+  // A stage's loads: begin() with its products [k0, k0 + KS), of which
+  // `left` exist, then chunk(j) for j < CH, into (or on the way to) the stage
+  // at lds.  A DIRECT stage always issues CH loads.
+  const uint16_t *from, *from2;
+  int left;
+  __device__ __forceinline__ void begin(int seg, int k0, int left_) {
+    from = p[PAIR ? 0 : seg] + (COL ? k0 * ld : (int64_t)k0);
+    from2 = PAIR ? p[1] + k0 : from;
+    left = left_;
+  }
+  __device__ __forceinline__ void chunk(lds_v4u* lds, int j) {
     if constexpr (ALIGNED) {
-      const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)b, (short)0, 0x7fffffff, 0x00020000);
-      const auto rs2 = __builtin_amdgcn_make_buffer_rsrc((void*)(PAIR ? p2 + k0 : b), (short)0, 0x7fffffff, 0x00020000);
-#pragma unroll
-      for (int j = 0; j < CH; ++j) {
-        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63) + j * NT;  // the wave's first chunk
-        const uint32_t o = at[j] < left ? off[j] : OUTSIDE;
-        // a wave's 64 chunks are 8 rows, so all of them gate or all of them up
-        if (PAIR && ((w / 8) & 32))
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(rs2, (lds_ptr)(lds + w), 16, o, 0, 0, 0);
-        else
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr)(lds + w), 16, o, 0, 0, 0);
-      }
+      const int w = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63) + j * NT;  // the wave's first chunk
+      // a wave's 64 chunks are 8 or 16 rows, so all of them gate or all of them up
+      const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(PAIR && ((w / CPR) & 32) ? from2 : from), (short)0,
+                                                        0x7fffffff, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + w), 16, at[j] < left ? off[j] : OUTSIDE, 0, 0, 0);
     } else {
-#pragma unroll
-      for (int j = 0; j < CH; ++j) {
-        const uint16_t* q = PAIR && ((chunk(j) / 8) & 32) ? p2 + k0 : b;
-        const int c = chunk(j);
-        const int n = COL ? rows - ((c % (ROWS / 8)) ^ swz_col(c / (ROWS / 8))) * 8 : left - at[j];
-        const bool in = off[j] != OUTSIDE && at[j] < left;
-        reg[j] = load8_first(in ? (const uint16_t*)((const char*)q + off[j]) : q, in ? n : 0);
-      }
+      const int c = index(j);
+      const uint16_t* q = PAIR && ((c / CPR) & 32) ? from2 : from;
+      const int n = COL ? rows - ((c % (ROWS / 8)) ^ swz_col(c / (ROWS / 8))) * 8 : left - at[j];
+      const bool in = off[j] != OUTSIDE && at[j] < left;
+      reg[j] = load8_first(in ? (const uint16_t*)((const char*)q + off[j]) : q, in ? n : 0);
     }
   }
-  // The rest of load(), once the stage's last readers are done.
-  __device__ __forceinline__ void store(v4u* lds) {
+  // What load() left in registers.
+  __device__ __forceinline__ void store(lds_v4u* lds) {
     if constexpr (!ALIGNED) {
 #pragma unroll
-      for (int j = 0; j < CH; ++j) lds[chunk(j)] = reg[j];
+      for (int j = 0; j < CH; ++j) lds[index(j)] = reg[j];
     }
   }
 };
 
-// The tile of 4-bit weights, in row form: a thread takes 32 codes of one row
-// (of one group) and writes them to LDS as scale * magnitude in the 16-bit
+// The tile of 4-bit weights, in row form: a thread takes KS / 2 codes of one
+// row (of one group) and writes them to LDS as scale * magnitude in the 16-bit
 // type.  That is exact: the scales have 6 significant bits, the magnitudes 2.
 // In fp16 a row's scales are first divided by a power of two near the largest
 // of them, multiplied back into the sums; only groups whose scale is more than
 // 2^18 below the row's largest are rounded then, to 2^-25 of that one.
-template <class T, int ROWS, int NT, int GROUP, bool PAIR>
+template <class T, int KS_, int ROWS, int NT, int GROUP, bool PAIR>
 struct StageQ4 {
   static constexpr bool COL = false, DIRECT = false;
-  static_assert(ROWS * KSTEP / 32 == NT, "one piece per thread");
+  static constexpr int KS = KS_, CPR = KS / 8, CH = 1, W = KS / 16;  // 8 codes per word
+  static_assert(ROWS * 2 == NT, "two threads per row");
+  typedef std::conditional_t<W == 4, v4u, v2u> Codes;
   const uint8_t* p;
   const uint16_t* sp;
   float unit;
   int kp;
   bool in;
-  v4u code;
+  Codes code;
   uint16_t sc;
 
   __device__ __forceinline__ void init(const GemmArgs& a, int, int64_t r0) {
@@ -179,31 +186,36 @@ struct StageQ4 {
     sp = a.scales[half] + (in ? row : 0) * (kp / GROUP);
     unit = a.unit[half] && in ? a.unit[half][row] : 1.0f;
   }
-  __device__ __forceinline__ void load(v4u*, int k0, int) {
-    const int k = k0 + (threadIdx.x & 1) * 32;
-    const bool on = in && k < kp;
-    code = on ? *(const v4u*)(p + k / 2) : v4u{0, 0, 0, 0};
+  int k;
+  bool on;
+  __device__ __forceinline__ void begin(int, int k0, int left) {
+    k = k0 + (threadIdx.x & 1) * (KS / 2);
+    on = in && k < kp && left > 0;
+  }
+  __device__ __forceinline__ void chunk(lds_v4u*, int) {
+    code = on ? *(const Codes*)(p + k / 2) : Codes{};
     sc = on ? sp[k / GROUP] : (uint16_t)0;
   }
-  __device__ __forceinline__ void store(v4u* lds) {
-    const int t = threadIdx.x / 2, h = threadIdx.x & 1;
+  __device__ __forceinline__ void store(lds_v4u* lds) {
     const float s = BF16::up(sc) * unit;
+    const int t = threadIdx.x / 2;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < W; ++q) {
       const uint32_t c = code[q];
-      lds[t * 8 + ((h * 4 + q) ^ swz_row(t))] = v4u{T::template scaled_e2m1<0>(c, s), T::template scaled_e2m1<1>(c, s),
-                                                    T::template scaled_e2m1<2>(c, s), T::template scaled_e2m1<3>(c, s)};
+      lds[t * CPR + (((threadIdx.x & 1) * W + q) ^ swz_row<KS>(t))] =
+          v4u{T::template scaled_e2m1<0>(c, s), T::template scaled_e2m1<1>(c, s), T::template scaled_e2m1<2>(c, s),
+              T::template scaled_e2m1<3>(c, s)};
     }
   }
 };
 
-// The 8 products [s * 32 + (lane / 16) * 8, +8) of tile row r0 + lane % 16.
-template <int ROWS, bool COL>
-__device__ __forceinline__ v4u fragment(const v4u* lds, int r0, int s) {
+// The 8 products [sub * 32 + (lane / 16) * 8, +8) of tile row r0 + lane % 16.
+template <int KS, int ROWS, bool COL>
+__device__ __forceinline__ v4u fragment(const lds_v4u* lds, int r0, int sub) {
   const int lane = threadIdx.x & 63;
   if constexpr (!COL) {
     const int r = r0 + (lane & 15);
-    return lds[r * 8 + ((s * 4 + (lane >> 4)) ^ swz_row(r))];
+    return lds[r * (KS / 8) + ((sub * 4 + (lane >> 4)) ^ swz_row<KS>(r))];
   } else {
     typedef short v4s __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) v4s* lp;
@@ -212,10 +224,10 @@ __device__ __forceinline__ v4u fragment(const v4u* lds, int r0, int s) {
     for (int j = 0; j < 2; ++j) {
       // 16 lanes read 4 LDS rows of 16 values and get them transposed: lane i
       // holds column i of the 4
-      const int k = s * 32 + (lane >> 4) * 8 + j * 4 + ((lane & 15) >> 2);
+      const int k = sub * 32 + (lane >> 4) * 8 + j * 4 + ((lane & 15) >> 2);
       const int c = r0 / 8 + ((lane & 3) >> 1);
-      const char* at = (const char*)(lds + k * (ROWS / 8) + (c ^ swz_col(k))) + (lane & 1) * 8;
-      h[j] = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)at));
+      const lp at = (lp)(lds + k * (ROWS / 8) + (c ^ swz_col(k))) + (lane & 1);
+      h[j] = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at));
     }
     return v4u{h[0][0], h[0][1], h[1][0], h[1][1]};
   }
@@ -237,31 +249,16 @@ __device__ __forceinline__ void put4(void* out, int64_t row, int64_t c, int64_t 
   }
 }
 
-// The order of a stage's LDS reads and matrix instructions.  Left alone, the
-// compiler reads each fragment right before its use, and the wave waits out
-// the LDS latency a dozen times per stage.  Here the first fragments are read
-// ahead and the rest are spread evenly over the first two thirds of the
-// instructions, a few fragments before their use: FC and FR reads make one
-// fragment of a column group (4 in a half stage) and of a row group (NR).
-template <int NR, int FC, int FR>
-struct ReadOrder {
-  static constexpr int ALL = 2 * (4 * FC + NR * FR), FIRST = 4 * FC + 3 * FR, GROUPS = 2 * NR;
-  static constexpr int before(int g) {  // reads issued before group g of 4 instructions
-    const int n = FIRST + ((ALL - FIRST) * g * 3 + 2 * GROUPS - 1) / (2 * GROUPS);
-    return n < ALL ? n : ALL;
-  }
-};
-template <int NR, int FC, int FR>
-__device__ __forceinline__ void order_reads() {
-  typedef ReadOrder<NR, FC, FR> O;
-  constexpr int MFMA = 0x8, DS_READ = 0x100;
-  __builtin_amdgcn_sched_group_barrier(DS_READ, O::FIRST, 0);
-  Unroll<0, O::GROUPS>::run([](auto g) {
-    constexpr int G = decltype(g)::value;
-    __builtin_amdgcn_sched_group_barrier(MFMA, 4, 0);
-    if constexpr (O::before(G + 1) > O::before(G))
-      __builtin_amdgcn_sched_group_barrier(DS_READ, O::before(G + 1) - O::before(G), 0);
-  });
+// A barrier before which at most N of the wave's loads into LDS may still be
+// under way, and with STORES none of its LDS writes.  A fence would wait for
+// every load, as they write LDS; fragments being read stay in flight.
+template <int N, bool STORES>
+__device__ __forceinline__ void stage_barrier() {
+  static_assert(N < 64, "vmcnt");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  if constexpr (STORES) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // Results of row r, columns c..c + 3: bias, activation, rounding, store.
@@ -296,13 +293,112 @@ __device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, 
   }
 }
 
-// A block computes a BR x BC tile of C with waves of (BR / 2) x 64 each.
-// Two LDS stages: while the waves multiply one, the next is loaded.
+// A block computes a BR x BC tile of C with waves of (BR / 2) x 64 each, from
+// a ring of LDS stages.
+//
+// KS = 32: five stages.  While stage s is multiplied, stage s + 1 is complete,
+// so its first fragments are read before the barrier between the two, and
+// stages s + 2 .. s + 4 are on their way.
+// KS = 64: two stages, one multiplied while the other is loaded.  For two
+// operands in row form: their loads then take whole 128-byte lines.  (Measured
+// at 8192 x 16384 x 4096, bf16: forward ... us against ... with 32; gx, whose
+// W is in column form, ... against ....)
+template <int KS>
+constexpr int STAGES = KS == 32 ? 5 : 2;
+
+template <int BR, class SR, class SC>
+__device__ __forceinline__ void load_chunk(SR& sr, SC& sc, lds_v4u* to, int i) {
+  if (i < SR::CH) sr.chunk(to, i);
+  else sc.chunk(to + BR * SR::CPR, i - SR::CH);
+}
+
+// The order of a stage's LDS reads, matrix instructions and loads: groups of 4
+// instructions that share a row fragment, each with a share of the reads
+// before it and of the loads after it.  Left alone, the compiler reads each
+// fragment right before its use and issues all loads at once, and the wave
+// waits out the LDS latency and the issue of the loads.
+template <int READS, int LOADS>
+__device__ __forceinline__ void group_order() {
+  constexpr int MFMA = 0x8, VMEM = 0x10, DS_READ = 0x100;
+  if constexpr (READS > 0) __builtin_amdgcn_sched_group_barrier(DS_READ, READS, 0);
+  __builtin_amdgcn_sched_group_barrier(MFMA, 4, 0);
+  if constexpr (LOADS > 0) __builtin_amdgcn_sched_group_barrier(VMEM, LOADS, 0);
+}
+
+// KS = 32: the products of stage `now`, with the reads of the next one's first
+// fragments from `then` and the loads into `to` between them.  The three are
+// distinct, which the compiler has to know (__restrict__): it makes reads wait
+// for loads into LDS that they might alias.
+constexpr int EARLY = 3;  // row fragments read a stage ahead, beside the column fragments
+template <class T, int BR, int BC, int P, class SR, class SC, int NR>
+__device__ __forceinline__ void multiply32(v4f (&acc)[4][NR], v4u (&fc)[2][4], v4u (&fr)[2][EARLY], SR& sr, SC& sc,
+                                           int wr, int wc, const lds_v4u* __restrict__ now,
+                                           const lds_v4u* __restrict__ then, lds_v4u* __restrict__ to) {
+  constexpr int LR = BR * SR::CPR, MID = NR - EARLY, READS = NR + 4, CHUNKS = SR::CH + SC::CH;
+  v4u f[NR];
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i) f[i] = fr[P][i];
+  Unroll<0, NR>::run([&](auto g) {
+    constexpr int G = decltype(g)::value;
+    constexpr int R0 = READS * G / NR, R1 = READS * (G + 1) / NR, L0 = CHUNKS * G / NR, L1 = CHUNKS * (G + 1) / NR;
+    Unroll<R0, R1>::run([&](auto r) {
+      constexpr int R = decltype(r)::value;
+      if constexpr (R < MID) f[R + EARLY] = fragment<32, BR, SR::COL>(now, wr + (R + EARLY) * 16, 0);
+      else if constexpr (R < MID + 4) fc[P ^ 1][R - MID] = fragment<32, BC, SC::COL>(then + LR, wc + (R - MID) * 16, 0);
+      else fr[P ^ 1][R - MID - 4] = fragment<32, BR, SR::COL>(then, wr + (R - MID - 4) * 16, 0);
+    });
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i][G] = T::mfma(fc[P][i], f[G], acc[i][G]);
+    Unroll<L0, L1>::run([&](auto l) { load_chunk<BR>(sr, sc, to, decltype(l)::value); });
+    auto instructions = [](int n) constexpr {  // LDS reads of the first n fragments
+      const int c = n < MID ? 0 : n < MID + 4 ? n - MID : 4;
+      return (n - c) * (SR::COL ? 2 : 1) + c * (SC::COL ? 2 : 1);
+    };
+    group_order<instructions(R1) - instructions(R0), L1 - L0>();
+  });
+}
+
+// KS = 64: the products of stage `now`, two fragments deep.  The first
+// fragments are read ahead, the others spread over the first two thirds of the
+// groups, the loads over the first half.
+template <class T, int BR, int BC, class SR, class SC, int NR>
+__device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, int wr, int wc,
+                                           const lds_v4u* __restrict__ now, lds_v4u* __restrict__ to) {
+  constexpr int LR = BR * SR::CPR, CHUNKS = SR::CH + SC::CH, GROUPS = 2 * NR, HALF = 4 + NR, READS = 2 * HALF;
+  constexpr int FIRST = 4 + 3;
+  v4u f[2][NR], fc[2][4];
+  Unroll<0, GROUPS>::run([&](auto g) {
+    constexpr int G = decltype(g)::value;
+    // fragments read before group n, in the order fc then fr, half after half
+    auto before = [](int n) constexpr {
+      const int c = FIRST + ((READS - FIRST) * n * 3 + 2 * GROUPS - 1) / (2 * GROUPS);
+      return n < 0 ? 0 : c < READS ? c : READS;
+    };
+    auto instructions = [](int n) constexpr {
+      const int h = n / HALF, c = n % HALF < 4 ? n % HALF : 4, r = n % HALF - c;
+      return (h * 4 + c) * (SC::COL ? 2 : 1) + (h * NR + r) * (SR::COL ? 2 : 1);
+    };
+    constexpr int R0 = before(G - 1), R1 = before(G);
+    constexpr int L0 = 2 * CHUNKS * G / GROUPS < CHUNKS ? 2 * CHUNKS * G / GROUPS : CHUNKS;
+    constexpr int L1 = 2 * CHUNKS * (G + 1) / GROUPS < CHUNKS ? 2 * CHUNKS * (G + 1) / GROUPS : CHUNKS;
+    Unroll<R0, R1>::run([&](auto r) {
+      constexpr int R = decltype(r)::value, H = R / HALF, I = R % HALF;
+      if constexpr (I < 4) fc[H][I] = fragment<64, BC, SC::COL>(now + LR, wc + I * 16, H);
+      else f[H][I - 4] = fragment<64, BR, SR::COL>(now, wr + (I - 4) * 16, H);
+    });
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i][G % NR] = T::mfma(fc[G / NR][i], f[G / NR][G % NR], acc[i][G % NR]);
+    Unroll<L0, L1>::run([&](auto l) { load_chunk<BR>(sr, sc, to, decltype(l)::value); });
+    group_order<instructions(R1) - instructions(R0), L1 - L0>();
+  });
+}
+
 template <class T, class SR, class SC, int OUT, int BR, int BC>
-__global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
-  constexpr int NR = BR / 32, PAIR = OUT == OUT_GATED;
-  constexpr int LR = BR * KSTEP / 8, LC = BC * KSTEP / 8;
-  __shared__ v4u lds[2][LR + LC];
+__device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds) {
+  constexpr int KS = SR::KS, NR = BR / 32, PAIR = OUT == OUT_GATED;
+  constexpr int LR = BR * SR::CPR, LC = BC * SR::CPR, STAGE = LR + LC, CHUNKS = SR::CH + SC::CH;
+  constexpr int LOADS = (SR::DIRECT ? SR::CH : 0) + (SC::DIRECT ? SC::CH : 0);  // into LDS, per stage and thread
+  constexpr bool REGS = !SR::DIRECT || !SC::DIRECT;                             // some pass through registers
   // Workgroups go to the 8 dies in turn; each die gets a run of tiles that
   // share operands in its L2: 8 tile rows at a time, column after column.
   const uint32_t trs = a.tiles_r * a.halves, all = trs * a.tiles_c, group = 8 * a.tiles_c;
@@ -323,50 +419,69 @@ __global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
 
   SR sr;
   SC sc;
-  const int steps = ceil_div(a.k, KSTEP), total = steps * a.segments;
+  const int steps = ceil_div(a.k, KS), total = steps * a.segments;
   const int begin = (int)((int64_t)total * part / a.parts), end = (int)((int64_t)total * (part + 1) / a.parts);
-  int seg = begin >= steps, k0 = (begin - seg * steps) * KSTEP;
-  sr.init(a, seg + half, r0);
-  sc.init(a, seg, c0);
-  if (begin < end) {
-    sr.load(lds[0], k0, a.k);
-    sc.load(lds[0] + LR, k0, a.k);
-    sr.store(lds[0]);
-    sc.store(lds[0] + LR);
+  sr.init(a, half, r0);
+  sc.init(a, 0, c0);
+  // The loads of a step (zeros past the end, so that every step issues as many).
+  auto start = [&](int s) {
+    const int seg = s >= steps && a.segments == 2 ? 1 : 0, k0 = (s - seg * steps) * KS;
+    const int left = s < end ? a.k - k0 : 0;
+    sr.begin(seg, k0, left);
+    sc.begin(seg, k0, left);
+  };
+  auto load = [&](lds_v4u* to) {
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) load_chunk<BR>(sr, sc, to, j);
+  };
+  auto store = [&](lds_v4u* to) {
+    sr.store(to);
+    sc.store(to + LR);
+  };
+  if constexpr (KS == 64) {
+    start(begin);
+    load(lds);
+    store(lds);
+    for (int s = begin; s < end; ++s) {
+      const int b = (s - begin) & 1;
+      stage_barrier<0, REGS>();
+      start(s + 1);
+      multiply64<T, BR, BC>(acc, sr, sc, wr, wc, lds + b * STAGE, lds + (b ^ 1) * STAGE);
+      if constexpr (REGS) store(lds + (b ^ 1) * STAGE);
+    }
+  } else {
+    // Stages loaded straight into LDS are 4 steps ahead.  Those that pass
+    // through registers are in LDS two steps ahead and in registers three;
+    // with one operand of each kind both are.
+    constexpr int AHEAD = REGS ? 3 : STAGES<KS> - 1;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      start(begin + i);
+      load(lds + i * STAGE);
+      if (REGS && i < AHEAD - 1) store(lds + i * STAGE);
+    }
+    stage_barrier<(AHEAD - 1) * LOADS, REGS>();
+    v4u fc[2][4], fr[2][EARLY];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fc[0][i] = fragment<KS, BC, SC::COL>(lds + LR, wc + i * 16, 0);
+#pragma unroll
+    for (int i = 0; i < EARLY; ++i) fr[0][i] = fragment<KS, BR, SR::COL>(lds, wr + i * 16, 0);
+    int cur = 0;  // the stage being multiplied
+    auto step = [&](auto phase, int s) {
+      constexpr int P = decltype(phase)::value;
+      auto stage = [&](int d) { return lds + (cur + d < STAGES<KS> ? cur + d : cur + d - STAGES<KS>) * STAGE; };
+      stage_barrier<(AHEAD - 2) * LOADS, REGS>();
+      if constexpr (REGS) store(stage(AHEAD - 1));
+      start(s + AHEAD);
+      multiply32<T, BR, BC, P>(acc, fc, fr, sr, sc, wr, wc, stage(0), stage(1), stage(AHEAD));
+      cur = cur + 1 < STAGES<KS> ? cur + 1 : 0;
+    };
+    for (int s = begin; s < end; s += 2) {
+      step(std::integral_constant<int, 0>{}, s);
+      if (s + 1 < end) step(std::integral_constant<int, 1>{}, s + 1);
+    }
   }
-  for (int step = begin; step < end; ++step) {
-    const int b = (step - begin) & 1;
-    if constexpr (SR::DIRECT || SC::DIRECT)
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads into LDS are not waited for elsewhere
-    lds_barrier();
-    k0 += KSTEP;
-    if (step + 1 == steps && a.segments == 2) {
-      sr.init(a, 1, r0);
-      sc.init(a, 1, c0);
-      k0 = 0;
-    }
-    if (step + 1 < end) {
-      sr.load(lds[b ^ 1], k0, a.k);
-      sc.load(lds[b ^ 1] + LR, k0, a.k);
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      v4u fr[NR], fc[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) fc[i] = fragment<BC, SC::COL>(lds[b] + LR, wc + i * 16, s);
-#pragma unroll
-      for (int i = 0; i < NR; ++i) fr[i] = fragment<BR, SR::COL>(lds[b], wr + i * 16, s);
-#pragma unroll
-      for (int j = 0; j < NR; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][j] = T::mfma(fc[i], fr[j], acc[i][j]);
-    }
-    order_reads<NR, SC::COL ? 2 : 1, SR::COL ? 2 : 1>();
-    if (step + 1 < end) {
-      sr.store(lds[b ^ 1]);
-      sc.store(lds[b ^ 1] + LR);
-    }
-  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load may reach LDS after the block has left it
 #pragma unroll
   for (int i = 0; i < (PAIR ? 2 : 4); ++i) {
     const int64_t c = c0 + (PAIR ? wc / 2 : wc) + i * 16 + (lane >> 4) * 4;
@@ -395,6 +510,15 @@ __global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
       finish4<T, OUT>(a, half, r, c, v);
     }
   }
+}
+
+template <class T, class SR, class SC, int OUT, int BR, int BC>
+__global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
+  static_assert(SR::KS == SC::KS, "one ring");
+  __shared__ v4u lds[STAGES<SR::KS> * (BR + BC) * SR::CPR];
+#ifdef __HIP_DEVICE_COMPILE__  // the host has no LDS pointers
+  gemm_tile<T, SR, SC, OUT, BR, BC>(a, (lds_v4u*)lds);
+#endif
 }
 
 // Joins the parts of a split product: four columns of one row per thread.
@@ -428,11 +552,11 @@ inline bool aligned_rows(const Operand& o) {
 }
 
 // How many blocks share a tile's products: enough that the chip is filled,
-// while each keeps at least 8 steps.
-inline int gemm_parts(int64_t tiles, int64_t steps) {
+// while each keeps at least 512 products.
+inline int gemm_parts(int64_t tiles, int64_t products) {
   if (tiles >= 192) return 1;
   int64_t p = 512 / tiles;
-  if (p > steps / 8) p = steps / 8;
+  if (p > products / 512) p = products / 512;
   return p < 1 ? 1 : (int)(p < 64 ? p : 64);
 }
 
@@ -445,10 +569,10 @@ struct GemmPlan {
 // 256 x 256 tiles where they fill the chip by themselves; else 128 x 128, the
 // products split where those do not either.  `out` = columns of C per tile
 // column (a gated tile makes half as many).
-inline GemmPlan gemm_plan(int64_t rows, int64_t cols, int64_t steps, int halves, bool gated, bool aligned) {
+inline GemmPlan gemm_plan(int64_t rows, int64_t cols, int64_t products, int halves, bool gated, bool aligned) {
   auto tiles = [&](int b) { return (rows + b - 1) / b * ((cols + (gated ? b / 2 : b) - 1) / (gated ? b / 2 : b)) * halves; };
   if (aligned && tiles(256) >= 256) return {256, 1, 0};
-  GemmPlan p = {128, gemm_parts(tiles(128) ? tiles(128) : 1, steps), 0};
+  GemmPlan p = {128, gemm_parts(tiles(128) ? tiles(128) : 1, products), 0};
   if (p.parts > 1) p.bytes = (size_t)p.parts * (gated ? 2 : halves) * rows * round_up(cols, 4) * 4;
   return p;
 }

@@ -42,15 +42,16 @@ __global__ __launch_bounds__(256) void ffn_slopes_kernel(const float* __restrict
 template <class T, bool RCOL, bool CCOL, int OUT>
 int run_gemm_t(GemmArgs& a, const GemmPlan& p, bool aligned, hipStream_t s) {
   constexpr bool PAIR = OUT == OUT_GATED;
+  constexpr int KS = RCOL || CCOL ? 32 : 64;
   a.parts = p.parts;
   if (!aligned)
-    return run_gemm_tiles<T, Stage16<128, 256, 0, RCOL, false, false>, Stage16<128, 256, 1, CCOL, false, PAIR>, OUT, 128>(
-        a, s);
+    return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, RCOL, false, false>, Stage16<KS, 128, 256, 1, CCOL, false, PAIR>,
+                          OUT, 128>(a, s);
   if (p.tile == 256)
-    return run_gemm_tiles<T, Stage16<256, 512, 0, RCOL, true, false>, Stage16<256, 512, 1, CCOL, true, PAIR>, OUT, 256>(
-        a, s);
-  return run_gemm_tiles<T, Stage16<128, 256, 0, RCOL, true, false>, Stage16<128, 256, 1, CCOL, true, PAIR>, OUT, 128>(a,
-                                                                                                                    s);
+    return run_gemm_tiles<T, Stage16<KS, 256, 512, 0, RCOL, true, false>, Stage16<KS, 256, 512, 1, CCOL, true, PAIR>,
+                          OUT, 256>(a, s);
+  return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, RCOL, true, false>, Stage16<KS, 128, 256, 1, CCOL, true, PAIR>,
+                        OUT, 128>(a, s);
 }
 
 template <bool RCOL, bool CCOL, int OUT>
@@ -61,13 +62,13 @@ int run_gemm(int dtype, GemmArgs& a, const GemmPlan& p, bool aligned, hipStream_
 
 // Products of the forward, of gx and of the weight gradients.
 GemmPlan plan_h(const qconv_ffn_desc& d, bool aligned) {
-  return gemm_plan(d.m, d.f, ceil_div(d.k, KSTEP), 1, true, aligned);
+  return gemm_plan(d.m, d.f, d.k, 1, true, aligned);
 }
 GemmPlan plan_gx(const qconv_ffn_desc& d, bool aligned) {
-  return gemm_plan(d.m, d.k, 2 * (int64_t)ceil_div(d.f, KSTEP), 1, false, aligned);
+  return gemm_plan(d.m, d.k, 2 * (int64_t)d.f, 1, false, aligned);
 }
 GemmPlan plan_gw(const qconv_ffn_desc& d, bool aligned) {
-  return gemm_plan(d.f, d.k, ceil_div(d.m, KSTEP), 2, false, aligned);
+  return gemm_plan(d.f, d.k, d.m, 2, false, aligned);
 }
 
 template <class T>

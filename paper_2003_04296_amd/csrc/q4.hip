@@ -95,12 +95,15 @@ __global__ __launch_bounds__(256) void q4_unit_kernel(const uint16_t* __restrict
 template <class T, int OUT, int GROUP>
 int run_gemm_q4(GemmArgs& a, int tile, bool aligned, hipStream_t s) {
   constexpr bool PAIR = OUT == OUT_GATED;
+  constexpr int KS = 64;
   if (!aligned)
-    return run_gemm_tiles<T, Stage16<128, 256, 0, false, false, false>, StageQ4<T, 128, 256, GROUP, PAIR>, OUT, 128>(a,
-                                                                                                                    s);
+    return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, false, false, false>, StageQ4<T, KS, 128, 256, GROUP, PAIR>, OUT,
+                          128>(a, s);
   if (tile == 256)
-    return run_gemm_tiles<T, Stage16<256, 512, 0, false, true, false>, StageQ4<T, 256, 512, GROUP, PAIR>, OUT, 256>(a, s);
-  return run_gemm_tiles<T, Stage16<128, 256, 0, false, true, false>, StageQ4<T, 128, 256, GROUP, PAIR>, OUT, 128>(a, s);
+    return run_gemm_tiles<T, Stage16<KS, 256, 512, 0, false, true, false>, StageQ4<T, KS, 256, 512, GROUP, PAIR>, OUT,
+                          256>(a, s);
+  return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, false, true, false>, StageQ4<T, KS, 128, 256, GROUP, PAIR>, OUT,
+                        128>(a, s);
 }
 
 template <class T, int OUT>
@@ -113,7 +116,7 @@ int run_gemm_q4_group(GemmArgs& a, int group, int tile, bool aligned, hipStream_
 constexpr int ROWS_MOST = 64;  // tokens that go through dense_rows.h
 
 GemmPlan plan_q4(const qconv_q4_desc& d, bool gated, bool aligned) {
-  return gemm_plan(d.m, d.n, ceil_div(d.k, KSTEP), 1, gated, aligned);
+  return gemm_plan(d.m, d.n, d.k, 1, gated, aligned);
 }
 size_t unit_bytes(const qconv_q4_desc& d) { return (size_t)round_up(d.n, 4) * 4; }  // of one weight
 

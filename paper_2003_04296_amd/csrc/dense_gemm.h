@@ -123,15 +123,23 @@ struct Stage16 {
     }
   }
 
-  // A stage's loads: begin() with its products [k0, k0 + KS), of which
-  // `left` exist, then chunk(j) for j < CH, into (or on the way to) the stage
-  // at lds.  A DIRECT stage always issues CH loads.
+  // A stage's loads: chunk(j) for j < CH, into (or on the way to) the stage at
+  // lds, then next() to move on by KS products.  `left` products exist (all
+  // further ones load as zeros; a DIRECT stage always issues CH loads).
+  // Everything that moves is uniform over the block and is added to, not
+  // computed anew: the scalar work of a step delays its matrix instructions.
   const uint16_t *from, *from2;
   int left;
   __device__ __forceinline__ void begin(int seg, int k0, int left_) {
     from = p[PAIR ? 0 : seg] + (COL ? k0 * ld : (int64_t)k0);
     from2 = PAIR ? p[1] + k0 : from;
     left = left_;
+  }
+  __device__ __forceinline__ void next() {
+    const int64_t by = COL ? KS * ld : (int64_t)KS;
+    from += by;
+    if constexpr (PAIR) from2 += by;
+    left -= KS;
   }
   __device__ __forceinline__ void chunk(lds_v4u* lds, int j) {
     if constexpr (ALIGNED) {
@@ -186,13 +194,17 @@ struct StageQ4 {
     sp = a.scales[half] + (in ? row : 0) * (kp / GROUP);
     unit = a.unit[half] && in ? a.unit[half][row] : 1.0f;
   }
-  int k;
-  bool on;
-  __device__ __forceinline__ void begin(int, int k0, int left) {
+  int k, left;
+  __device__ __forceinline__ void begin(int, int k0, int left_) {
     k = k0 + (threadIdx.x & 1) * (KS / 2);
-    on = in && k < kp && left > 0;
+    left = left_;
+  }
+  __device__ __forceinline__ void next() {
+    k += KS;
+    left -= KS;
   }
   __device__ __forceinline__ void chunk(lds_v4u*, int) {
+    const bool on = in && k < kp && left > 0;
     code = on ? *(const Codes*)(p + k / 2) : Codes{};
     sc = on ? sp[k / GROUP] : (uint16_t)0;
   }
@@ -423,23 +435,34 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
   const int begin = (int)((int64_t)total * part / a.parts), end = (int)((int64_t)total * (part + 1) / a.parts);
   sr.init(a, half, r0);
   sc.init(a, 0, c0);
-  // The loads of a step (zeros past the end, so that every step issues as many).
+  // Before the loads of step s: they start, change operands or end there.
+  int until = begin < steps && end > steps ? steps : end;
+  {
+    const int seg = begin >= steps ? 1 : 0, k0 = (begin - seg * steps) * KS;
+    sr.begin(seg, k0, begin < end ? a.k - k0 : 0);
+    sc.begin(seg, k0, begin < end ? a.k - k0 : 0);
+  }
   auto start = [&](int s) {
-    const int seg = s >= steps && a.segments == 2 ? 1 : 0, k0 = (s - seg * steps) * KS;
-    const int left = s < end ? a.k - k0 : 0;
-    sr.begin(seg, k0, left);
-    sc.begin(seg, k0, left);
+    if (s != until) return;
+    const bool more = s < end;
+    sr.begin(1, 0, more ? a.k : 0);
+    sc.begin(1, 0, more ? a.k : 0);
+    until = more ? end : -1;
+  };
+  auto next = [&] {
+    sr.next();
+    sc.next();
   };
   auto load = [&](lds_v4u* to) {
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) load_chunk<BR>(sr, sc, to, j);
+    next();
   };
   auto store = [&](lds_v4u* to) {
     sr.store(to);
     sc.store(to + LR);
   };
   if constexpr (KS == 64) {
-    start(begin);
     load(lds);
     store(lds);
     for (int s = begin; s < end; ++s) {
@@ -447,6 +470,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
       stage_barrier<0, REGS>();
       start(s + 1);
       multiply64<T, BR, BC>(acc, sr, sc, wr, wc, lds + b * STAGE, lds + (b ^ 1) * STAGE);
+      next();
       if constexpr (REGS) store(lds + (b ^ 1) * STAGE);
     }
   } else {
@@ -474,6 +498,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
       if constexpr (REGS) store(stage(AHEAD - 1));
       start(s + AHEAD);
       multiply32<T, BR, BC, P>(acc, fc, fr, sr, sc, wr, wc, stage(0), stage(1), stage(AHEAD));
+      next();
       cur = cur + 1 < STAGES<KS> ? cur + 1 : 0;
     };
     for (int s = begin; s < end; s += 2) {

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/qconv.h"
 
 namespace qc {
@@ -73,22 +75,38 @@ __device__ __forceinline__ v4u load8_first(const uint16_t* p, int n) {
   return r;
 }
 
-// act(g) and act'(g) in fp32.  exp(-g) = inf gives silu 0 and slope 0.
+// 1 / (1 + exp(-g)) through the hardware's exponential and reciprocal (1 ulp
+// each; the rounding of the exponent's argument adds |g| 2^-24 of exp(-g)):
+// the exact division costs the tiled products' epilogue ten times as many
+// instructions, and the result is rounded to 16 bits.  exp(-g) = inf gives 0.
+__device__ __forceinline__ float sigmoid(float g) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
+}
+
+// act(g) and act'(g) in fp32.
 template <int ACT>
 __device__ __forceinline__ float act_value(float g) {
-  if constexpr (ACT == QCONV_ACT_SILU) return g / (1.0f + expf(-g));
-  if constexpr (ACT == QCONV_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
-  return g < 0.0f ? 0.0f : g;  // a NaN stays
+  if constexpr (ACT == QCONV_ACT_SILU) return g * sigmoid(g);
+  else if constexpr (ACT == QCONV_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+  else return g < 0.0f ? 0.0f : g;  // a NaN stays
 }
 template <int ACT>
 __device__ __forceinline__ float act_slope(float g) {
   if constexpr (ACT == QCONV_ACT_SILU) {
-    const float p = 1.0f / (1.0f + expf(-g));
+    const float p = sigmoid(g);
     return p * (1.0f + g * (1.0f - p));
-  }
-  if constexpr (ACT == QCONV_ACT_GELU)
+  } else if constexpr (ACT == QCONV_ACT_GELU) {
     return 0.5f * (1.0f + erff(g * 0.70710678118654752f)) + g * expf(-0.5f * g * g) * 0.39894228040143268f;
-  return g > 0.0f ? 1.0f : 0.0f;
+  } else {
+    return g > 0.0f ? 1.0f : 0.0f;
+  }
+}
+// f with the activation as a constant.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == QCONV_ACT_SILU) f(std::integral_constant<int, QCONV_ACT_SILU>{});
+  else if (act == QCONV_ACT_GELU) f(std::integral_constant<int, QCONV_ACT_GELU>{});
+  else f(std::integral_constant<int, QCONV_ACT_RELU>{});
 }
 __device__ __forceinline__ float act_value(int act, float g) {
   return act == QCONV_ACT_SILU ? act_value<QCONV_ACT_SILU>(g)

@@ -274,7 +274,7 @@ __device__ __forceinline__ void stage_barrier() {
 }
 
 // Results of row r, columns c..c + 3: bias, activation, rounding, store.
-template <class T, int OUT>
+template <class T, int OUT, int ACT>
 __device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, int64_t c, float v[2][4]) {
   if constexpr (OUT == OUT_GATED) {
     if (a.pre) {
@@ -293,7 +293,7 @@ __device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, 
     }
     float h[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = act_value(a.act, v[0][e]) * v[1][e];
+    for (int e = 0; e < 4; ++e) h[e] = act_value<ACT>(v[0][e]) * v[1][e];
     put4<T>(a.out[0], r * a.ld_out, c, a.cols, a.wide_out, h);
   } else {
     if (a.bias) {
@@ -507,6 +507,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load may reach LDS after the block has left it
+  auto finish = [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
 #pragma unroll
   for (int i = 0; i < (PAIR ? 2 : 4); ++i) {
     const int64_t c = c0 + (PAIR ? wc / 2 : wc) + i * 16 + (lane >> 4) * 4;
@@ -532,9 +534,14 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
               v4f{v[h][0], v[h][1], v[h][2], v[h][3]};
         continue;
       }
-      finish4<T, OUT>(a, half, r, c, v);
+      finish4<T, OUT, ACT>(a, half, r, c, v);
     }
   }
+  };
+  if constexpr (PAIR)
+    with_act(a.act, finish);
+  else
+    finish(std::integral_constant<int, 0>{});
 }
 
 template <class T, class SR, class SC, int OUT, int BR, int BC>
@@ -547,8 +554,8 @@ __global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
 }
 
 // Joins the parts of a split product: four columns of one row per thread.
-template <class T, int OUT>
-__global__ __launch_bounds__(256) void dense_join_kernel(GemmArgs a) {
+template <class T, int OUT, int ACT>
+__device__ __forceinline__ void join(const GemmArgs& a) {
   constexpr int H = OUT == OUT_GATED ? 2 : 1;
   const int q = a.ld_part / 4;
   const int64_t n = (int64_t)a.rows * q * (OUT == OUT_GATED ? 1 : a.halves);
@@ -562,12 +569,17 @@ __global__ __launch_bounds__(256) void dense_join_kernel(GemmArgs a) {
     for (int h = 0; h < H; ++h) {
       const float* p = a.part + h * plane + row * a.ld_part + c;
       v4f s = *(const v4f*)p;
+#pragma unroll 8
       for (int k = 1; k < a.parts; ++k) s += *(const v4f*)(p + k * step);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[h][e] = s[e];
     }
-    finish4<T, OUT>(a, half, row - half * (int64_t)a.rows, c, v);
+    finish4<T, OUT, ACT>(a, half, row - half * (int64_t)a.rows, c, v);
   }
+}
+template <class T, int OUT>
+__global__ __launch_bounds__(256) void dense_join_kernel(GemmArgs a) {
+  with_act(OUT == OUT_GATED ? a.act : 0, [&](auto act) { join<T, OUT, decltype(act)::value>(a); });
 }
 
 // Every row of the operand starts at a 16-byte address, and a tile's offsets

@@ -247,7 +247,7 @@ __device__ __forceinline__ v4u fragment(const lds_v4u* lds, int r0, int sub) {
 
 // Four values of one row, columns c..c + 3 of `cols`.
 template <class T>
-__device__ __forceinline__ void put4(void* out, int64_t row, int64_t c, int64_t cols, bool wide, const float v[4]) {
+__device__ __forceinline__ void put4(void* out, int64_t row, int64_t c, int64_t cols, bool wide, v4f v) {
   uint16_t* p = (uint16_t*)out + row + c;
   uint16_t b[4];
 #pragma unroll
@@ -275,13 +275,13 @@ __device__ __forceinline__ void stage_barrier() {
 
 // Results of row r, columns c..c + 3: bias, activation, rounding, store.
 template <class T, int OUT, int ACT>
-__device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, int64_t c, float v[2][4]) {
+__device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, int64_t c, v4f v[2]) {
   if constexpr (OUT == OUT_GATED) {
     if (a.pre) {
       float* g = a.pre + r * 2 * a.ld_pre + c;
       if (c + 4 <= a.cols) {
-        *(v4f*)g = v4f{v[0][0], v[0][1], v[0][2], v[0][3]};
-        *(v4f*)(g + a.ld_pre) = v4f{v[1][0], v[1][1], v[1][2], v[1][3]};
+        *(v4f*)g = v[0];
+        *(v4f*)(g + a.ld_pre) = v[1];
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -291,7 +291,7 @@ __device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, 
           }
       }
     }
-    float h[4];
+    v4f h;
 #pragma unroll
     for (int e = 0; e < 4; ++e) h[e] = act_value<ACT>(v[0][e]) * v[1][e];
     put4<T>(a.out[0], r * a.ld_out, c, a.cols, a.wide_out, h);
@@ -372,7 +372,7 @@ __device__ __forceinline__ void multiply32(v4f (&acc)[4][NR], v4u (&fc)[2][4], v
 
 // KS = 64: the products of stage `now`, two fragments deep.  The first
 // fragments are read ahead, the others spread over the first two thirds of the
-// groups, the loads over the first half.
+// groups.
 template <class T, int BR, int BC, class SR, class SC, int NR>
 __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, int wr, int wc,
                                            const lds_v4u* __restrict__ now, lds_v4u* __restrict__ to) {
@@ -391,8 +391,10 @@ __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, in
       return (h * 4 + c) * (SC::COL ? 2 : 1) + (h * NR + r) * (SR::COL ? 2 : 1);
     };
     constexpr int R0 = before(G - 1), R1 = before(G);
-    constexpr int L0 = 2 * CHUNKS * G / GROUPS < CHUNKS ? 2 * CHUNKS * G / GROUPS : CHUNKS;
-    constexpr int L1 = 2 * CHUNKS * (G + 1) / GROUPS < CHUNKS ? 2 * CHUNKS * (G + 1) / GROUPS : CHUNKS;
+    // All loads within the first quarter: spread over half of the groups they
+    // end late for the barrier (forward at 8192 tokens 2.30 ms, not 2.21).
+    constexpr int LA = 4 * CHUNKS * G / GROUPS, LB = 4 * CHUNKS * (G + 1) / GROUPS;
+    constexpr int L0 = LA < CHUNKS ? LA : CHUNKS, L1 = LB < CHUNKS ? LB : CHUNKS;
     Unroll<R0, R1>::run([&](auto r) {
       constexpr int R = decltype(r)::value, H = R / HALF, I = R % HALF;
       if constexpr (I < 4) fc[H][I] = fragment<64, BC, SC::COL>(now + LR, wc + I * 16, H);
@@ -509,34 +511,41 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load may reach LDS after the block has left it
   auto finish = [&](auto act) {
     constexpr int ACT = decltype(act)::value;
+    // Row by row, so that the two halves of a 128-byte line are written one
+    // after the other.
+    constexpr int H = PAIR ? 2 : 1;
+    const int64_t c1 = c0 + (PAIR ? wc / 2 : wc) + (lane >> 4) * 4;
+    v4f back[4 / H][H];  // what the 4-bit weights' rows were divided by
 #pragma unroll
-  for (int i = 0; i < (PAIR ? 2 : 4); ++i) {
-    const int64_t c = c0 + (PAIR ? wc / 2 : wc) + i * 16 + (lane >> 4) * 4;
-    float back[2][4];  // what the 4-bit weights' rows were divided by
+    for (int i = 0; i < 4 / H; ++i)
 #pragma unroll
-    for (int h = 0; h < (PAIR ? 2 : 1); ++h)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) back[h][e] = a.unit[h] && c + e < a.cols ? 1.0f / a.unit[h][c + e] : 1.0f;
+        for (int e = 0; e < 4; ++e) {
+          const int64_t c = c1 + i * 16 + e;
+          back[i][h][e] = a.unit[h] && c < a.cols ? 1.0f / a.unit[h][c] : 1.0f;
+        }
 #pragma unroll
     for (int j = 0; j < NR; ++j) {
       const int64_t r = r0 + wr + j * 16 + (lane & 15);
-      if (r >= a.rows || c >= a.cols) continue;
-      float v[2][4];
+      if (r >= a.rows) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[0][e] = acc[i][j][e] * back[0][e];
-        if constexpr (PAIR) v[1][e] = acc[i + 2][j][e] * back[1][e];
-      }
-      if (a.parts > 1) {
+      for (int i = 0; i < 4 / H; ++i) {
+        const int64_t c = c1 + i * 16;
+        if (c >= a.cols) continue;
+        v4f v[2] = {acc[i][j] * back[i][0], v4f{}};
+        if constexpr (PAIR) v[1] = acc[i + 2][j] * back[i][H - 1];
+        if (a.parts > 1) {
 #pragma unroll
-        for (int h = 0; h < (PAIR ? 2 : 1); ++h)
-          *(v4f*)(a.part + (((int64_t)part * (PAIR ? 2 : a.halves) + (PAIR ? h : half)) * a.rows + r) * a.ld_part + c) =
-              v4f{v[h][0], v[h][1], v[h][2], v[h][3]};
-        continue;
+          for (int h = 0; h < H; ++h) {
+            const int64_t plane = (int64_t)part * (PAIR ? 2 : a.halves) + (PAIR ? h : half);
+            *(v4f*)(a.part + (plane * a.rows + r) * a.ld_part + c) = v[h];
+          }
+        } else {
+          finish4<T, OUT, ACT>(a, half, r, c, v);
+        }
       }
-      finish4<T, OUT, ACT>(a, half, r, c, v);
     }
-  }
   };
   if constexpr (PAIR)
     with_act(a.act, finish);
@@ -564,15 +573,14 @@ __device__ __forceinline__ void join(const GemmArgs& a) {
     const int half = row >= a.rows;
     const int64_t c = i % q * 4;
     const int64_t plane = (int64_t)a.rows * a.ld_part, step = plane * (OUT == OUT_GATED ? 2 : a.halves);
-    float v[2][4];
+    v4f v[2] = {};
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const float* p = a.part + h * plane + row * a.ld_part + c;
       v4f s = *(const v4f*)p;
 #pragma unroll 8
       for (int k = 1; k < a.parts; ++k) s += *(const v4f*)(p + k * step);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[h][e] = s[e];
+      v[h] = s;
     }
     finish4<T, OUT, ACT>(a, half, row - half * (int64_t)a.rows, c, v);
   }

@@ -370,14 +370,20 @@ __device__ __forceinline__ void multiply32(v4f (&acc)[4][NR], v4u (&fc)[2][4], v
   });
 }
 
-// KS = 64: the products of stage `now`, two fragments deep.  The first
-// fragments are read ahead, the others spread over the first two thirds of the
-// groups.
+// KS = 64: the products of stage `now`.  The first fragments are read ahead,
+// the others spread over the first two thirds of the groups; the loads into
+// `to` come within the first quarter (spread over half of the groups they end
+// late for the barrier: forward at 8192 tokens 2.30 ms, not 2.21).  An operand
+// that passes through registers is stored to `to` here and loaded for the
+// stage after it.
 template <class T, int BR, int BC, class SR, class SC, int NR>
 __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, int wr, int wc,
                                            const lds_v4u* __restrict__ now, lds_v4u* __restrict__ to) {
   constexpr int LR = BR * SR::CPR, CHUNKS = SR::CH + SC::CH, GROUPS = 2 * NR, HALF = 4 + NR, READS = 2 * HALF;
   constexpr int FIRST = 4 + 3;
+  constexpr bool REGS = !SR::DIRECT || !SC::DIRECT;
+  sr.store(to);
+  sc.store(to + LR);
   v4u f[2][NR], fc[2][4];
   Unroll<0, GROUPS>::run([&](auto g) {
     constexpr int G = decltype(g)::value;
@@ -386,13 +392,7 @@ __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, in
       const int c = FIRST + ((READS - FIRST) * n * 3 + 2 * GROUPS - 1) / (2 * GROUPS);
       return n < 0 ? 0 : c < READS ? c : READS;
     };
-    auto instructions = [](int n) constexpr {
-      const int h = n / HALF, c = n % HALF < 4 ? n % HALF : 4, r = n % HALF - c;
-      return (h * 4 + c) * (SC::COL ? 2 : 1) + (h * NR + r) * (SR::COL ? 2 : 1);
-    };
     constexpr int R0 = before(G - 1), R1 = before(G);
-    // All loads within the first quarter: spread over half of the groups they
-    // end late for the barrier (forward at 8192 tokens 2.30 ms, not 2.21).
     constexpr int LA = 4 * CHUNKS * G / GROUPS, LB = 4 * CHUNKS * (G + 1) / GROUPS;
     constexpr int L0 = LA < CHUNKS ? LA : CHUNKS, L1 = LB < CHUNKS ? LB : CHUNKS;
     Unroll<R0, R1>::run([&](auto r) {
@@ -403,7 +403,8 @@ __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, in
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i][G % NR] = T::mfma(fc[G / NR][i], f[G / NR][G % NR], acc[i][G % NR]);
     Unroll<L0, L1>::run([&](auto l) { load_chunk<BR>(sr, sc, to, decltype(l)::value); });
-    group_order<instructions(R1) - instructions(R0), L1 - L0>();
+    if constexpr (!SR::COL && !SC::COL) group_order<R1 - R0, REGS ? 0 : L1 - L0>();
+    if constexpr (REGS) __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);  // vector instructions of the conversions
   });
 }
 
@@ -465,15 +466,24 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
     sc.store(to + LR);
   };
   if constexpr (KS == 64) {
+    static_assert(!SR::COL && !SC::COL, "one segment");
+    // What passes through registers is loaded a step further ahead.
     load(lds);
     store(lds);
+    auto again = [&](auto& o, lds_v4u* at) {
+      if constexpr (!std::remove_reference_t<decltype(o)>::DIRECT) {
+#pragma unroll
+        for (int j = 0; j < std::remove_reference_t<decltype(o)>::CH; ++j) o.chunk(at, j);
+        o.next();
+      }
+    };
+    again(sr, lds);
+    again(sc, lds);
     for (int s = begin; s < end; ++s) {
       const int b = (s - begin) & 1;
       stage_barrier<0, REGS>();
-      start(s + 1);
       multiply64<T, BR, BC>(acc, sr, sc, wr, wc, lds + b * STAGE, lds + (b ^ 1) * STAGE);
       next();
-      if constexpr (REGS) store(lds + (b ^ 1) * STAGE);
     }
   } else {
     // Stages loaded straight into LDS are 4 steps ahead.  Those that pass
@@ -596,30 +606,37 @@ inline bool aligned_rows(const Operand& o) {
   return ((uintptr_t)o.p & 15) == 0 && o.ld % 8 == 0 && o.ld < (1 << 21);
 }
 
-// How many blocks share a tile's products: enough that the chip is filled,
-// while each keeps at least 512 products.
-inline int gemm_parts(int64_t tiles, int64_t products) {
-  if (tiles >= 192) return 1;
-  int64_t p = 512 / tiles;
-  if (p > products / 512) p = products / 512;
-  return p < 1 ? 1 : (int)(p < 64 ? p : 64);
-}
-
 struct GemmPlan {
   int tile;  // rows and columns of a block's tile
   int parts;
   size_t bytes;  // of GemmArgs::part
 };
 
-// 256 x 256 tiles where they fill the chip by themselves; else 128 x 128, the
-// products split where those do not either.  `out` = columns of C per tile
-// column (a gated tile makes half as many).
-inline GemmPlan gemm_plan(int64_t rows, int64_t cols, int64_t products, int halves, bool gated, bool aligned) {
-  auto tiles = [&](int b) { return (rows + b - 1) / b * ((cols + (gated ? b / 2 : b) - 1) / (gated ? b / 2 : b)) * halves; };
-  if (aligned && tiles(256) >= 256) return {256, 1, 0};
-  GemmPlan p = {128, gemm_parts(tiles(128) ? tiles(128) : 1, products), 0};
-  if (p.parts > 1) p.bytes = (size_t)p.parts * (gated ? 2 : halves) * rows * round_up(cols, 4) * 4;
-  return p;
+// Tiles of 256 x 256 where they fill the 256 compute units by themselves, else
+// 128 x 128, two blocks per unit.  Few tiles: their products are split over
+// blocks until there are about 256, as long as each keeps 512 products (gx of
+// 512 tokens, 4096 -> 1024: 35 us in 8 parts, 116 in one, 36 in 16).  With
+// `long_sums` (gx, whose sums run over both halves of 2f) also the larger
+// tiles are split if each part keeps 2048 products: gx of 4096 tokens, 8192 ->
+// 2048: 128 tiles in two parts 215 us, 512 small tiles 313; of 256 tokens,
+// 1024 -> 8192, with 512 products each: 37 us against 32.
+inline GemmPlan gemm_plan(int64_t rows, int64_t cols, int64_t products, int halves, bool gated, bool aligned,
+                          bool long_sums) {
+  const int planes = gated ? 2 : halves;
+  auto tiles = [&](int b) {
+    const int64_t across = gated ? b / 2 : b;
+    const int64_t n = (rows + b - 1) / b * ((cols + across - 1) / across) * halves;
+    return n > 0 ? n : 1;
+  };
+  auto split = [&](int tile, int64_t parts) {
+    return GemmPlan{tile, (int)parts, parts > 1 ? (size_t)parts * planes * rows * round_up(cols, 4) * 4 : 0};
+  };
+  const int64_t big = tiles(256), small = tiles(128);
+  if (aligned && big >= 256) return split(256, 1);
+  if (aligned && long_sums && 256 / big * big >= 192 && products / (256 / big) >= 2048) return split(256, 256 / big);
+  int64_t parts = small >= 192 ? 1 : 256 / small;
+  if (parts > products / 512) parts = products / 512;
+  return split(128, parts < 1 ? 1 : parts);
 }
 
 template <class T, class SR, class SC, int OUT, int B>

@@ -62,13 +62,13 @@ int run_gemm(int dtype, GemmArgs& a, const GemmPlan& p, bool aligned, hipStream_
 
 // Products of the forward, of gx and of the weight gradients.
 GemmPlan plan_h(const qconv_ffn_desc& d, bool aligned) {
-  return gemm_plan(d.m, d.f, d.k, 1, true, aligned);
+  return gemm_plan(d.m, d.f, d.k, 1, true, aligned, false);
 }
 GemmPlan plan_gx(const qconv_ffn_desc& d, bool aligned) {
-  return gemm_plan(d.m, d.k, 2 * (int64_t)d.f, 1, false, aligned);
+  return gemm_plan(d.m, d.k, 2 * (int64_t)d.f, 1, false, aligned, true);
 }
 GemmPlan plan_gw(const qconv_ffn_desc& d, bool aligned) {
-  return gemm_plan(d.f, d.k, d.m, 2, false, aligned);
+  return gemm_plan(d.f, d.k, d.m, 2, false, aligned, false);
 }
 
 template <class T>

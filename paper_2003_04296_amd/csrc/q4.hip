@@ -116,7 +116,7 @@ int run_gemm_q4_group(GemmArgs& a, int group, int tile, bool aligned, hipStream_
 constexpr int ROWS_MOST = 64;  // tokens that go through dense_rows.h
 
 GemmPlan plan_q4(const qconv_q4_desc& d, bool gated, bool aligned) {
-  return gemm_plan(d.m, d.n, d.k, 1, gated, aligned);
+  return gemm_plan(d.m, d.n, d.k, 1, gated, aligned, false);
 }
 size_t unit_bytes(const qconv_q4_desc& d) { return (size_t)round_up(d.n, 4) * 4; }  // of one weight
 

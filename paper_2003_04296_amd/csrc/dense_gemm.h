@@ -75,6 +75,15 @@ __device__ __forceinline__ int weight_row(int t) {
   return PAIR ? (t / 64) * 32 + t % 32 : t;
 }
 
+// A pointer that is the same in every lane, in scalar registers.  (Where other
+// code of the loop diverges, the compiler loses sight of that and loads lane
+// group by lane group.)
+__device__ __forceinline__ const uint16_t* uniform(const uint16_t* p) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (const uint16_t*)((uint64_t)hi << 32 | lo);
+}
+
 // The tile of one 16-bit operand: ROWS rows (or columns) of C by KS
 // products, staged by NT threads, CH chunks each.  SIDE 0: GemmArgs::r, 1: c.
 //
@@ -145,7 +154,7 @@ struct Stage16 {
     if constexpr (ALIGNED) {
       const int w = __builtin_amdgcn_readfirstlane(threadIdx.x & ~63) + j * NT;  // the wave's first chunk
       // a wave's 64 chunks are 8 or 16 rows, so all of them gate or all of them up
-      const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)(PAIR && ((w / CPR) & 32) ? from2 : from), (short)0,
+      const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)uniform(PAIR && ((w / CPR) & 32) ? from2 : from), (short)0,
                                                         0x7fffffff, 0x00020000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + w), 16, at[j] < left ? off[j] : OUTSIDE, 0, 0, 0);
     } else {
@@ -156,13 +165,9 @@ struct Stage16 {
       reg[j] = load8_first(in ? (const uint16_t*)((const char*)q + off[j]) : q, in ? n : 0);
     }
   }
-  // What load() left in registers.
-  __device__ __forceinline__ void store(lds_v4u* lds) {
-    if constexpr (!ALIGNED) {
-#pragma unroll
-      for (int j = 0; j < CH; ++j) lds[index(j)] = reg[j];
-    }
-  }
+  // What chunk() left in registers, piece by piece.
+  static constexpr int PIECES = ALIGNED ? 0 : CH;
+  __device__ __forceinline__ void store(lds_v4u* lds, int j) { lds[index(j)] = reg[j]; }
 };
 
 // The tile of 4-bit weights, in row form: a thread takes KS / 2 codes of one
@@ -183,7 +188,7 @@ struct StageQ4 {
   int kp;
   bool in;
   Codes code;
-  uint16_t sc;
+  uint32_t sc;
 
   __device__ __forceinline__ void init(const GemmArgs& a, int, int64_t r0) {
     const int t = threadIdx.x / 2, half = PAIR && (t & 32) ? 1 : 0;
@@ -206,18 +211,16 @@ struct StageQ4 {
   __device__ __forceinline__ void chunk(lds_v4u*, int) {
     const bool on = in && k < kp && left > 0;
     code = on ? *(const Codes*)(p + k / 2) : Codes{};
-    sc = on ? sp[k / GROUP] : (uint16_t)0;
+    sc = on ? sp[k / GROUP] : 0u;
   }
-  __device__ __forceinline__ void store(lds_v4u* lds) {
-    const float s = BF16::up(sc) * unit;
+  static constexpr int PIECES = W;
+  __device__ __forceinline__ void store(lds_v4u* lds, int q) {
+    const float s = BF16::up((uint16_t)sc) * unit;
     const int t = threadIdx.x / 2;
-#pragma unroll
-    for (int q = 0; q < W; ++q) {
-      const uint32_t c = code[q];
-      lds[t * CPR + (((threadIdx.x & 1) * W + q) ^ swz_row<KS>(t))] =
-          v4u{T::template scaled_e2m1<0>(c, s), T::template scaled_e2m1<1>(c, s), T::template scaled_e2m1<2>(c, s),
-              T::template scaled_e2m1<3>(c, s)};
-    }
+    const uint32_t c = code[q];
+    lds[t * CPR + (((threadIdx.x & 1) * W + q) ^ swz_row<KS>(t))] =
+        v4u{T::template scaled_e2m1<0>(c, s), T::template scaled_e2m1<1>(c, s), T::template scaled_e2m1<2>(c, s),
+            T::template scaled_e2m1<3>(c, s)};
   }
 };
 
@@ -318,10 +321,28 @@ __device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, 
 template <int KS>
 constexpr int STAGES = KS == 32 ? 5 : 2;
 
-template <int BR, class SR, class SC>
-__device__ __forceinline__ void load_chunk(SR& sr, SC& sc, lds_v4u* to, int i) {
-  if (i < SR::CH) sr.chunk(to, i);
-  else sc.chunk(to + BR * SR::CPR, i - SR::CH);
+template <class SR, class SC>
+__device__ __forceinline__ void load_chunk(SR& sr, SC& sc, lds_v4u* tr, lds_v4u* tc, int i) {
+  if (i < SR::CH) sr.chunk(tr, i);
+  else sc.chunk(tc, i - SR::CH);
+}
+
+template <class SR, class SC>
+__device__ __forceinline__ void store_piece(SR& sr, SC& sc, lds_v4u* tr, lds_v4u* tc, int i) {
+  if constexpr (SR::PIECES > 0) {
+    if (i < SR::PIECES) sr.store(tr, i);
+  }
+  if constexpr (SC::PIECES > 0) {
+    if (i >= SR::PIECES) sc.store(tc, i - SR::PIECES);
+  }
+}
+// The loads of an operand that goes straight into LDS, or of one that does not.
+template <bool DIRECT, class S>
+__device__ __forceinline__ void load_if(S& s, lds_v4u* to) {
+  if constexpr (S::DIRECT == DIRECT) {
+#pragma unroll
+    for (int j = 0; j < S::CH; ++j) s.chunk(to, j);
+  }
 }
 
 // The order of a stage's LDS reads, matrix instructions and loads: groups of 4
@@ -361,7 +382,7 @@ __device__ __forceinline__ void multiply32(v4f (&acc)[4][NR], v4u (&fc)[2][4], v
     });
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i][G] = T::mfma(fc[P][i], f[G], acc[i][G]);
-    Unroll<L0, L1>::run([&](auto l) { load_chunk<BR>(sr, sc, to, decltype(l)::value); });
+    Unroll<L0, L1>::run([&](auto l) { load_chunk(sr, sc, to, to + LR, decltype(l)::value); });
     auto instructions = [](int n) constexpr {  // LDS reads of the first n fragments
       const int c = n < MID ? 0 : n < MID + 4 ? n - MID : 4;
       return (n - c) * (SR::COL ? 2 : 1) + c * (SC::COL ? 2 : 1);
@@ -372,19 +393,18 @@ __device__ __forceinline__ void multiply32(v4f (&acc)[4][NR], v4u (&fc)[2][4], v
 
 // KS = 64: the products of stage `now`.  The first fragments are read ahead,
 // the others spread over the first two thirds of the groups; the loads into
-// `to` come within the first quarter (spread over half of the groups they end
+// tr and tc, the next stage's two parts, come within the first quarter (spread over half of the groups they end
 // late for the barrier: forward at 8192 tokens 2.30 ms, not 2.21).  An operand
-// that passes through registers is stored to `to` here and loaded for the
-// stage after it.
+// that passes through registers is loaded first and stored last.
 template <class T, int BR, int BC, class SR, class SC, int NR>
 __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, int wr, int wc,
-                                           const lds_v4u* __restrict__ now, lds_v4u* __restrict__ to) {
-  constexpr int LR = BR * SR::CPR, CHUNKS = SR::CH + SC::CH, GROUPS = 2 * NR, HALF = 4 + NR, READS = 2 * HALF;
-  constexpr int FIRST = 4 + 3;
-  constexpr bool REGS = !SR::DIRECT || !SC::DIRECT;
-  sr.store(to);
-  sc.store(to + LR);
+                                           const lds_v4u* __restrict__ now, lds_v4u* __restrict__ tr,
+                                           lds_v4u* __restrict__ tc) {
+  constexpr int LR = BR * SR::CPR, GROUPS = 2 * NR, HALF = 4 + NR, READS = 2 * HALF, FIRST = 4 + 3;
+  constexpr int LOADS = (SR::DIRECT ? SR::CH : 0) + (SC::DIRECT ? SC::CH : 0), PIECES = SR::PIECES + SC::PIECES;
   v4u f[2][NR], fc[2][4];
+  load_if<false>(sr, tr);
+  load_if<false>(sc, tc);
   Unroll<0, GROUPS>::run([&](auto g) {
     constexpr int G = decltype(g)::value;
     // fragments read before group n, in the order fc then fr, half after half
@@ -393,8 +413,8 @@ __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, in
       return n < 0 ? 0 : c < READS ? c : READS;
     };
     constexpr int R0 = before(G - 1), R1 = before(G);
-    constexpr int LA = 4 * CHUNKS * G / GROUPS, LB = 4 * CHUNKS * (G + 1) / GROUPS;
-    constexpr int L0 = LA < CHUNKS ? LA : CHUNKS, L1 = LB < CHUNKS ? LB : CHUNKS;
+    constexpr int LA = 4 * LOADS * G / GROUPS, LB = 4 * LOADS * (G + 1) / GROUPS;
+    constexpr int L0 = LA < LOADS ? LA : LOADS, L1 = LB < LOADS ? LB : LOADS;
     Unroll<R0, R1>::run([&](auto r) {
       constexpr int R = decltype(r)::value, H = R / HALF, I = R % HALF;
       if constexpr (I < 4) fc[H][I] = fragment<64, BC, SC::COL>(now + LR, wc + I * 16, H);
@@ -402,10 +422,13 @@ __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, in
     });
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i][G % NR] = T::mfma(fc[G / NR][i], f[G / NR][G % NR], acc[i][G % NR]);
-    Unroll<L0, L1>::run([&](auto l) { load_chunk<BR>(sr, sc, to, decltype(l)::value); });
-    if constexpr (!SR::COL && !SC::COL) group_order<R1 - R0, REGS ? 0 : L1 - L0>();
-    if constexpr (REGS) __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);  // vector instructions of the conversions
+    Unroll<L0, L1>::run([&](auto l) {
+      load_chunk(sr, sc, tr, tc, decltype(l)::value + (SR::DIRECT ? 0 : SR::CH));
+    });
+    group_order<R1 - R0, L1 - L0>();
   });
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) store_piece(sr, sc, tr, tc, i);
 }
 
 template <class T, class SR, class SC, int OUT, int BR, int BC>
@@ -458,31 +481,22 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
   };
   auto load = [&](lds_v4u* to) {
 #pragma unroll
-    for (int j = 0; j < CHUNKS; ++j) load_chunk<BR>(sr, sc, to, j);
+    for (int j = 0; j < CHUNKS; ++j) load_chunk(sr, sc, to, to + LR, j);
     next();
   };
   auto store = [&](lds_v4u* to) {
-    sr.store(to);
-    sc.store(to + LR);
+#pragma unroll
+    for (int i = 0; i < SR::PIECES + SC::PIECES; ++i) store_piece(sr, sc, to, to + LR, i);
   };
   if constexpr (KS == 64) {
     static_assert(!SR::COL && !SC::COL, "one segment");
-    // What passes through registers is loaded a step further ahead.
     load(lds);
     store(lds);
-    auto again = [&](auto& o, lds_v4u* at) {
-      if constexpr (!std::remove_reference_t<decltype(o)>::DIRECT) {
-#pragma unroll
-        for (int j = 0; j < std::remove_reference_t<decltype(o)>::CH; ++j) o.chunk(at, j);
-        o.next();
-      }
-    };
-    again(sr, lds);
-    again(sc, lds);
     for (int s = begin; s < end; ++s) {
       const int b = (s - begin) & 1;
       stage_barrier<0, REGS>();
-      multiply64<T, BR, BC>(acc, sr, sc, wr, wc, lds + b * STAGE, lds + (b ^ 1) * STAGE);
+      multiply64<T, BR, BC>(acc, sr, sc, wr, wc, lds + b * STAGE, lds + (b ^ 1) * STAGE,
+                            lds + (b ^ 1) * STAGE + LR);
       next();
     }
   } else {

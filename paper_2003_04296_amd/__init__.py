@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import os
+import struct
 from array import array
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -107,7 +108,7 @@ def lib() -> ctypes.CDLL:
     L.aqe_forward.argtypes = [vp, i64, i32, f32, vp, vp, i64, vp, vp]
     L.aqe_backward.argtypes = [vp, vp, i64, f32, vp, vp]
     L.aqe_sgd_clip.argtypes = [vp, vp, i64, f32, vp]
-    ffn, q4 = ctypes.POINTER(qconv_ffn_desc), ctypes.POINTER(qconv_q4_desc)
+    ffn = q4 = vp  # a descriptor by reference, or its bytes
     L.qconv_ffn_pre_floats.restype = sz
     L.qconv_ffn_pre_floats.argtypes = [i32, i32]
     L.qconv_ffn_forward_bytes.restype = sz
@@ -309,10 +310,10 @@ def _dtype_code(t) -> int:
 def _new(shape, dtype, like, stream):
     """A new tensor that belongs to the stream the kernels run on (freed memory
     is handed out again in that stream's order)."""
+    if stream is None:
+        return like.new_empty(shape) if dtype is like.dtype else like.new_empty(shape, dtype=dtype)
     import torch
 
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
@@ -322,48 +323,70 @@ def _on_gpu(t, what: str):
         raise ValueError(f"{what}: tensors are on the GPU, got one on {t.device}")
 
 
-def _rows(t, rows, cols, like, what: str) -> int:
-    """Row stride of a matrix [rows][cols] (rows None: any) with unit column
-    stride, of the type and on the device of `like`."""
-    s = t.shape
-    if len(s) != 2 or s[1] != cols or (rows is not None and s[0] != rows):
-        raise ValueError(f"{what}: shape {tuple(s)}, expected ({'m' if rows is None else rows}, {cols})")
-    if t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+# A call for one token takes 3 us on the GPU, so the checks below ask each
+# property of a tensor once and by its cheapest name.
+
+def _ld(t, s, what: str) -> int:
+    """Row stride of a matrix of shape s with unit column stride."""
+    rows, cols = s
     ld, unit = t.stride()
     if unit != 1 and cols > 1:
         raise ValueError(f"{what}: columns must be contiguous (strides {t.stride()})")
-    if s[0] <= 1:
+    if rows <= 1:
         return cols  # no second row
     if ld < cols:
         raise ValueError(f"{what}: row stride {ld} is below the {cols} columns")
     return ld
 
 
+def _rows(t, rows, cols, like, what: str) -> int:
+    """Row stride of a matrix [rows][cols] of the type and on the device of `like`."""
+    s = t.shape
+    if len(s) != 2 or s[0] != rows or s[1] != cols:
+        raise ValueError(f"{what}: shape {tuple(s)}, expected ({rows}, {cols})")
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    return _ld(t, s, what)
+
+
 def _workspace(ws, nbytes: int, like, what: str, stream):
     """The caller's workspace (checked on the C side for its size) or a new one."""
-    if ws is None and nbytes:
+    if ws is None:
+        if not nbytes:
+            return None, 0
         import torch
 
-        ws = _new(nbytes, torch.uint8, like, stream)
-    if ws is None:
-        return None, 0
+        return _new((nbytes,), torch.uint8, like, stream), nbytes
     if ws.device != like.device or not ws.is_contiguous():
         raise ValueError(f"{what}: the workspace is a contiguous tensor on {like.device}")
     return ws, ws.numel() * ws.element_size()
 
 
-def _ffn_desc(x, w_gate, w_up, act, h, what):
-    if x.dim() != 2 or w_gate.dim() != 2:
+# Descriptors as bytes: filling a ctypes structure takes 1 us.
+_FFN_DESC = struct.Struct("5i4x3q")
+_Q4_DESC = struct.Struct("5i4x2q")
+
+
+def _ffn_sizes(x, w_gate, what):
+    """(m, k, f) of a feed-forward call."""
+    s, w = x.shape, w_gate.shape
+    if len(s) != 2 or len(w) != 2:
         raise ValueError(f"{what}: x and the weights are matrices")
     _on_gpu(x, what)
-    m, k = x.shape
-    f = w_gate.shape[0]
-    ld_w = _rows(w_gate, f, k, x, f"{what} w_gate")
-    if _rows(w_up, f, k, x, f"{what} w_up") != ld_w:
+    return s[0], s[1], w[0]
+
+
+def _ffn_desc(x, w_gate, w_up, act, ld_h, m, k, f, what):
+    ld_w = _rows(w_gate, f, k, x, what)
+    if _rows(w_up, f, k, x, what) != ld_w:
         raise ValueError(f"{what}: w_gate and w_up have different row strides")
-    return qconv_ffn_desc(m, k, f, _dtype_code(x), act, _rows(x, m, k, x, f"{what} x"), ld_w,
-                          _rows(h, m, f, x, f"{what} h"))
+    return _FFN_DESC.pack(_int(m), _int(k), _int(f), _dtypes[x.dtype], act, _ld(x, (m, k), what), ld_w, ld_h)
+
+
+def _int(v: int) -> int:
+    if v > 0x7fffffff:
+        raise QconvError(QCONV_EUNSUPPORTED, "a size past 2^31")
+    return v
 
 
 def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pre=None, out=None,
@@ -371,19 +394,20 @@ def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pr
     """h = act(x w_gate^T) * (x w_up^T) for 16-bit x [m][k] and weights [f][k]
     -> (h [m][f], pre).  keep_pre (or a buffer `pre` of a former call) keeps
     what ffn_backward needs, else pre is None."""
-    import torch
-
-    _on_gpu(x, "ffn_forward")
-    m, f = x.shape[0], w_gate.shape[0]
+    m, k, f = _ffn_sizes(x, w_gate, "ffn_forward")
+    d = _ffn_desc(x, w_gate, w_up, act, f if out is None else _rows(out, m, f, x, "ffn_forward out"), m, k, f,
+                  "ffn_forward")
+    L = lib()
     h = _new((m, f), x.dtype, x, stream) if out is None else out
-    d = _ffn_desc(x, w_gate, w_up, act, h, "ffn_forward")
-    if keep_pre and pre is None:
-        pre = _new(lib().qconv_ffn_pre_floats(m, f), torch.float32, x, stream)
-    elif pre is not None:
+    if pre is not None:
         _check_pre(pre, m, f, x, "ffn_forward")
-    ws, nbytes = _workspace(workspace, lib().qconv_ffn_forward_bytes(ctypes.byref(d)), x, "ffn_forward", stream)
-    _check(lib().qconv_ffn_forward(ctypes.byref(d), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(h), _ptr(pre), _ptr(ws),
-                                   nbytes, _stream(stream)), "qconv_ffn_forward")
+    elif keep_pre:
+        import torch
+
+        pre = _new((L.qconv_ffn_pre_floats(m, f),), torch.float32, x, stream)
+    ws, nbytes = _workspace(workspace, L.qconv_ffn_forward_bytes(d), x, "ffn_forward", stream)
+    _check(L.qconv_ffn_forward(d, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(pre), _ptr(ws),
+                               nbytes, _stream(stream)), "qconv_ffn_forward")
     return h, pre
 
 
@@ -400,8 +424,8 @@ def ffn_backward(x, w_gate, w_up, pre, gh, act: int = ACT_SILU, need_x: bool = T
     """From gh [m][f] and the forward's pre -> (gx [m][k], gw_gate [f][k],
     gw_up [f][k]) in x's type; None for what need_x / need_w leave out.  out:
     contiguous tensors to write instead of new ones."""
-    d = _ffn_desc(x, w_gate, w_up, act, gh, "ffn_backward")
-    m, k, f = d.m, d.k, d.f
+    m, k, f = _ffn_sizes(x, w_gate, "ffn_backward")
+    d = _ffn_desc(x, w_gate, w_up, act, _rows(gh, m, f, x, "ffn_backward gh"), m, k, f, "ffn_backward")
     _check_pre(pre, m, f, x, "ffn_backward")
     gx, gg, gu = out if out is not None else (None, None, None)
     shapes = [(m, k), (f, k), (f, k)]
@@ -410,8 +434,8 @@ def ffn_backward(x, w_gate, w_up, pre, gh, act: int = ACT_SILU, need_x: bool = T
             raise ValueError("ffn_backward: out tensors are contiguous")
     new = lambda t, need, s: (_new(s, x.dtype, x, stream) if t is None else t) if need else None
     gx, gg, gu = new(gx, need_x, shapes[0]), new(gg, need_w, shapes[1]), new(gu, need_w, shapes[2])
-    ws, nbytes = _workspace(workspace, lib().qconv_ffn_backward_bytes(ctypes.byref(d)), x, "ffn_backward", stream)
-    _check(lib().qconv_ffn_backward(ctypes.byref(d), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(pre), _ptr(gh), _ptr(gx),
+    ws, nbytes = _workspace(workspace, lib().qconv_ffn_backward_bytes(d), x, "ffn_backward", stream)
+    _check(lib().qconv_ffn_backward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(pre), _ptr(gh), _ptr(gx),
                                     _ptr(gg), _ptr(gu), _ptr(ws), nbytes, _stream(stream)), "qconv_ffn_backward")
     return gx, gg, gu
 
@@ -433,68 +457,81 @@ def q4_pack(w, group: int = 64, top: int = 6, out=None, stream=None):
         out = (_new((n, cb // n if n else 0), torch.uint8, w, stream),
                _new((n, sb // (2 * n) if n else 0), torch.bfloat16, w, stream))
     else:
-        _q4_group(*out, n, k, w.device, "q4_pack", group)
+        _q4_group(*out, n, k, w, "q4_pack", group)
     codes, scales = out
     _check(lib().qconv_q4_pack(_ptr(w), _dtype_code(w), n, k, ld, group, top, _ptr(codes), _ptr(scales),
                                _stream(stream)), "qconv_q4_pack")
     return codes, scales
 
 
-def _q4_group(codes, scales, n, k, device, what, group=None) -> int:
+def _q4_group(codes, scales, n, k, like, what, group=None) -> int:
     """The group size of packed weights [n][k], their buffers checked against it."""
     import torch
 
-    if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16 or codes.device != device or \
-            scales.device != device or not codes.is_contiguous() or not scales.is_contiguous():
-        raise ValueError(f"{what}: codes are uint8 and scales bf16, contiguous, on {device}")
+    dev = like.get_device()
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.bfloat16 or codes.get_device() != dev or \
+            scales.get_device() != dev or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError(f"{what}: codes are uint8 and scales bf16, contiguous, on {like.device}")
     cs, ss = codes.shape, scales.shape
     if group is None:
         group = 2 * cs[1] // ss[1] if len(cs) == 2 and len(ss) == 2 and ss[1] else 0
     if group not in (32, 64, 128):
         raise ValueError(f"{what}: groups of {group} values (32, 64 and 128 are supported)")
     groups = (k + group - 1) // group
-    if tuple(cs) != (n, groups * group // 2) or tuple(ss) != (n, groups):
+    if cs != (n, groups * group // 2) or ss != (n, groups):
         raise ValueError(f"{what}: codes {tuple(cs)} and scales {tuple(ss)} are not those of a ({n}, {k}) weight")
     return group
 
 
-def _q4_desc(x, codes, scales, out, what, stream):
-
-    if x.dim() != 2 or codes.dim() != 2:
+def _q4_sizes(x, codes, scales, what):
+    """(m, n, k, group) of a product with packed weights."""
+    s, c = x.shape, codes.shape
+    if len(s) != 2 or len(c) != 2:
         raise ValueError(f"{what}: x and codes are matrices")
     _on_gpu(x, what)
-    m, k = x.shape
-    n = codes.shape[0]
-    y = _new((m, n), x.dtype, x, stream) if out is None else out
-    group = _q4_group(codes, scales, n, k, x.device, what)
-    return qconv_q4_desc(m, n, k, group, _dtype_code(x), _rows(x, m, k, x, f"{what} x"),
-                         _rows(y, m, n, x, f"{what} out")), y
+    m, k = s
+    n = c[0]
+    return m, n, k, _q4_group(codes, scales, n, k, x, what)
+
+
+def _q4_desc(x, m, n, k, group, out, what):
+    return _Q4_DESC.pack(_int(m), _int(n), _int(k), group, _dtypes[x.dtype], _ld(x, (m, k), what),
+                         n if out is None else _rows(out, m, n, x, what))
 
 
 def q4_linear(x, codes, scales, bias=None, out=None, workspace=None, stream=None):
     """y [m][n] = x [m][k] w^T + bias with 4-bit weights (q4_pack); x and y
     fp16 or bf16, bias fp32 [n]."""
-    import torch
+    m, n, k, group = _q4_sizes(x, codes, scales, "q4_linear")
+    d = _q4_desc(x, m, n, k, group, out, "q4_linear")
+    if bias is not None:
+        import torch
 
-    d, y = _q4_desc(x, codes, scales, out, "q4_linear", stream)
-    if bias is not None and (bias.dtype != torch.float32 or bias.device != x.device or tuple(bias.shape) != (d.n,)
-                             or not bias.is_contiguous()):
-        raise ValueError(f"q4_linear: bias is a contiguous fp32 vector of {d.n} on {x.device}")
-    ws, nbytes = _workspace(workspace, lib().qconv_q4_workspace_bytes(ctypes.byref(d), 0), x, "q4_linear", stream)
-    _check(lib().qconv_q4_linear(ctypes.byref(d), _ptr(x), _ptr(codes), _ptr(scales), _ptr(bias), _ptr(y), _ptr(ws),
-                                 nbytes, _stream(stream)), "qconv_q4_linear")
+        if bias.dtype is not torch.float32 or bias.get_device() != x.get_device() or bias.shape != (n,) or \
+                not bias.is_contiguous():
+            raise ValueError(f"q4_linear: bias is a contiguous fp32 vector of {n} on {x.device}")
+        bias = bias.data_ptr()
+    L = lib()
+    y = _new((m, n), x.dtype, x, stream) if out is None else out
+    ws, nbytes = _workspace(workspace, L.qconv_q4_workspace_bytes(d, 0), x, "q4_linear", stream)
+    _check(L.qconv_q4_linear(d, x.data_ptr(), codes.data_ptr(), scales.data_ptr(), bias, y.data_ptr(), _ptr(ws), nbytes,
+                             _stream(stream)), "qconv_q4_linear")
     return y
 
 
 def q4_gated(x, gate_codes, gate_scales, up_codes, up_scales, act: int = ACT_SILU, out=None, workspace=None,
              stream=None):
     """h [m][n] = act(x w_gate^T) * (x w_up^T) with 4-bit weights."""
-    d, y = _q4_desc(x, gate_codes, gate_scales, out, "q4_gated", stream)
-    if _q4_group(up_codes, up_scales, d.n, d.k, x.device, "q4_gated up") != d.group:
+    m, n, k, group = _q4_sizes(x, gate_codes, gate_scales, "q4_gated")
+    if _q4_group(up_codes, up_scales, n, k, x, "q4_gated up") != group:
         raise ValueError("q4_gated: gate and up weights have different groups")
-    ws, nbytes = _workspace(workspace, lib().qconv_q4_workspace_bytes(ctypes.byref(d), 1), x, "q4_gated", stream)
-    _check(lib().qconv_q4_gated(ctypes.byref(d), _ptr(x), _ptr(gate_codes), _ptr(gate_scales), _ptr(up_codes),
-                                _ptr(up_scales), act, _ptr(y), _ptr(ws), nbytes, _stream(stream)), "qconv_q4_gated")
+    d = _q4_desc(x, m, n, k, group, out, "q4_gated")
+    L = lib()
+    y = _new((m, n), x.dtype, x, stream) if out is None else out
+    ws, nbytes = _workspace(workspace, L.qconv_q4_workspace_bytes(d, 1), x, "q4_gated", stream)
+    _check(L.qconv_q4_gated(d, x.data_ptr(), gate_codes.data_ptr(), gate_scales.data_ptr(), up_codes.data_ptr(),
+                            up_scales.data_ptr(), act, y.data_ptr(), _ptr(ws), nbytes, _stream(stream)),
+           "qconv_q4_gated")
     return y
 
 

@@ -580,7 +580,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
 template <class T, class SR, class SC, int OUT, int BR, int BC>
 __global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
   static_assert(SR::KS == SC::KS, "one ring");
-  __shared__ v4u lds[STAGES<SR::KS> * (BR + BC) * SR::CPR];
+  [[maybe_unused]] __shared__ v4u lds[STAGES<SR::KS> * (BR + BC) * SR::CPR];
 #ifdef __HIP_DEVICE_COMPILE__  // the host has no LDS pointers
   gemm_tile<T, SR, SC, OUT, BR, BC>(a, (lds_v4u*)lds);
 #endif

@@ -2,17 +2,20 @@
 //   y[m][n] = sum_k x[m][k] w[n][k]  (plain with bias, or gated from two w),
 // for 16-bit weights and for 4-bit ones with group scales.
 //
-// Bound by reading the weights once.  A block owns 16 outputs (16 rows of w)
-// and 16 MT tokens; its waves take every NW-th block of 128 inputs, so all of
-// w is in flight at once from many waves, and they are joined through LDS at
-// the end.  Each load of a row is 16 bytes per lane.  The matrix instruction
-// does the sums even for one token: its work is far below its rate, and it
-// spares the reduction over lanes.  In its result a lane holds output
-// lane % 16 and tokens (lane / 16) * 4 + 0..3, so one scale per lane and
-// group serves 4-bit weights.
+// Bound by reading the weights once, and past 16 tokens by x, which every
+// block reads whole.  A block owns 16 outputs (16 rows of w) and its tokens;
+// its waves take every NW-th block of 128 inputs, so all of w is in flight at
+// once from many waves, and they are joined through LDS at the end.  Each load
+// of a row is 16 bytes per lane.  The matrix instruction does the sums even for
+// one token: its work is far below its rate, and it spares the reduction over
+// lanes.  In its result a lane holds output lane % 16 and tokens
+// (lane / 16) * 4 + 0..3, so one scale per lane and group serves 4-bit weights.
+// Measured at 4096 x 4096 in 4 bits (9.4 MB): 4.1 us for one token (2.3 TB/s;
+// a kernel that reads the codes alone takes 3.3), 6.8 for 16, 9.6 for 32.
 #pragma once
 
 #include "dense.h"
+#include "qconv_internal.h"
 
 namespace qc {
 
@@ -76,19 +79,17 @@ struct Q4 {
   }
 };
 
-// What a wave reads of one block of 128 inputs.
-template <class W, int H, int MT>
+// A wave's weights in one block of 128 inputs.
+template <class W, int H>
 struct RowsBlock {
   static constexpr int SCALES = W::GROUP ? 128 / W::GROUP : 1;
-  v4u x[MT][4];
   v4u w[H][W::GROUP ? 1 : 4];
   uint16_t s[H][SCALES];
 
   // FULL: all 128 inputs exist.  Otherwise what lies past k, or past the
   // codes and scales of the row, is zero and not read.
   template <bool FULL>
-  __device__ __forceinline__ void load(const RowsArgs& a, const uint16_t* const xr[MT], const bool in[MT], int64_t row,
-                                       int k0, int o) {
+  __device__ __forceinline__ void load(const RowsArgs& a, int64_t row, int k0, int o) {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       if constexpr (W::GROUP != 0) {
@@ -115,53 +116,62 @@ struct RowsBlock {
         }
       }
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = k0 + W::k_of(i, o);
-        x[t][i] = v4u{0, 0, 0, 0};
-        if (in[t]) x[t][i] = FULL ? load8(xr[t] + k) : load8_first(xr[t] + k, a.k - k);
-      }
   }
 
-  template <class T>
-  __device__ __forceinline__ void multiply(v4f acc[H][MT]) {
+  // x: the lane's token in LDS, at the block's first input; tiles of 16 tokens
+  // `tile` values apart.
+  template <class T, int MT>
+  __device__ __forceinline__ void multiply(v4f (&acc)[H][MT], const uint16_t* x, int tile, int o) const {
+    v4u wf[H][4];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       if constexpr (W::GROUP != 0) {
         uint32_t d[4] = {w[h][0][0], w[h][0][1], w[h][0][2], w[h][0][3]};
         W::arrange(d);
-        v4u wf[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          wf[i] = v4u{T::template from_e2m1<0>(d[i]), T::template from_e2m1<1>(d[i]), T::template from_e2m1<2>(d[i]),
-                      T::template from_e2m1<3>(d[i])};
+          wf[h][i] = v4u{T::template from_e2m1<0>(d[i]), T::template from_e2m1<1>(d[i]), T::template from_e2m1<2>(d[i]),
+                         T::template from_e2m1<3>(d[i])};
+      } else {
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int i = 0; i < 4; ++i) wf[h][i] = w[h][i];
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      v4u xf[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xf[i] = *(const v4u*)(x + t * tile + W::k_of(i, o));
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        if constexpr (W::GROUP != 0) {
 #pragma unroll
           for (int g = 0; g < SCALES; ++g) {
             v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int i = g * (4 / SCALES); i < (g + 1) * (4 / SCALES); ++i) sum = T::mfma(x[t][i], wf[i], sum);
+            for (int i = g * (4 / SCALES); i < (g + 1) * (4 / SCALES); ++i) sum = T::mfma(xf[i], wf[h][i], sum);
             const float f = BF16::up(s[h][g]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[h][t][e] = fmaf(f, sum[e], acc[h][t][e]);
           }
-      } else {
+        } else {
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[h][t] = T::mfma(x[t][i], w[h][i], acc[h][t]);
+          for (int i = 0; i < 4; ++i) acc[h][t] = T::mfma(xf[i], wf[h][i], acc[h][t]);
+        }
       }
     }
   }
 };
 
 // H = 1: y = sum + bias.  H = 2: y = act(sum 0) * sum 1.
-template <class T, class W, int H, int MT, int NW, int U>
+// A pass is NW blocks of 128 inputs, one per wave.  Its x lies in LDS, put
+// there by all waves in whole rows; the next pass's x and weights are on their
+// way into registers while it is multiplied.
+template <class T, class W, int H, int MT, int NW>
 __global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
-  __shared__ float part[NW][H][MT * 256];
+  constexpr int PASS = NW * 128, LD = PASS + 8, WPT = PASS / 512, STEP = NW / WPT, PER = 16 * MT / STEP;
+  __shared__ v4u xs[16 * MT * LD / 8];  // at the end: the waves' sums
+  static_assert(sizeof(xs) >= sizeof(float) * NW * H * MT * 256, "sums fit");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, o = lane >> 4;
   // workgroups go to the 8 dies in turn: the token tiles of one set of outputs
@@ -169,42 +179,48 @@ __global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
   const int nt = blockIdx.x / (8 * a.tiles_m) * 8 + blockIdx.x % 8, mt = blockIdx.x / 8 % a.tiles_m;
   if (nt >= a.tiles_n) return;
   const int n0 = nt * 16, m0 = mt * 16 * MT;
-  const uint16_t* xr[MT];
-  bool in[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    in[t] = m0 + t * 16 + r < a.m;
-    xr[t] = a.x + (in[t] ? (int64_t)(m0 + t * 16 + r) * a.ld_x : 0);
-  }
   const int64_t row = n0 + r < a.n ? n0 + r : 0;
   v4f acc[H][MT];
 #pragma unroll
   for (int h = 0; h < H; ++h)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[h][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  const int full = a.k / 128, blocks = (a.k + 127) / 128;
-  RowsBlock<W, H, MT> b[U];
-  int kb = wave;
-  for (; kb + (U - 1) * NW < full; kb += U * NW) {
+  RowsBlock<W, H> b;
+  v4u xr[PER];
+  // A wave copies 512 inputs of every STEP-th token.  In place of those past
+  // the last it takes that one; their results go nowhere.
+  const int first = wave / WPT, col = (wave % WPT) * 512 + lane * 8;
+  auto load = [&](int base) {
+    const int k0 = base + wave * 128;
+    if (k0 + 128 <= a.k) b.template load<true>(a, row, k0, o);
+    else if (k0 < a.k) b.template load<false>(a, row, k0, o);
+    const bool whole = a.k - base >= PASS;
 #pragma unroll
-    for (int u = 0; u < U; ++u) b[u].template load<true>(a, xr, in, row, (kb + u * NW) * 128, o);
+    for (int j = 0; j < PER; ++j) {
+      const int m = m0 + first + j * STEP, k = base + col;
+      const uint16_t* p = a.x + (int64_t)(m < a.m ? m : a.m - 1) * a.ld_x + k;
+      xr[j] = whole ? load8(p) : load8_first(p, a.k - k);
+    }
+  };
+  load(0);
+  for (uint32_t base = 0; base < (uint32_t)a.k; base += PASS) {
+    if (base > 0) __syncthreads();
 #pragma unroll
-    for (int u = 0; u < U; ++u) b[u].template multiply<T>(acc);
+    for (int j = 0; j < PER; ++j) xs[(first + j * STEP) * (LD / 8) + col / 8] = xr[j];
+    __syncthreads();
+    const RowsBlock<W, H> now = b;
+    if ((uint32_t)a.k - base > PASS) load(base + PASS);
+    if ((int)base + wave * 128 < a.k)
+      now.template multiply<T, MT>(acc, (const uint16_t*)xs + r * LD + wave * 128, 16 * LD, o);
   }
-  for (; kb < full; kb += NW) {
-    b[0].template load<true>(a, xr, in, row, kb * 128, o);
-    b[0].template multiply<T>(acc);
-  }
-  if (kb < blocks) {
-    b[0].template load<false>(a, xr, in, row, kb * 128, o);
-    b[0].template multiply<T>(acc);
-  }
+  __syncthreads();
+  float* part = (float*)xs;  // [NW][H][MT * 256]
 #pragma unroll
   for (int h = 0; h < H; ++h)
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) part[wave][h][t * 256 + (o * 4 + e) * 16 + r] = acc[h][t][e];
+      for (int e = 0; e < 4; ++e) part[(wave * H + h) * (MT * 256) + t * 256 + (o * 4 + e) * 16 + r] = acc[h][t][e];
   __syncthreads();
   for (int i = threadIdx.x; i < MT * 256; i += NW * 64) {
     const int m = m0 + i / 16, n = n0 + i % 16;
@@ -212,9 +228,9 @@ __global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
     float v[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      v[h] = part[0][h][i];
+      v[h] = part[h * (MT * 256) + i];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) v[h] += part[w][h][i];
+      for (int w = 1; w < NW; ++w) v[h] += part[(w * H + h) * (MT * 256) + i];
     }
     float y;
     if constexpr (H == 2) {
@@ -230,9 +246,211 @@ __global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
   }
 }
 
+// The end of the kernels for at most 4 tokens: thread i < M * 16 joins the
+// waves' sums of token i / 16 and output n0 + i % 16.
+template <class T, int H, int M, int NW>
+__device__ __forceinline__ void finish_few(const RowsArgs& a, const float (&part)[NW][H][M * 16], int n0) {
+  __syncthreads();
+  const int i = threadIdx.x, m = i / 16, n = n0 + i % 16;
+  if (i >= M * 16 || m >= a.m || n >= a.n) return;
+  float v[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    v[h] = part[0][h][i];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) v[h] += part[w][h][i];
+  }
+  float y;
+  if constexpr (H == 2) {
+    y = act_value(a.act, v[0]) * v[1];
+    if (a.pre) {
+      a.pre[(int64_t)m * 2 * a.ld_pre + n] = v[0];
+      a.pre[((int64_t)m * 2 + 1) * a.ld_pre + n] = v[1];
+    }
+  } else {
+    y = a.bias ? v[0] + a.bias[n] : v[0];
+  }
+  a.y[(int64_t)m * a.ld_y + n] = T::down(y);
+}
+
+constexpr int FEW_MOST = 4;  // tokens they take
+
+// At most 4 tokens on 4-bit weights.  Lane row o holds 32 codes of one group,
+// and the row of x's operand that stands for token t and lane row o is zero in
+// the other lane rows: the matrix instruction's 16 rows, of which tokens would
+// fill 4 at most, keep the lane rows' sums apart.  So the codes need no
+// exchange between lanes, whatever the group, a lane needs one scale per 32
+// codes instead of up to four, and the scales take one fma per token.
+// x lies in LDS, PASS inputs at a time, and lanes that stand for no token read
+// zeros there: no load is conditional (a branch around them made the compiler
+// copy all operands).  Gated 4096 -> 16384 in groups of 32, in us: 17.6 for one
+// token and 21.5 for four, against 20.6 and 23 of a form like
+// dense_rows_kernel's; reading the codes alone takes 10.7.
+template <class T, int GROUP, int H, int M, int NW>
+__global__ __launch_bounds__(NW * 64) void dense_few_kernel(RowsArgs a) {
+  constexpr int PASS = 4096, LD = PASS + 8;  // + 8: the tokens' values in different banks
+  static_assert(PASS % (NW * 128) == 0, "a pass is whole rounds");
+  __shared__ float part[NW][H][M * 16];
+  __shared__ v4u xs[(M * LD + 128) / 8];  // the tokens, then zeros
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, o = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  const bool in = r >> 2 == o && (r & 3) < M;
+  const int64_t row = n0 + r < a.n ? n0 + r : 0;
+  const char* wr[H];
+  const uint16_t* sr[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    wr[h] = (const char*)a.w[h] + row * (a.kp / 2);
+    sr[h] = a.sc[h] + row * (a.kp / GROUP);
+  }
+  float acc[H][M];
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int t = 0; t < M; ++t) acc[h][t] = 0.0f;
+  v4u w[H];
+  float sc[H];
+  // 32 codes of input k0 + o * 32; past the row its last ones, with a scale of
+  // zero (x is zero there, too, but a scale may be an infinity)
+  auto load = [&](int k0) {
+    const int k = k0 + o * 32, c = k < a.kp ? k : a.kp - 32;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      w[h] = *(const v4u*)(wr[h] + (uint32_t)c / 2);
+      sc[h] = k < a.kp ? BF16::up(sr[h][(uint32_t)c / GROUP]) : 0.0f;
+    }
+  };
+  if (threadIdx.x < 16) xs[M * LD / 8 + threadIdx.x] = v4u{0, 0, 0, 0};
+  for (uint32_t base = 0; base < (uint32_t)a.k; base += PASS) {
+    const int here = a.k - base < PASS ? a.k - base : PASS, blocks = (here + 127) / 128;
+    if (wave < blocks) load(base + wave * 128);
+    if (base > 0) __syncthreads();
+#pragma unroll
+    for (int t = 0; t < M; ++t)
+      for (int i = threadIdx.x; i < blocks * 16; i += NW * 64)
+        xs[t * (LD / 8) + i] = t < a.m ? load8_first(a.x + t * a.ld_x + base + i * 8, here - i * 8) : v4u{0, 0, 0, 0};
+    __syncthreads();
+    const char* xp = (const char*)xs + (in ? ((r & 3) * LD + wave * 128 + o * 32) * 2 : M * LD * 2);
+    const int by = in ? NW * 256 : 0;
+    for (int kb = wave; kb < blocks; kb += NW) {
+      v4u x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = *(const v4u*)(xp + i * 16);
+      xp += by;
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        const v4u c = w[h];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sum = T::mfma(x[i], v4u{T::template from_e2m1<0>(c[i]), T::template from_e2m1<1>(c[i]),
+                                  T::template from_e2m1<2>(c[i]), T::template from_e2m1<3>(c[i])}, sum);
+#pragma unroll
+        for (int t = 0; t < M; ++t) acc[h][t] = fmaf(sc[h], sum[t], acc[h][t]);
+      }
+      if (kb + NW < blocks) load(base + (kb + NW) * 128);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int t = 0; t < M; ++t) {
+      float v = acc[h][t];
+      v += __shfl_xor(v, 16);
+      v += __shfl_xor(v, 32);
+      if (o == 0) part[wave][h][t * 16 + r] = v;
+    }
+  finish_few<T, H, M, NW>(a, part, n0);
+}
+
+// At most 4 tokens on 16-bit weights: two blocks of 128 inputs are under way
+// per wave.  Lanes past the tokens keep zeros.  No LDS for x: what is waited for
+// is the weights, and a barrier before the first product costs more (2048 ->
+// 8192, one token, two weights: 12.3 us against 11.7).
+template <class T, int H, int NW>
+__global__ __launch_bounds__(NW * 64) void dense_few16_kernel(RowsArgs a) {
+  constexpr int M = FEW_MOST, U = 2;
+  __shared__ float part[NW][H][M * 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, o = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  const bool in = r < a.m;
+  const uint16_t* xr = a.x + (in ? (int64_t)r * a.ld_x : 0) + o * 8;
+  const uint16_t* wr[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) wr[h] = (const uint16_t*)a.w[h] + (int64_t)(n0 + r < a.n ? n0 + r : 0) * a.ld_w + o * 8;
+  v4f acc[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) acc[h] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  v4u x[U][4] = {}, w[U][H][4];
+  auto load = [&](int u, int k0) {
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[u][h][i] = load8(wr[h] + k0 + i * 32);
+    if (in) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[u][i] = load8(xr + k0 + i * 32);
+    }
+  };
+  auto multiply = [&](int u) {
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[h] = T::mfma(x[u][i], w[u][h][i], acc[h]);
+  };
+  const int full = a.k / 128;
+  int kb = wave;
+  for (; kb + (U - 1) * NW < full; kb += U * NW) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(u, (kb + u * NW) * 128);
+#pragma unroll
+    for (int u = 0; u < U; ++u) multiply(u);
+  }
+  for (; kb < full; kb += NW) {
+    load(0, kb * 128);
+    multiply(0);
+  }
+  if (kb * 128 < a.k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = kb * 128 + i * 32, left = a.k - k - o * 8;
+      x[0][i] = load8_first(xr + k, in ? left : 0);
+#pragma unroll
+      for (int h = 0; h < H; ++h) w[0][h][i] = load8_first(wr[h] + k, left);
+    }
+    multiply(0);
+  }
+  if (o == 0) {
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int t = 0; t < M; ++t) part[wave][h][t * 16 + r] = acc[h][t];
+  }
+  finish_few<T, H, M, NW>(a, part, n0);
+}
+
+// GROUP 0: 16-bit weights.
+template <class T, int GROUP, int H>
+int run_dense_few(RowsArgs& a, hipStream_t s) {
+  constexpr int NW = 8;
+  const int blocks = ceil_div(a.n, 16);
+  if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;  // 2^31 threads
+  if constexpr (GROUP == 0)
+    dense_few16_kernel<T, H, NW><<<blocks, NW * 64, 0, s>>>(a);
+  else if (a.m == 1)
+    dense_few_kernel<T, GROUP, H, 1, NW><<<blocks, NW * 64, 0, s>>>(a);
+  else
+    dense_few_kernel<T, GROUP, H, FEW_MOST, NW><<<blocks, NW * 64, 0, s>>>(a);
+  return hip_status();
+}
+
 // Tokens per block: 16 while the blocks do not fill the 256 compute units
 // (weights read again come from L2), up to 64 otherwise, so that x is not read
-// again for every 16 outputs.
+// again for every 16 outputs.  From 32 on four waves per block, whose x leaves
+// LDS for two or more blocks per unit: 4-bit 4096 -> 16384 for 64 tokens 39 us
+// against 56 with eight, gated for 32 tokens 36 against 43.
 template <class T, class W, int H>
 int run_dense_rows(RowsArgs& a, hipStream_t s) {
   constexpr int NW = 8;
@@ -245,12 +463,12 @@ int run_dense_rows(RowsArgs& a, hipStream_t s) {
   const int64_t blocks = (int64_t)(a.tiles_n + 7) / 8 * 8 * a.tiles_m;
   if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;  // 2^31 threads
   if (mt == 4)
-    dense_rows_kernel<T, W, H, 4, NW, 1><<<(unsigned)blocks, NW * 64, 0, s>>>(a);
+    dense_rows_kernel<T, W, H, 4, 4><<<(unsigned)blocks, 4 * 64, 0, s>>>(a);
   else if (mt == 2)
-    dense_rows_kernel<T, W, H, 2, NW, 1><<<(unsigned)blocks, NW * 64, 0, s>>>(a);
+    dense_rows_kernel<T, W, H, 2, 4><<<(unsigned)blocks, 4 * 64, 0, s>>>(a);
   else
-    dense_rows_kernel<T, W, H, 1, NW, 2><<<(unsigned)blocks, NW * 64, 0, s>>>(a);
-  return hipGetLastError() == hipSuccess ? QCONV_OK : QCONV_EHIP;
+    dense_rows_kernel<T, W, H, 1, NW><<<(unsigned)blocks, NW * 64, 0, s>>>(a);
+  return hip_status();
 }
 
 }  // namespace qc

@@ -113,6 +113,7 @@ int launch_ffn_forward(const qconv_ffn_desc& d, const void* x, const void* wg, c
     r.n = d.f;
     r.k = d.k;
     r.act = d.act;
+    if (d.m <= FEW_MOST) return d.dtype == QCONV_F16 ? run_dense_few<F16, 0, 2>(r, s) : run_dense_few<BF16, 0, 2>(r, s);
     return d.dtype == QCONV_F16 ? run_dense_rows<F16, Dense16, 2>(r, s) : run_dense_rows<BF16, Dense16, 2>(r, s);
   }
   GemmArgs a = {};

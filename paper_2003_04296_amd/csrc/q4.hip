@@ -158,6 +158,11 @@ int launch_gemm(const qconv_q4_desc& d, const void* x, const uint8_t* const w[2]
 
 template <class T, int H>
 int run_rows(RowsArgs& a, int group, hipStream_t s) {
+  if (a.m <= FEW_MOST) {
+    if (group == 32) return run_dense_few<T, 32, H>(a, s);
+    if (group == 64) return run_dense_few<T, 64, H>(a, s);
+    return run_dense_few<T, 128, H>(a, s);
+  }
   if (group == 32) return run_dense_rows<T, Q4<32>, H>(a, s);
   if (group == 64) return run_dense_rows<T, Q4<64>, H>(a, s);
   return run_dense_rows<T, Q4<128>, H>(a, s);

@@ -194,6 +194,18 @@ def test_gated(dev, m, n, k, group, dtype):
         _check_gated(q.q4_gated(x, *gate, *up, code), x, gate, up, act)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m,n,k", [(1, 20, 9001), (2, 16, 8192), (3, 35, 12400), (4, 31, 5183), (4, 1, 640)])
+def test_few_tokens_long_rows(dev, m, n, k, group, dtype):
+    """Rows longer than one pass of a block's waves, with ends inside a block and a group."""
+    packed, up = q.q4_pack(_weights(dev, n, k), group), q.q4_pack(_weights(dev, n, k, seed=9), group)
+    x = _x(dev, m, k, TYPES[dtype], wide=3)
+    bias = torch.linspace(-1, 1, n, device=dev)
+    _check_linear(q.q4_linear(x, *packed, bias=bias), x, packed, bias)
+    _check_gated(q.q4_gated(x, *packed, *up, q.ACT_GELU), x, packed, up, "gelu")
+
+
 @pytest.mark.parametrize("scale", [2.0 ** -30, 2.0 ** 12])
 @pytest.mark.parametrize("m", [1, 20, 200])
 def test_scales_of_any_size(dev, m, scale):

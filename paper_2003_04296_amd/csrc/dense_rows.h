@@ -450,7 +450,9 @@ int run_dense_few(RowsArgs& a, hipStream_t s) {
 // (weights read again come from L2), up to 64 otherwise, so that x is not read
 // again for every 16 outputs.  From 32 on four waves per block, whose x leaves
 // LDS for two or more blocks per unit: 4-bit 4096 -> 16384 for 64 tokens 39 us
-// against 56 with eight, gated for 32 tokens 36 against 43.
+// against 56 with eight, gated for 32 tokens 36 against 43.  A single block per
+// unit and long rows: sixteen, half as many passes one after the other (4-bit
+// 8192 -> 1024 for 64 tokens, weights not in the caches: 14.4 us against 16.8).
 template <class T, class W, int H>
 int run_dense_rows(RowsArgs& a, hipStream_t s) {
   constexpr int NW = 8;
@@ -466,6 +468,8 @@ int run_dense_rows(RowsArgs& a, hipStream_t s) {
     dense_rows_kernel<T, W, H, 4, 4><<<(unsigned)blocks, 4 * 64, 0, s>>>(a);
   else if (mt == 2)
     dense_rows_kernel<T, W, H, 2, 4><<<(unsigned)blocks, 4 * 64, 0, s>>>(a);
+  else if (blocks <= 256 && a.k > NW * 128)
+    dense_rows_kernel<T, W, H, 1, 2 * NW><<<(unsigned)blocks, 2 * NW * 64, 0, s>>>(a);
   else
     dense_rows_kernel<T, W, H, 1, NW><<<(unsigned)blocks, NW * 64, 0, s>>>(a);
   return hip_status();

@@ -92,10 +92,19 @@ int run_slopes(const qconv_ffn_desc& d, const float* pre, const void* gh, int fp
 
 constexpr int ROWS_MOST = 64;  // tokens that go through dense_rows.h
 
+// Copies of x and the weights in aligned rows, first in the workspace.  The
+// backward always makes them; the forward from as many tokens on as make up
+// for copying both weights (4095 -> 16384: 242 us against 119 at 100 tokens).
+constexpr int COPY_LEAST = 384;
+static size_t copies_bytes(const qconv_ffn_desc& d, bool forward) {
+  if (forward && d.m < COPY_LEAST) return 0;
+  return realigns(d.k, d.ld_x, d.ld_w) ? realign_bytes(d.m, d.k) + 2 * realign_bytes(d.f, d.k) : 0;
+}
+
 size_t ffn_forward_bytes(const qconv_ffn_desc& d) {
   if (d.m <= ROWS_MOST) return 0;
   const size_t p = plan_h(d, false).bytes, q = plan_h(d, true).bytes;
-  return p > q ? p : q;
+  return copies_bytes(d, true) + (p > q ? p : q);
 }
 
 int launch_ffn_forward(const qconv_ffn_desc& d, const void* x, const void* wg, const void* wu, void* h, float* pre,
@@ -132,35 +141,53 @@ int launch_ffn_forward(const qconv_ffn_desc& d, const void* x, const void* wg, c
   a.pre = pre;
   a.ld_pre = (int)round_up(d.f, 8);
   a.act = d.act;
-  const bool aligned = aligned_rows(a.r[0]) && aligned_rows(a.c[0]) && aligned_rows(a.c[1]) && d.k % 8 == 0;
-  a.part = (float*)ws;
+  if (copies_bytes(d, true)) {
+    Realigner re(d.k, ws);
+    re.add(a.r[0], d.m);
+    re.add_pair(a.c[0], a.c[1], d.f);
+    const int rc = re.run(s);
+    if (rc) return rc;
+    a.k = re.a.kp;
+  }
+  const bool aligned = aligned_rows(a.r[0]) && aligned_rows(a.c[0]) && aligned_rows(a.c[1]) && a.k % 8 == 0;
+  a.part = (float*)((char*)ws + copies_bytes(d, true));
   return run_gemm<false, false, OUT_GATED>(d.dtype, a, plan_h(d, aligned), aligned, s);
 }
 
-// dg and du, then the parts of whichever product has more of them.
+// The copies, dg and du, then the parts of whichever product has more of them.
 static size_t slopes_bytes(const qconv_ffn_desc& d) { return (size_t)round_up((int64_t)d.m * 2 * round_up(d.f, 8) * 2, 16); }
 size_t ffn_backward_bytes(const qconv_ffn_desc& d) {
   size_t most = 0;
   for (bool aligned : {false, true})
     for (const GemmPlan& p : {plan_gx(d, aligned), plan_gw(d, aligned)})
       if (p.bytes > most) most = p.bytes;
-  return slopes_bytes(d) + most;
+  return copies_bytes(d, false) + slopes_bytes(d) + most;
 }
 
 int launch_ffn_backward(const qconv_ffn_desc& d, const void* x, const void* wg, const void* wu, const float* pre,
                         const void* gh, void* gx, void* gwg, void* gwu, void* ws, hipStream_t s) {
   const int fp = (int)round_up(d.f, 8);
-  uint16_t* dgu = (uint16_t*)ws;
-  float* part = (float*)((char*)ws + slopes_bytes(d));
+  uint16_t* dgu = (uint16_t*)((char*)ws + copies_bytes(d, false));
+  float* part = (float*)((char*)dgu + slopes_bytes(d));
   int rc = QCONV_OK;
+  Operand ox = {(const uint16_t*)x, d.ld_x}, og = {(const uint16_t*)wg, d.ld_w}, ou = {(const uint16_t*)wu, d.ld_w};
+  bool whole = d.k % 8 == 0;  // rows end with 16 bytes
+  if (copies_bytes(d, false)) {
+    Realigner re(d.k, ws);
+    if (gwg) re.add(ox, d.m);
+    if (gx && d.m > 0) re.add_pair(og, ou, d.f);
+    rc = re.run(s);
+    if (rc) return rc;
+    whole = true;
+  }
   if (d.m > 0)
     rc = d.dtype == QCONV_F16 ? run_slopes<F16>(d, pre, gh, fp, dgu, s) : run_slopes<BF16>(d, pre, gh, fp, dgu, s);
   if (rc == QCONV_OK && gx && d.m > 0) {
     GemmArgs a = {};
     a.r[0] = {dgu, 2 * (int64_t)fp};
     a.r[1] = {dgu + fp, 2 * (int64_t)fp};
-    a.c[0] = {(const uint16_t*)wg, d.ld_w};
-    a.c[1] = {(const uint16_t*)wu, d.ld_w};
+    a.c[0] = og;
+    a.c[1] = ou;
     a.rows = d.m;
     a.cols = d.k;
     a.k = d.f;
@@ -168,7 +195,7 @@ int launch_ffn_backward(const qconv_ffn_desc& d, const void* x, const void* wg, 
     a.halves = 1;
     a.out[0] = gx;
     a.ld_out = d.k;
-    const bool aligned = aligned_rows(a.r[0]) && aligned_rows(a.c[0]) && aligned_rows(a.c[1]) && d.k % 8 == 0;
+    const bool aligned = aligned_rows(a.r[0]) && aligned_rows(a.c[0]) && aligned_rows(a.c[1]) && whole;
     a.part = part;
     rc = run_gemm<false, true, OUT_PLAIN>(d.dtype, a, plan_gx(d, aligned), aligned, s);
   }
@@ -176,7 +203,7 @@ int launch_ffn_backward(const qconv_ffn_desc& d, const void* x, const void* wg, 
     GemmArgs a = {};
     a.r[0] = {dgu, 2 * (int64_t)fp};
     a.r[1] = {dgu + fp, 2 * (int64_t)fp};
-    a.c[0] = {(const uint16_t*)x, d.ld_x};
+    a.c[0] = ox;
     a.rows = d.f;
     a.cols = d.k;
     a.k = d.m;
@@ -185,7 +212,7 @@ int launch_ffn_backward(const qconv_ffn_desc& d, const void* x, const void* wg, 
     a.out[0] = gwg;
     a.out[1] = gwu;
     a.ld_out = d.k;
-    const bool aligned = aligned_rows(a.r[0]) && aligned_rows(a.c[0]) && d.k % 8 == 0;
+    const bool aligned = aligned_rows(a.r[0]) && aligned_rows(a.c[0]) && whole;
     a.part = part;
     rc = run_gemm<true, true, OUT_PLAIN>(d.dtype, a, plan_gw(d, aligned), aligned, s);
   }

@@ -118,6 +118,8 @@ constexpr int ROWS_MOST = 64;  // tokens that go through dense_rows.h
 GemmPlan plan_q4(const qconv_q4_desc& d, bool gated, bool aligned) {
   return gemm_plan(d.m, d.n, d.k, 1, gated, aligned, false);
 }
+// Of x's copy in aligned rows.
+size_t copy_bytes(const qconv_q4_desc& d) { return realigns(d.k, d.ld_x, 0) ? realign_bytes(d.m, d.k) : 0; }
 size_t unit_bytes(const qconv_q4_desc& d) { return (size_t)round_up(d.n, 4) * 4; }  // of one weight
 
 int launch_gemm(const qconv_q4_desc& d, const void* x, const uint8_t* const w[2], const uint16_t* const sc[2],
@@ -141,7 +143,15 @@ int launch_gemm(const qconv_q4_desc& d, const void* x, const uint8_t* const w[2]
       at += unit_bytes(d);
     }
   }
-  const bool aligned = aligned_rows(a.r[0]) && d.k % 8 == 0;
+  if (copy_bytes(d)) {
+    Realigner re(d.k, at);
+    re.add(a.r[0], d.m);
+    const int rc = re.run(s);
+    if (rc) return rc;
+    a.k = re.a.kp;  // codes past k are zero
+    at += copy_bytes(d);
+  }
+  const bool aligned = aligned_rows(a.r[0]) && a.k % 8 == 0;
   const GemmPlan p = plan_q4(d, gated, aligned);
   a.parts = p.parts;
   a.part = (float*)at;
@@ -189,7 +199,7 @@ size_t q4_workspace_bytes(const qconv_q4_desc& d, bool gated) {
   if (d.m <= ROWS_MOST) return 0;
   const size_t u = d.dtype == QCONV_F16 ? unit_bytes(d) * (gated ? 2 : 1) : 0;
   const size_t p = plan_q4(d, gated, false).bytes, q = plan_q4(d, gated, true).bytes;
-  return u + (p > q ? p : q);
+  return u + copy_bytes(d) + (p > q ? p : q);
 }
 
 int launch_q4(const qconv_q4_desc& d, const void* x, const uint8_t* w, const uint16_t* sc, const uint8_t* wu,

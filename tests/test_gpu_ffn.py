@@ -152,6 +152,31 @@ def test_rows_of_wider_tensors(dev, m, k, f, wide):
     _check_backward(gx, gg, gu, x, wg, wu, pre, gh, "silu")
 
 
+@pytest.mark.parametrize("k", [96, 61])
+@pytest.mark.parametrize("off_x,off_g,off_u,pad", [(4, 4, 4, 8), (4, 0, 0, 8), (0, 0, 4, 8), (0, 0, 4, 3), (1, 2, 3, 5),
+                                                   (0, 0, 0, 3), (0, 8, 4, 11)])
+def test_operands_aligned_differently(dev, k, off_x, off_g, off_u, pad):
+    """Each operand at an address of its own, with row strides that are and are not multiples of 16 bytes, NaN beside
+    every row: more tokens than the kernels for few take."""
+    m, f = 150 if off_x else 390, 137
+    x, wg, wu, gh = _problem(dev, m, k, f, torch.float16)
+    ld = (k + 8 + 7) // 8 * 8 + pad
+
+    def put(t, off, stride):
+        b = torch.full(((t.shape[0] + 1) * stride,), float("nan"), dtype=t.dtype, device=dev)
+        v = b[off:].as_strided(t.shape, (stride, 1), b.storage_offset() + off)
+        v.copy_(t)
+        return v
+
+    xs, gs, us = put(x, off_x, ld), put(wg, off_g, ld), put(wu, off_u, ld)
+    h, pre = q.ffn_forward(xs, gs, us, q.ACT_SILU, keep_pre=True)
+    _check_forward(h, pre, x, wg, wu, "silu")
+    gx, gg, gu = q.ffn_backward(xs, gs, us, pre, gh, q.ACT_SILU)
+    _check_backward(gx, gg, gu, x, wg, wu, pre, gh, "silu")
+    assert torch.equal(q.ffn_backward(xs, gs, us, pre, gh, q.ACT_SILU, need_w=False)[0], gx)
+    assert torch.equal(q.ffn_backward(xs, gs, us, pre, gh, q.ACT_SILU, need_x=False)[1], gg)
+
+
 def test_values_past_the_ends_are_not_read(dev):
     """NaN in a row's columns past k, in the rows after the last and in the pre buffer's padding reaches no result."""
     m, k, f = 37, 61, 45

@@ -234,6 +234,20 @@ def test_rows_of_wider_tensors(dev, m, n, k, wide):
     _check_gated(h, x, packed, packed, "silu")
 
 
+@pytest.mark.parametrize("k,off,pad", [(320, 4, 8), (320, 0, 3), (317, 0, 8), (317, 3, 5), (320, 1, 7)])
+def test_many_tokens_at_any_address(dev, k, off, pad):
+    """x with rows at and off 16-byte addresses, NaN beside every row."""
+    m, n = 130, 70
+    packed = q.q4_pack(_weights(dev, n, k), 64)
+    x = _x(dev, m, k, torch.bfloat16)
+    stride = (k + 7) // 8 * 8 + pad
+    b = torch.full(((m + 1) * stride,), float("nan"), dtype=x.dtype, device=dev)
+    v = b.as_strided((m, k), (stride, 1), off)
+    v.copy_(x)
+    _check_linear(q.q4_linear(v, *packed), x, packed, None)
+    _check_gated(q.q4_gated(v, *packed, *packed, q.ACT_RELU), x, packed, packed, "relu")
+
+
 @pytest.mark.parametrize("m", [1, 3, 40, 200])
 def test_nan_and_inf_stay_in_their_row(dev, m):
     packed = q.q4_pack(_weights(dev, 70, 320), 64)

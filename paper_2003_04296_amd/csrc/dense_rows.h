@@ -412,7 +412,7 @@ __global__ __launch_bounds__(NW * 64) void dense_few16_kernel(RowsArgs a) {
     load(0, kb * 128);
     multiply(0);
   }
-  if (kb * 128 < a.k) {
+  if (kb < (a.k + 127) / 128) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int k = kb * 128 + i * 32, left = a.k - k - o * 8;

@@ -79,6 +79,11 @@ struct Q4 {
   }
 };
 
+// Whether all inputs [k0, k0 + 128) of k exist.  k0 may lie past k, where a
+// pass is longer than what is left, and k0 + 128 past an int.
+__host__ __device__ constexpr bool whole_block(int k, int k0) { return k - k0 >= 128; }
+static_assert(whole_block(128, 0) && !whole_block(128, 1) && !whole_block(0x7fffff00, 0x7fffff80), "no overflow");
+
 // A wave's weights in one block of 128 inputs.
 template <class W, int H>
 struct RowsBlock {
@@ -192,7 +197,7 @@ __global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
   const int first = wave / WPT, col = (wave % WPT) * 512 + lane * 8;
   auto load = [&](int base) {
     const int k0 = base + wave * 128;
-    if (k0 + 128 <= a.k) b.template load<true>(a, row, k0, o);
+    if (whole_block(a.k, k0)) b.template load<true>(a, row, k0, o);
     else if (k0 < a.k) b.template load<false>(a, row, k0, o);
     const bool whole = a.k - base >= PASS;
 #pragma unroll

@@ -369,7 +369,12 @@ typedef struct {
 size_t qconv_q4_workspace_bytes(const qconv_q4_desc* d, int gated);
 
 /* y[m][n] = x[m][k] w^T + bias[n] (fp32, NULL for none); the weights are used
- * exactly (no rounding of scale * magnitude).  m == 0 launches nothing. */
+ * exactly (no rounding of scale * magnitude), for scales of any bf16 value.
+ * Past 64 tokens those that packing makes are the fast ones: others of 8
+ * significant bits take about twice the time with bf16 tokens, and others yet
+ * (subnormal ones, ones past 2^124; with fp16 tokens, ones under 2^-28 of their
+ * row's largest) several times.  Sums may take x times magnitude before its
+ * scale: bf16 tokens past 2^118 overflow.  m == 0 launches nothing. */
 int qconv_q4_linear(const qconv_q4_desc* d, const void* x, const uint8_t* codes, const uint16_t* scales,
                     const float* bias, void* y, void* workspace, size_t workspace_bytes, void* stream);
 

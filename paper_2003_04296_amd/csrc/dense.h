@@ -40,6 +40,14 @@ struct F16 {
     const _Float16 h = (_Float16)s;
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, BYTE) * v2h{h, h});
   }
+  // For a finite bf16 scale (its bits) times `unit`: 0 if the type holds its
+  // products with all magnitudes, 1 if it does together with rest_e2m1, else 2.
+  // They have at most 8 + 2 significant bits, so that the smallest one decides.
+  static constexpr bool REST = false;
+  __device__ __forceinline__ static uint32_t odd_e2m1(uint32_t scale, float unit) {
+    const float h = __uint_as_float(scale << 16) * unit * 0.5f;
+    return (float)(_Float16)h == h && h != 0.0f ? 0 : 2;
+  }
 };
 struct BF16 {
   __device__ __forceinline__ static float up(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
@@ -55,6 +63,20 @@ struct BF16 {
   __device__ __forceinline__ static uint32_t scaled_e2m1(uint32_t w, float s) {
     const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, BYTE);
     return __builtin_bit_cast(uint32_t, v2b{(__bf16)(v[0] * s), (__bf16)(v[1] * s)});
+  }
+  // what scaled_e2m1 has rounded away
+  static constexpr bool REST = true;
+  template <int BYTE>
+  __device__ __forceinline__ static uint32_t rest_e2m1(uint32_t w, float s) {
+    const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, BYTE);
+    const float x = v[0] * s, y = v[1] * s;
+    return __builtin_bit_cast(uint32_t, v2b{(__bf16)(x - (float)(__bf16)x), (__bf16)(y - (float)(__bf16)y)});
+  }
+  // 1.5 times a scale takes one bit more than it: 6 significant bits of 8 fit, and
+  // the rest of more has 2.  2: parts of it are subnormal or 6 times it infinite.
+  __device__ __forceinline__ static uint32_t odd_e2m1(uint32_t scale, float) {
+    const uint32_t e = (scale >> 7) & 0xFF;
+    return e - 2u > 249u ? 2 : (scale & 3) == 0 ? 0 : e >= 12 ? 1 : 2;
   }
 };
 

@@ -102,6 +102,7 @@ __device__ __forceinline__ const uint16_t* uniform(const uint16_t* p) {
 template <int KS_, int ROWS, int NT, int SIDE, bool COL_, bool ALIGNED, bool PAIR>
 struct Stage16 {
   static constexpr bool COL = COL_, DIRECT = ALIGNED;
+  static constexpr int SCALED = 0;  // 4-bit weights: values per scale
   static constexpr int KS = KS_, CPR = KS / 8, CH = ROWS * CPR / NT;
   const uint16_t* p[2];  // the tile's first value, product 0; by segment, or gate and up for PAIR
   int64_t ld;
@@ -179,13 +180,19 @@ struct Stage16 {
 
 // The tile of 4-bit weights, in row form: a thread takes KS / 2 codes of one
 // row (of one group) and writes them to LDS as scale * magnitude in the 16-bit
-// type.  That is exact: the scales have 6 significant bits, the magnitudes 2.
-// In fp16 a row's scales are first divided by a power of two near the largest
-// of them, multiplied back into the sums; only groups whose scale is more than
-// 2^18 below the row's largest are rounded then, to 2^-25 of that one.
+// type.  That is exact for scales of 6 significant bits, as q4_pack makes them:
+// the magnitudes have 2.  In fp16 a row's scales are first multiplied by a power
+// of two that takes the largest of them to [2^12, 2^13) (6 times as much is
+// still below 65504), divided out of the sums again, and groups down to 2^-28 of
+// that one are exact.  A scale whose products the type does not hold shows in
+// `odd` as it passes.  The tile then gets a second pass over what the first has
+// rounded away (bf16), or is summed anew by multiply_groups.  512 tokens, 4096 ->
+// 16384 in bf16: 84 us for packed scales, 142 with one scale of 8 bits in the
+// weight, 181 with nothing else; by multiply_groups alone 399 and 731.
 template <class T, int KS_, int ROWS, int NT, int GROUP, bool PAIR>
 struct StageQ4 {
   static constexpr bool COL = false, DIRECT = false;
+  static constexpr int SCALED = GROUP;
   static constexpr int KS = KS_, CPR = KS / 8, CH = 1, W = KS / 16;  // 8 codes per word
   static_assert(ROWS * 2 == NT, "two threads per row");
   typedef std::conditional_t<W == 4, v4u, v2u> Codes;
@@ -194,10 +201,14 @@ struct StageQ4 {
   float unit;
   int kp;
   bool in;
+  bool rest;     // the second pass
+  uint32_t odd;  // bit 0: it is needed; bit 1: it does not do
   Codes code;
   uint32_t sc;
 
   __device__ __forceinline__ void init(const GemmArgs& a, int, int64_t r0) {
+    rest = false;
+    odd = 0;
     const int t = threadIdx.x / 2, half = PAIR && (t & 32) ? 1 : 0;
     const int64_t row = r0 + weight_row<PAIR>(t);
     in = row < a.cols;
@@ -223,11 +234,19 @@ struct StageQ4 {
   static constexpr int PIECES = W;
   __device__ __forceinline__ void store(lds_v4u* lds, int q) {
     const float s = BF16::up((uint16_t)sc) * unit;
+    if (q == 0 && (sc & 0x7FFF) != 0 && (sc & 0x7F80) != 0x7F80) odd |= T::odd_e2m1(sc, unit);
     const int t = threadIdx.x / 2;
     const uint32_t c = code[q];
-    lds[t * CPR + (((threadIdx.x & 1) * W + q) ^ swz_row<KS>(t))] =
-        v4u{T::template scaled_e2m1<0>(c, s), T::template scaled_e2m1<1>(c, s), T::template scaled_e2m1<2>(c, s),
-            T::template scaled_e2m1<3>(c, s)};
+    lds_v4u* const to = lds + t * CPR + (((threadIdx.x & 1) * W + q) ^ swz_row<KS>(t));
+    if constexpr (T::REST) {
+      if (rest) {
+        *to = v4u{T::template rest_e2m1<0>(c, s), T::template rest_e2m1<1>(c, s), T::template rest_e2m1<2>(c, s),
+                  T::template rest_e2m1<3>(c, s)};
+        return;
+      }
+    }
+    *to = v4u{T::template scaled_e2m1<0>(c, s), T::template scaled_e2m1<1>(c, s), T::template scaled_e2m1<2>(c, s),
+              T::template scaled_e2m1<3>(c, s)};
   }
 };
 
@@ -440,6 +459,69 @@ __device__ __forceinline__ void multiply64(v4f (&acc)[4][NR], SR& sr, SC& sc, in
   for (int i = 0; i < PIECES; ++i) store_piece(sr, sc, tr, tc, i);
 }
 
+// The two low bits of all lanes of the block, or-ed.  LDS is free for it, before and after.
+template <int WAVES>
+__device__ __forceinline__ uint32_t or_lanes(uint32_t bits, lds_v4u* lds) {
+  const uint32_t mine = (__ballot(bits & 1) != 0 ? 1u : 0u) | (__ballot(bits & 2) != 0 ? 2u : 0u);
+  __syncthreads();
+  lds[threadIdx.x / 64] = v4u{mine, 0, 0, 0};
+  __syncthreads();
+  uint32_t all = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) all |= lds[w][0];
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(all);
+}
+
+// The sums over products [from, to) of 16 columns (of gate and up, H = 2) and
+// all of a wave's rows, for 4-bit weights of any scales: 32 products of the bare
+// magnitudes at a time, times the scale in fp32.  r, w: the first row of x and
+// of the weights.  Operands come from global memory as they are needed: weights
+// that take this path are right, not fast.
+template <class T, int GROUP, int H, bool WHOLE, int NR>
+__device__ __forceinline__ void multiply_groups(v4f (&sums)[H][NR], const GemmArgs& a, int64_t r, int64_t w, int from,
+                                                int to) {
+  const int lane = threadIdx.x & 63, o = lane >> 4;
+  // rows past the ends: the last one, whose results there go nowhere
+  auto row = [&](int64_t first, int n) { return first + (lane & 15) < n ? first + (lane & 15) : (int64_t)n - 1; };
+  const int64_t wr = row(w, a.cols);
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int j = 0; j < NR; ++j) sums[h][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k0 = from; k0 < to; k0 += 32) {
+    const int k = k0 + o * 8;
+    v4u fc[H];
+    v4f s[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const uint32_t c = *(const uint32_t*)(a.codes[h] + wr * (a.kp / 2) + k / 2);
+      const float scale = BF16::up(a.scales[h][wr * (a.kp / GROUP) + k0 / GROUP]);
+      fc[h] = v4u{T::template from_e2m1<0>(c), T::template from_e2m1<1>(c), T::template from_e2m1<2>(c),
+                  T::template from_e2m1<3>(c)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[h][e] = __shfl(scale, o * 4 + e);
+    }
+#pragma unroll
+    for (int j = 0; j < NR; ++j) {
+      const uint16_t* x = a.r[0].p + row(r + j * 16, a.rows) * a.r[0].ld;
+      v4u f;
+      if constexpr (WHOLE) {
+        f = load8(x + (k < a.k ? k : 0));
+        f = k < a.k ? f : v4u{0, 0, 0, 0};
+      } else {
+        f = load8_first(x + k, a.k - k);
+      }
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const v4f sum = T::mfma(fc[h], f, v4f{0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[h][j][e] = fmaf(s[h][e], sum[e], sums[h][j][e]);
+      }
+    }
+  }
+}
+
 template <class T, class SR, class SC, int OUT, int BR, int BC>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds) {
   constexpr int KS = SR::KS, NR = BR / 32, PAIR = OUT == OUT_GATED;
@@ -472,11 +554,12 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
   sc.init(a, 0, c0);
   // Before the loads of step s: they start, change operands or end there.
   int until = begin < steps && end > steps ? steps : end;
-  {
+  auto restart = [&] {
     const int seg = begin >= steps ? 1 : 0, k0 = (begin - seg * steps) * KS;
     sr.begin(seg, k0, begin < end ? a.k - k0 : 0);
     sc.begin(seg, k0, begin < end ? a.k - k0 : 0);
-  }
+  };
+  restart();
   auto start = [&](int s) {
     if (s != until) return;
     const bool more = s < end;
@@ -497,16 +580,42 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
 #pragma unroll
     for (int i = 0; i < SR::PIECES + SC::PIECES; ++i) store_piece(sr, sc, to, to + LR, i);
   };
+  [[maybe_unused]] uint32_t odd = 0;
   if constexpr (KS == 64) {
     static_assert(!SR::COL && !SC::COL, "one segment");
-    load(lds);
-    store(lds);
-    for (int s = begin; s < end; ++s) {
-      const int b = (s - begin) & 1;
-      stage_barrier<0, REGS>();
-      multiply64<T, BR, BC>(acc, sr, sc, wr, wc, lds + b * STAGE, lds + (b ^ 1) * STAGE,
-                            lds + (b ^ 1) * STAGE + LR);
-      next();
+    auto pass = [&] {
+      load(lds);
+      store(lds);
+      for (int s = begin; s < end; ++s) {
+        const int b = (s - begin) & 1;
+        stage_barrier<0, REGS>();
+        multiply64<T, BR, BC>(acc, sr, sc, wr, wc, lds + b * STAGE, lds + (b ^ 1) * STAGE,
+                              lds + (b ^ 1) * STAGE + LR);
+        next();
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load may reach LDS after what uses it next
+    };
+    if constexpr (SC::SCALED == 0) {
+      pass();
+    } else {
+      for (;;) {
+        pass();
+        if (T::REST && sc.rest) break;
+        odd = or_lanes<BC / 32>(sc.odd, lds);
+        if (!T::REST || odd != 1) break;
+        // an infinite sum stays: the second pass would add infinity times zero
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < NR; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z += acc[i][j][e] * 0.0f;
+        odd |= or_lanes<BC / 32>(z == 0.0f ? 0 : 2, lds);
+        if (odd & 2) break;
+        sc.rest = true;
+        restart();
+      }
     }
   } else {
     // Stages loaded straight into LDS are 4 steps ahead.  Those that pass
@@ -542,12 +651,25 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load may reach LDS after the block has left it
+  constexpr int H = PAIR ? 2 : 1;
+  const int64_t c1 = c0 + (PAIR ? wc / 2 : wc) + (lane >> 4) * 4;
+  // The sums of row group j and column group i.
+  auto put = [&](auto act, int i, int j, v4f v[2]) {
+    const int64_t r = r0 + wr + j * 16 + (lane & 15), c = c1 + i * 16;
+    if (r >= a.rows || c >= a.cols) return;
+    if (a.parts > 1) {
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const int64_t plane = (int64_t)part * (PAIR ? 2 : a.halves) + (PAIR ? h : half);
+        *(v4f*)(a.part + (plane * a.rows + r) * a.ld_part + c) = v[h];
+      }
+    } else {
+      finish4<T, OUT, decltype(act)::value>(a, half, r, c, v);
+    }
+  };
   auto finish = [&](auto act) {
-    constexpr int ACT = decltype(act)::value;
     // Row by row, so that the two halves of a 128-byte line are written one
     // after the other.
-    constexpr int H = PAIR ? 2 : 1;
-    const int64_t c1 = c0 + (PAIR ? wc / 2 : wc) + (lane >> 4) * 4;
     v4f back[4 / H][H];  // what the 4-bit weights' rows were divided by
 #pragma unroll
     for (int i = 0; i < 4 / H; ++i)
@@ -559,31 +681,36 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds)
           back[i][h][e] = a.unit[h] && c < a.cols ? 1.0f / a.unit[h][c] : 1.0f;
         }
 #pragma unroll
-    for (int j = 0; j < NR; ++j) {
-      const int64_t r = r0 + wr + j * 16 + (lane & 15);
-      if (r >= a.rows) continue;
+    for (int j = 0; j < NR; ++j)
 #pragma unroll
       for (int i = 0; i < 4 / H; ++i) {
-        const int64_t c = c1 + i * 16;
-        if (c >= a.cols) continue;
         v4f v[2] = {acc[i][j] * back[i][0], v4f{}};
         if constexpr (PAIR) v[1] = acc[i + 2][j] * back[i][H - 1];
-        if (a.parts > 1) {
-#pragma unroll
-          for (int h = 0; h < H; ++h) {
-            const int64_t plane = (int64_t)part * (PAIR ? 2 : a.halves) + (PAIR ? h : half);
-            *(v4f*)(a.part + (plane * a.rows + r) * a.ld_part + c) = v[h];
-          }
-        } else {
-          finish4<T, OUT, ACT>(a, half, r, c, v);
-        }
+        put(act, i, j, v);
       }
-    }
   };
   if constexpr (PAIR)
     with_act(a.act, finish);
   else
     finish(std::integral_constant<int, 0>{});
+  // Each lane stores over what it has stored: the sums above need no registers then.
+  if constexpr (SC::SCALED != 0) {
+    if (odd & 2) {
+#pragma unroll 1
+      for (int i = 0; i < 4 / H; ++i) {
+        v4f sums[H][NR];
+        multiply_groups<T, SC::SCALED, H, SR::DIRECT>(sums, a, r0 + wr, c0 + (PAIR ? wc / 2 : wc) + i * 16, begin * KS,
+                                                      end < steps ? end * KS : a.k);
+        with_act(PAIR ? a.act : 0, [&](auto act) {
+#pragma unroll
+          for (int j = 0; j < NR; ++j) {
+            v4f v[2] = {sums[0][j], sums[H - 1][j]};
+            put(act, i, j, v);
+          }
+        });
+      }
+    }
+  }
 }
 
 template <class T, class SR, class SC, int OUT, int BR, int BC>

@@ -1,9 +1,11 @@
 // q4.hip -- weights of 4 bits with group scales: packing, and the products
 //   y = x W^T + bias,   h = act(x Wg^T) * (x Wu^T)
-// with W = scale * E2M1 magnitude.  The codes become 16-bit operands by the
-// conversion instruction (exact), one matrix instruction sums 32 products of
-// a group, and the fp32 sum of a group is multiplied by its scale, so no
-// weight is ever rounded.
+// with W = scale * E2M1 magnitude, whatever bf16 value the scale is.  No weight is
+// rounded: for few tokens the codes become 16-bit operands by the conversion
+// instruction (exact), one matrix instruction sums 32 products of a group, and
+// the group's fp32 sum is multiplied by its scale; for many the operands are
+// scale * magnitude, and a tile with scales whose products 16 bits do not hold is
+// summed in two parts or group by group (dense_gemm.h).
 #include "dense_gemm.h"
 #include "dense_rows.h"
 
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const void* __restrict__ w
 }
 
 // For each weight row the power of two that takes its largest finite scale to
-// [1, 2); a wave per row.
+// [2^12, 2^13); a wave per row.
 __global__ __launch_bounds__(256) void q4_unit_kernel(const uint16_t* __restrict__ scales, int n, int groups,
                                                       float* __restrict__ unit) {
   const int row = blockIdx.x * 4 + threadIdx.x / 64;
@@ -88,8 +90,8 @@ __global__ __launch_bounds__(256) void q4_unit_kernel(const uint16_t* __restrict
     const uint32_t v = __shfl_xor(top, d);
     if (v > top) top = v;
   }
-  // 2^(127 - top), kept a normal number
-  if ((threadIdx.x & 63) == 0) unit[row] = __uint_as_float((top < 1 ? 253u : top > 253 ? 1u : 254u - top) << 23);
+  // 2^(139 - top), it and its reciprocal kept normal numbers
+  if ((threadIdx.x & 63) == 0) unit[row] = __uint_as_float((top < 13 ? 253u : 266u - top) << 23);
 }
 
 template <class T, int OUT, int GROUP>

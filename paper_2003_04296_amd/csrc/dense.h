@@ -105,11 +105,13 @@ __device__ __forceinline__ float sigmoid(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
 }
 
-// act(g) and act'(g) in fp32.
+// act(g) and act'(g) in fp32.  GELU's normal distribution function through erfc,
+// which keeps its leading digits where g is negative: 1 + erf(g / sqrt(2))
+// cancels, has 3 bits left at g = -5 and is 0 from -5.6 on.
 template <int ACT>
 __device__ __forceinline__ float act_value(float g) {
   if constexpr (ACT == QCONV_ACT_SILU) return g * sigmoid(g);
-  else if constexpr (ACT == QCONV_ACT_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+  else if constexpr (ACT == QCONV_ACT_GELU) return 0.5f * g * erfcf(g * -0.70710678118654752f);
   else return g < 0.0f ? 0.0f : g;  // a NaN stays
 }
 template <int ACT>
@@ -118,7 +120,7 @@ __device__ __forceinline__ float act_slope(float g) {
     const float p = sigmoid(g);
     return p * (1.0f + g * (1.0f - p));
   } else if constexpr (ACT == QCONV_ACT_GELU) {
-    return 0.5f * (1.0f + erff(g * 0.70710678118654752f)) + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+    return 0.5f * erfcf(g * -0.70710678118654752f) + g * expf(-0.5f * g * g) * 0.39894228040143268f;
   } else {
     return g > 0.0f ? 1.0f : 0.0f;
   }

@@ -25,17 +25,22 @@ class GatedBlock:
         self.masters = [torch.randn((f, k), generator=gen, device=device).mul_(k ** -0.5).clamp_(-1, 1)
                         for _ in range(2)]
         self.weights = [w.to(dtype) for w in self.masters]
-        self._pre = None
 
     def forward(self, x):
-        h, self._pre = ffn_forward(x, *self.weights, self.act, keep_pre=True)
-        return h
+        return ffn_forward(x, *self.weights, self.act)[0]
 
-    def step(self, x, gh, lr: float, max_norm: float):
-        """From the gradient of the last forward's h: the weights one SGD step
-        on, with the gradients' joint norm held to max_norm -> (gradient of x,
-        norm before clipping)."""
-        gx, *grads = ffn_backward(x, *self.weights, self._pre, gh, self.act)
+    def forward_train(self, x):
+        """-> (h, what step needs of this forward)."""
+        return ffn_forward(x, *self.weights, self.act, keep_pre=True)
+
+    def step(self, x, gh, lr: float, max_norm: float, pre=None):
+        """From the gradient gh of h at x: the weights one SGD step on, with the
+        gradients' joint norm held to max_norm -> (gradient of x, norm before
+        clipping).  pre: from forward_train(x) with the present weights;
+        without it the forward is computed again."""
+        if pre is None:
+            pre = self.forward_train(x)[1]
+        gx, *grads = ffn_backward(x, *self.weights, pre, gh, self.act)
         grads = [g.float() for g in grads]
         norm = aqe_clip_grads(grads, max_norm)
         for w, master, g in zip(self.weights, self.masters, grads):
@@ -67,10 +72,10 @@ def train(steps: int = 150, m: int = 256, k: int = 128, f: int = 192, lr: float 
     losses = []
     for _ in range(steps):
         x = torch.randn((m, k), generator=gen, device=device).to(torch.bfloat16)
-        want, h = teacher.forward(x), block.forward(x)
+        want, (h, pre) = teacher.forward(x), block.forward_train(x)
         diff = h.float() - want.float()
         losses.append(diff.square().mean())
-        block.step(x, (diff * (2.0 / m)).to(h.dtype), lr, max_norm)
+        block.step(x, (diff * (2.0 / m)).to(h.dtype), lr, max_norm, pre)
     return block, teacher, torch.stack(losses).tolist()
 
 

@@ -578,6 +578,7 @@ def _norm_out(grads, norm, what, stream):
         return _new((), torch.float32, grads[0] if len(grads) else torch.empty(0, device="cuda"), stream)
     if norm.dtype != torch.float32 or norm.numel() != 1 or (len(grads) and norm.device != grads[0].device):
         raise ValueError(f"{what}: norm is one fp32 value on the gradients' device")
+    _on_gpu(norm, what)  # there may be no gradient to compare it with
     return norm
 
 

@@ -318,9 +318,22 @@ def _new(shape, dtype, like, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _on_gpu(t, what: str):
+_current_device = None  # torch's lookup, once it has a device
+
+
+def _on_gpu(t, what: str, stream):
+    """Kernels go to a stream of the current device: it has to be the tensors'."""
+    global _current_device
     if not t.is_cuda:
         raise ValueError(f"{what}: tensors are on the GPU, got one on {t.device}")
+    if _current_device is None:
+        import torch
+
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    d = t.get_device()
+    if d != _current_device() or (stream is not None and stream.device_index != d):
+        raise ValueError(f"{what}: tensors are on cuda:{d}, the current device is cuda:{_current_device()}"
+                         + (f", the stream is of cuda:{stream.device_index}" if stream is not None else ""))
 
 
 # A call for one token takes 3 us on the GPU, so the checks below ask each
@@ -367,12 +380,12 @@ _FFN_DESC = struct.Struct("5i4x3q")
 _Q4_DESC = struct.Struct("5i4x2q")
 
 
-def _ffn_sizes(x, w_gate, what):
+def _ffn_sizes(x, w_gate, what, stream):
     """(m, k, f) of a feed-forward call."""
     s, w = x.shape, w_gate.shape
     if len(s) != 2 or len(w) != 2:
         raise ValueError(f"{what}: x and the weights are matrices")
-    _on_gpu(x, what)
+    _on_gpu(x, what, stream)
     return s[0], s[1], w[0]
 
 
@@ -394,7 +407,7 @@ def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pr
     """h = act(x w_gate^T) * (x w_up^T) for 16-bit x [m][k] and weights [f][k]
     -> (h [m][f], pre).  keep_pre (or a buffer `pre` of a former call) keeps
     what ffn_backward needs, else pre is None."""
-    m, k, f = _ffn_sizes(x, w_gate, "ffn_forward")
+    m, k, f = _ffn_sizes(x, w_gate, "ffn_forward", stream)
     d = _ffn_desc(x, w_gate, w_up, act, f if out is None else _rows(out, m, f, x, "ffn_forward out"), m, k, f,
                   "ffn_forward")
     L = lib()
@@ -424,7 +437,7 @@ def ffn_backward(x, w_gate, w_up, pre, gh, act: int = ACT_SILU, need_x: bool = T
     """From gh [m][f] and the forward's pre -> (gx [m][k], gw_gate [f][k],
     gw_up [f][k]) in x's type; None for what need_x / need_w leave out.  out:
     contiguous tensors to write instead of new ones."""
-    m, k, f = _ffn_sizes(x, w_gate, "ffn_backward")
+    m, k, f = _ffn_sizes(x, w_gate, "ffn_backward", stream)
     d = _ffn_desc(x, w_gate, w_up, act, _rows(gh, m, f, x, "ffn_backward gh"), m, k, f, "ffn_backward")
     _check_pre(pre, m, f, x, "ffn_backward")
     gx, gg, gu = out if out is not None else (None, None, None)
@@ -449,7 +462,7 @@ def q4_pack(w, group: int = 64, top: int = 6, out=None, stream=None):
 
     if w.dim() != 2:
         raise ValueError("q4_pack: w is a matrix")
-    _on_gpu(w, "q4_pack")
+    _on_gpu(w, "q4_pack", stream)
     n, k = w.shape
     ld = _rows(w, n, k, w, "q4_pack")
     if out is None:
@@ -483,12 +496,12 @@ def _q4_group(codes, scales, n, k, like, what, group=None) -> int:
     return group
 
 
-def _q4_sizes(x, codes, scales, what):
+def _q4_sizes(x, codes, scales, what, stream):
     """(m, n, k, group) of a product with packed weights."""
     s, c = x.shape, codes.shape
     if len(s) != 2 or len(c) != 2:
         raise ValueError(f"{what}: x and codes are matrices")
-    _on_gpu(x, what)
+    _on_gpu(x, what, stream)
     m, k = s
     n = c[0]
     return m, n, k, _q4_group(codes, scales, n, k, x, what)
@@ -502,7 +515,7 @@ def _q4_desc(x, m, n, k, group, out, what):
 def q4_linear(x, codes, scales, bias=None, out=None, workspace=None, stream=None):
     """y [m][n] = x [m][k] w^T + bias with 4-bit weights (q4_pack); x and y
     fp16 or bf16, bias fp32 [n]."""
-    m, n, k, group = _q4_sizes(x, codes, scales, "q4_linear")
+    m, n, k, group = _q4_sizes(x, codes, scales, "q4_linear", stream)
     d = _q4_desc(x, m, n, k, group, out, "q4_linear")
     if bias is not None:
         import torch
@@ -522,7 +535,7 @@ def q4_linear(x, codes, scales, bias=None, out=None, workspace=None, stream=None
 def q4_gated(x, gate_codes, gate_scales, up_codes, up_scales, act: int = ACT_SILU, out=None, workspace=None,
              stream=None):
     """h [m][n] = act(x w_gate^T) * (x w_up^T) with 4-bit weights."""
-    m, n, k, group = _q4_sizes(x, gate_codes, gate_scales, "q4_gated")
+    m, n, k, group = _q4_sizes(x, gate_codes, gate_scales, "q4_gated", stream)
     if _q4_group(up_codes, up_scales, n, k, x, "q4_gated up") != group:
         raise ValueError("q4_gated: gate and up weights have different groups")
     d = _q4_desc(x, m, n, k, group, out, "q4_gated")
@@ -547,7 +560,7 @@ def _dense(t) -> bool:
     return True
 
 
-def _grad_arrays(grads, what):
+def _grad_arrays(grads, what, stream):
     """(count, pointers, sizes, types, dense order) of a list of gradients as C
     arrays.  One pass per property with the tensors' own methods: a model has
     hundreds of gradients, and a Python loop body costs more than the kernels."""
@@ -559,7 +572,7 @@ def _grad_arrays(grads, what):
     codes = array("i", [_dtypes[types[0]]]) * n if n and types.count(types[0]) == n else \
         array("i", map(_dtypes.__getitem__, types))
     if n:
-        _on_gpu(grads[0], what)
+        _on_gpu(grads[0], what, stream)
     plain = all(map(T.is_contiguous, grads))
     if len(set(map(T.get_device, grads))) > 1 or -1 in codes or not (plain or all(map(_dense, grads))):
         raise ValueError(f"{what}: gradients are dense fp32, fp16 or bf16 tensors on one device")
@@ -578,13 +591,13 @@ def _norm_out(grads, norm, what, stream):
         return _new((), torch.float32, grads[0] if len(grads) else torch.empty(0, device="cuda"), stream)
     if norm.dtype != torch.float32 or norm.numel() != 1 or (len(grads) and norm.device != grads[0].device):
         raise ValueError(f"{what}: norm is one fp32 value on the gradients' device")
-    _on_gpu(norm, what)  # there may be no gradient to compare it with
+    _on_gpu(norm, what, stream)  # there may be no gradient to compare it with
     return norm
 
 
 def aqe_grad_norm(grads, norm=None, workspace=None, stream=None):
     """The 2-norm over all values of a list of gradients, as a device scalar."""
-    n, ptrs, sizes, types, _ = _grad_arrays(grads, "aqe_grad_norm")
+    n, ptrs, sizes, types, _ = _grad_arrays(grads, "aqe_grad_norm", stream)
     norm = _norm_out(grads, norm, "aqe_grad_norm", stream)
     ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, _addr(sizes)), norm, "aqe_grad_norm", stream)
     _check(lib().aqe_grad_norm(n, _addr(ptrs), _addr(sizes), _addr(types), _ptr(norm), _ptr(ws), nbytes,
@@ -596,10 +609,10 @@ def aqe_clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, 
     """Scale a list of gradients so that their joint norm is at most max_norm,
     in place or into the tensors of `out` (same sizes, types and layouts); returns
     the norm before, as a device scalar."""
-    n, ptrs, sizes, types, plain = _grad_arrays(grads, "aqe_clip_grads")
+    n, ptrs, sizes, types, plain = _grad_arrays(grads, "aqe_clip_grads", stream)
     outs = ptrs
     if out is not None:
-        m, outs, out_sizes, out_types, out_plain = _grad_arrays(out, "aqe_clip_grads")
+        m, outs, out_sizes, out_types, out_plain = _grad_arrays(out, "aqe_clip_grads", stream)
         if m != n or out_sizes != sizes or out_types != types or (n and out[0].device != grads[0].device) or \
                 not (plain and out_plain or all(o.stride() == g.stride() for o, g in zip(out, grads))):
             raise ValueError("aqe_clip_grads: out holds one tensor per gradient, of its size, layout, type and device")

@@ -178,7 +178,7 @@ struct Stage16 {
   __device__ __forceinline__ void store(lds_v4u* lds, int j) { lds[index(j)] = reg[j]; }
 };
 
-// The tile of 4-bit weights, in row form: a thread takes KS / 2 codes of one
+// The tile of 4-bit weights, in row form: a thread takes 32 codes of one
 // row (of one group) and writes them to LDS as scale * magnitude in the 16-bit
 // type.  That is exact for scales of 6 significant bits, as q4_pack makes them:
 // the magnitudes have 2.  In fp16 a row's scales are first multiplied by a power
@@ -189,13 +189,12 @@ struct Stage16 {
 // rounded away (bf16), or is summed anew by multiply_groups.  512 tokens, 4096 ->
 // 16384 in bf16: 84 us for packed scales, 142 with one scale of 8 bits in the
 // weight, 181 with nothing else; by multiply_groups alone 399 and 731.
-template <class T, int KS_, int ROWS, int NT, int GROUP, bool PAIR>
+template <class T, int ROWS, int NT, int GROUP, bool PAIR>
 struct StageQ4 {
   static constexpr bool COL = false, DIRECT = false;
   static constexpr int SCALED = GROUP;
-  static constexpr int KS = KS_, CPR = KS / 8, CH = 1, W = KS / 16;  // 8 codes per word
+  static constexpr int KS = 64, CPR = KS / 8, CH = 1, W = KS / 16;  // 8 codes per word
   static_assert(ROWS * 2 == NT, "two threads per row");
-  typedef std::conditional_t<W == 4, v4u, v2u> Codes;
   const uint8_t* p;
   const uint16_t* sp;
   float unit;
@@ -203,7 +202,7 @@ struct StageQ4 {
   bool in;
   bool rest;     // the second pass
   uint32_t odd;  // bit 0: it is needed; bit 1: it does not do
-  Codes code;
+  v4u code;
   uint32_t sc;
 
   __device__ __forceinline__ void init(const GemmArgs& a, int, int64_t r0) {
@@ -228,7 +227,7 @@ struct StageQ4 {
   }
   __device__ __forceinline__ void chunk(lds_v4u*, int) {
     const bool on = in && k < kp && left > 0;
-    code = on ? *(const Codes*)(p + k / 2) : Codes{};
+    code = on ? *(const v4u*)(p + k / 2) : v4u{};
     sc = on ? sp[k / GROUP] : 0u;
   }
   static constexpr int PIECES = W;

@@ -99,12 +99,12 @@ int run_gemm_q4(GemmArgs& a, int tile, bool aligned, hipStream_t s) {
   constexpr bool PAIR = OUT == OUT_GATED;
   constexpr int KS = 64;
   if (!aligned)
-    return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, false, false, false>, StageQ4<T, KS, 128, 256, GROUP, PAIR>, OUT,
+    return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, false, false, false>, StageQ4<T, 128, 256, GROUP, PAIR>, OUT,
                           128>(a, s);
   if (tile == 256)
-    return run_gemm_tiles<T, Stage16<KS, 256, 512, 0, false, true, false>, StageQ4<T, KS, 256, 512, GROUP, PAIR>, OUT,
+    return run_gemm_tiles<T, Stage16<KS, 256, 512, 0, false, true, false>, StageQ4<T, 256, 512, GROUP, PAIR>, OUT,
                           256>(a, s);
-  return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, false, true, false>, StageQ4<T, KS, 128, 256, GROUP, PAIR>, OUT,
+  return run_gemm_tiles<T, Stage16<KS, 128, 256, 0, false, true, false>, StageQ4<T, 128, 256, GROUP, PAIR>, OUT,
                         128>(a, s);
 }
 

@@ -560,6 +560,12 @@ def _dense(t) -> bool:
     return True
 
 
+def _same_layout(a, b) -> bool:
+    """Whether two dense tensors of as many values hold them in the same order."""
+    return (a.is_contiguous() and b.is_contiguous()) or \
+        (a.shape == b.shape and all(n == 1 or i == j for n, i, j in zip(a.shape, a.stride(), b.stride())))
+
+
 def _grad_arrays(grads, what, stream):
     """(count, pointers, sizes, types, dense order) of a list of gradients as C
     arrays.  One pass per property with the tensors' own methods: a model has
@@ -614,7 +620,7 @@ def aqe_clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, 
     if out is not None:
         m, outs, out_sizes, out_types, out_plain = _grad_arrays(out, "aqe_clip_grads", stream)
         if m != n or out_sizes != sizes or out_types != types or (n and out[0].device != grads[0].device) or \
-                not (plain and out_plain or all(o.stride() == g.stride() for o, g in zip(out, grads))):
+                not (plain and out_plain or all(map(_same_layout, out, grads))):
             raise ValueError("aqe_clip_grads: out holds one tensor per gradient, of its size, layout, type and device")
     norm = _norm_out(grads, norm, "aqe_clip_grads", stream)
     ws, nbytes = _workspace(workspace, lib().aqe_grad_norm_bytes(n, _addr(sizes)), norm, "aqe_clip_grads", stream)

@@ -330,7 +330,8 @@ int qconv_ffn_forward(const qconv_ffn_desc* d, const void* x, const void* w_gate
 size_t qconv_ffn_backward_bytes(const qconv_ffn_desc* d);
 
 /* From gh[m][f] (the gradient of h) and the forward's pre:
- *   dg = gh u act'(g), du = gh act(g), rounded to the tensors' type, then
+ *   dg = gh u act'(g), du = gh act(g), rounded to the tensors' type (with fp16
+ *   infinite past 65504: the caller scales the loss as for any gradient), then
  *   gx[m][k] = dg w_gate + du w_up,  gw_gate[f][k] = dg^T x,  gw_up[f][k] = du^T x.
  * gx, and gw_gate together with gw_up, may be NULL to leave them out; they
  * are contiguous.  m == 0 gives zero weight gradients. */
@@ -389,8 +390,9 @@ int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_co
 
 /* grads (host array of `count` device pointers), numel (host), dtypes (host;
  * qconv_dtype each).  norm (device float) receives sqrt(sum of all squares),
- * summed in fp64 in an order that the sizes alone fix. count == 0 and tensors
- * of no values are allowed (a null pointer is, with numel 0). */
+ * summed in fp64 in an order fixed by the sizes, the types and the addresses
+ * modulo 16 bytes. count == 0 and tensors of no values are allowed (a null
+ * pointer is, with numel 0). */
 size_t aqe_grad_norm_bytes(int count, const int64_t* numel);
 int aqe_grad_norm(int count, const void* const* grads, const int64_t* numel, const int* dtypes, float* norm,
                   void* workspace, size_t workspace_bytes, void* stream);
@@ -399,7 +401,7 @@ int aqe_grad_norm(int count, const void* const* grads, const int64_t* numel, con
  * norm > max_norm and 1 otherwise (a NaN norm leaves the values as they are;
  * an infinite one gives c = 0); c is rounded to fp32, the product to the
  * tensor's type.  out[t] may be grads[t] itself (clipping in place) or a
- * tensor that overlaps no gradient.  max_norm >= 0. */
+ * tensor that overlaps no gradient; a tensor is named once.  max_norm >= 0. */
 int aqe_clip_grads(int count, const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes,
                    float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
 

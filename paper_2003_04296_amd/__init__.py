@@ -287,7 +287,9 @@ def aqe_sgd_clip(w, g, lr: float, stream=None):
 
 
 # ---------------------------------------------------------------------------
-# Fully connected operators and the gradient norm
+# Fully connected operators and the gradient norm.  They work on the tensors'
+# memory: autograd records nothing (ffn_backward is the gradient), and what is
+# written in place does not change a tensor's version.
 # ---------------------------------------------------------------------------
 
 class _Dtypes(dict):
@@ -406,7 +408,7 @@ def ffn_forward(x, w_gate, w_up, act: int = ACT_SILU, keep_pre: bool = False, pr
                 workspace=None, stream=None):
     """h = act(x w_gate^T) * (x w_up^T) for 16-bit x [m][k] and weights [f][k]
     -> (h [m][f], pre).  keep_pre (or a buffer `pre` of a former call) keeps
-    what ffn_backward needs, else pre is None."""
+    what ffn_backward needs, else pre is None.  h has no autograd graph."""
     m, k, f = _ffn_sizes(x, w_gate, "ffn_forward", stream)
     d = _ffn_desc(x, w_gate, w_up, act, f if out is None else _rows(out, m, f, x, "ffn_forward out"), m, k, f,
                   "ffn_forward")
@@ -457,7 +459,8 @@ def q4_pack(w, group: int = 64, top: int = 6, out=None, stream=None):
     """A matrix [n][k] (fp32 or 16-bit) -> (codes uint8 [n][kp / 2], scales
     bf16 [n][kp / group]): 4-bit E2M1 codes with a scale per `group` values of
     a row; top: the magnitude a group's largest value maps to (6, or 4 for
-    weights that sit on the levels of 1..3 bits)."""
+    weights that sit on the levels of 1..3 bits).  The products take any bf16
+    scales, those made here fastest."""
     import torch
 
     if w.dim() != 2:
@@ -614,7 +617,7 @@ def aqe_grad_norm(grads, norm=None, workspace=None, stream=None):
 def aqe_clip_grads(grads, max_norm: float, out=None, norm=None, workspace=None, stream=None):
     """Scale a list of gradients so that their joint norm is at most max_norm,
     in place or into the tensors of `out` (same sizes, types and layouts); returns
-    the norm before, as a device scalar."""
+    the norm before, as a device scalar.  A tensor is listed once."""
     n, ptrs, sizes, types, plain = _grad_arrays(grads, "aqe_clip_grads", stream)
     outs = ptrs
     if out is not None:

@@ -8,11 +8,12 @@
 // transposing LDS reads.  4-bit weights are expanded on their way into LDS.
 //
 // Bound by the matrix cores at many tokens, by reading the operands at few.
-// Measured in bf16, 4096 <-> 16384 features and 8192 tokens (2.2 TFLOP each):
-// forward 1.87 ms (1175 TFLOP/s; 2.11 with the 1.07 GB of pre, which leave at
-// the memory's rate while the next tile waits), gx 1.70 ms (1290), both weight
-// gradients 1.78 ms (1235).  One library product of these sizes reaches 1335,
-// 1195 and 1059 TFLOP/s in the three forms.
+// Measured in bf16, 4096 <-> 16384 features and 8192 tokens (2.2 TFLOP each), one
+// pass after the other: forward 1.79 ms (1230 TFLOP/s; 2.12 with the 1.07 GB of
+// pre, which leave at the memory's rate while the next tile waits), gx 1.67 ms
+// (1315), both weight gradients 1.77 ms (1240).  A launch alone, before which the
+// device was idle: 2.23 with pre, 1.68 and 1.91.  One library product of these
+// sizes reaches 1335, 1195 and 1059 TFLOP/s in the three forms.
 #pragma once
 
 #include <type_traits>
@@ -291,7 +292,9 @@ __device__ __forceinline__ void put4(void* out, int64_t row, int64_t c, int64_t 
 
 // A barrier before which at most N of the wave's loads into LDS may still be
 // under way, and with STORES none of its LDS writes.  A fence would wait for
-// every load, as they write LDS; fragments being read stay in flight.
+// every load, as they write LDS; fragments being read stay in flight: with 64
+// products a stage none are (each has been used), with 32 the next stage's first
+// ones, which is written again one barrier later.
 template <int N, bool STORES>
 __device__ __forceinline__ void stage_barrier() {
   static_assert(N < 64, "vmcnt");

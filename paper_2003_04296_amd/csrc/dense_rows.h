@@ -10,14 +10,27 @@
 // one token: its work is far below its rate, and it spares the reduction over
 // lanes.  In its result a lane holds output lane % 16 and tokens
 // (lane / 16) * 4 + 0..3, so one scale per lane and group serves 4-bit weights.
-// Measured at 4096 x 4096 in 4 bits (9.4 MB): 4.1 us for one token (2.3 TB/s;
-// a kernel that reads the codes alone takes 3.3), 6.8 for 16, 9.6 for 32.
+// Measured at 4096 x 4096 in 4 bits (8.9 MB), one call after the other in a
+// graph, weights from the cache and from memory: one token 4.3 and 6.3 us (2.1
+// and 1.4 TB/s; a kernel that reads the codes alone takes 3.3 from the cache), 16
+// tokens 6.8 and 8.6, 32 10.4 and 11.7, 64 11.9 and 16.4.
 #pragma once
 
 #include "dense.h"
 #include "qconv_internal.h"
 
 namespace qc {
+
+// The most tokens that take this way; from the next on, products go through
+// tiles (dense_gemm.h).  us here and there in 4 bits, weights in the 256 MB cache:
+//   4096 -> 4096   13.7 and 20.6 at 64 tokens, 20.3 and 22.0 at 80
+//   4096 -> 16384  38.7 and 37.6, 70.1 and 38.1
+//   2048 -> 8192   13.7 and 16.5, 21.2 and 17.4
+//   8192 -> 1024   12.5 and 18.5, 17.2 and 18.9
+// In 16 bits (gated, weights of 300 MB in turn) the two meet earlier: 22.3 and
+// 24.2, 58 and 65, 18.0 and 23.4, 22.5 and 20.4 at 32 tokens, 28.2 and 25.6, 74
+// and 68, 23.0 and 24.8, 22.8 and 21.2 at 64.
+constexpr int ROWS_MOST = 64;
 
 struct RowsArgs {
   const uint16_t* x;
@@ -288,9 +301,10 @@ constexpr int FEW_MOST = 4;  // tokens they take
 // codes instead of up to four, and the scales take one fma per token.
 // x lies in LDS, PASS inputs at a time, and lanes that stand for no token read
 // zeros there: no load is conditional (a branch around them made the compiler
-// copy all operands).  Gated 4096 -> 16384 in groups of 32, in us: 17.6 for one
-// token and 21.5 for four, against 20.6 and 23 of a form like
-// dense_rows_kernel's; reading the codes alone takes 10.7.
+// copy all operands).  Gated 4096 -> 16384 in groups of 32, in us from the cache:
+// 17.6 for one token and 21.5 for four, against 20.6 and 23 of a form like
+// dense_rows_kernel's; reading the codes alone takes 10.7.  From memory 19.0 and
+// 23.9.
 template <class T, int GROUP, int H, int M, int NW>
 __global__ __launch_bounds__(NW * 64) void dense_few_kernel(RowsArgs a) {
   constexpr int PASS = 4096, LD = PASS + 8;  // + 8: the tokens' values in different banks

@@ -17,8 +17,11 @@ namespace {
 // dg and du of four hidden features per thread, into [m][2][fp] with the
 // columns past f zero (gx's products run over all fp of them).  They are
 // rounded to the tensors' type, once, because the matrix cores take 16-bit
-// operands; g and u themselves stay in fp32 between the passes.  Bound by HBM:
-// 8192 tokens of 16384 features read 1.3 GB and write 0.5 in 344 us, 5.5 TB/s.
+// operands; g and u themselves stay in fp32 between the passes.  The gradients'
+// error is 1.4 times that of fp32 factors (two roundings in place of one), and a
+// factor past fp16's 65504 is infinite, as a gradient of that type is.  Two parts
+// per factor would hold both and double the backward's products.  Bound by HBM:
+// 8192 tokens of 16384 features read 1.3 GB and write 0.5 in 352 us, 5.3 TB/s.
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void ffn_slopes_kernel(const float* __restrict__ pre, const uint16_t* __restrict__ gh,
                                                          int64_t ld_h, int m, int f, int fp,
@@ -90,11 +93,15 @@ int run_slopes(const qconv_ffn_desc& d, const float* pre, const void* gh, int fp
 
 }  // namespace
 
-constexpr int ROWS_MOST = 64;  // tokens that go through dense_rows.h
-
 // Copies of x and the weights in aligned rows, first in the workspace.  The
-// backward always makes them; the forward from as many tokens on as make up
-// for copying both weights (4095 -> 16384: 242 us against 119 at 100 tokens).
+// forward makes them from as many tokens on as make up for copying both weights
+// where these are large; us with copies and without:
+//   4095 -> 16384  238 and 114 at 100 tokens, 261 and 220 at 384, 351 and 441 at 800
+//   2047 -> 4001   36 and 36, 50 and 55, 61 and 78
+//   1001 -> 1000   25 and 32, 26 and 30, 26 and 37
+// The backward, which reads the weights down their columns, always does:
+//   4095 -> 8192   237 and 371 for one token, 296 and 621 for 200
+//   1001 -> 1000   33 and 62, 42 and 73
 constexpr int COPY_LEAST = 384;
 static size_t copies_bytes(const qconv_ffn_desc& d, bool forward) {
   if (forward && d.m < COPY_LEAST) return 0;

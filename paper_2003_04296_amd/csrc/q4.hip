@@ -35,7 +35,8 @@ __device__ __forceinline__ float load_value(const void* p, int64_t i) {
 }
 
 // Eight values of a group per thread, group / 8 neighbouring lanes a group.
-// Bound by reading w.
+// Once per weight: 16384 x 16384 values take 460 us in fp32 and 380 in 16 bits (2.6
+// and 1.8 TB/s), bound by the loads, one value each, that rows at any address allow.
 template <int DT>
 __global__ __launch_bounds__(256) void q4_pack_kernel(const void* __restrict__ w, int n, int k, int64_t ld, int group,
                                                       int kp, float top, uint32_t* __restrict__ codes,
@@ -114,8 +115,6 @@ int run_gemm_q4_group(GemmArgs& a, int group, int tile, bool aligned, hipStream_
   if (group == 64) return run_gemm_q4<T, OUT, 64>(a, tile, aligned, s);
   return run_gemm_q4<T, OUT, 128>(a, tile, aligned, s);
 }
-
-constexpr int ROWS_MOST = 64;  // tokens that go through dense_rows.h
 
 GemmPlan plan_q4(const qconv_q4_desc& d, bool gated, bool aligned) {
   return gemm_plan(d.m, d.n, d.k, 1, gated, aligned, false);

@@ -385,6 +385,83 @@ int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_co
                    size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Rows that go to different weights: tokens sorted by expert and back, the   */
+/* experts' products, and low-rank adapters of many requests.  Which rows     */
+/* belong to which weight is known to the device alone: offsets[groups + 1]   */
+/* (device, int32; rows offsets[g] .. offsets[g + 1] are group g's).  Nothing  */
+/* synchronises.  Whatever the device arrays hold, no call touches memory     */
+/* outside its tensors.                                                       */
+/* ------------------------------------------------------------------------ */
+
+/* The most groups (experts, adapters). */
+#define QCONV_MOE_GROUPS_MOST 4096
+
+/* ids[tokens][slots] (int32, or int64 with wide != 0; row stride ld): the
+ * group of each assignment i = token * slots + slot; an id outside [0, groups)
+ * drops it.  Writes
+ *   offsets[groups + 1]      : offsets[g] = assignments with an id below g (of those kept)
+ *   order[tokens * slots]    : the assignments by group, those of one group in
+ *                              their own order, the dropped ones last
+ *   place[tokens][slots]     : where order holds the assignment, -1 if dropped.
+ * tokens == 0 gives offsets of zero. */
+size_t qconv_moe_sort_bytes(int tokens, int slots, int groups);
+int qconv_moe_sort(const void* ids, int wide, int tokens, int slots, int64_t ld, int groups, int32_t* offsets,
+                   int32_t* order, int32_t* place, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int tokens, slots, width;
+  int dtype;                  /* qconv_dtype of the tokens' and the experts' rows */
+  int64_t ld_tokens, ld_rows; /* row strides */
+} qconv_moe_rows_desc;
+
+/* rows[place[t][s]] = x[t]; rows[tokens * slots][width].  Places outside
+ * [0, tokens * slots) are passed over, rows that no place names stay as they are
+ * (here and below).  A place is named once. */
+int qconv_moe_gather(const qconv_moe_rows_desc* d, const void* x, const int32_t* place, void* rows, void* stream);
+
+/* y[t] = sum_s weights[t][s] rows[place[t][s]] (weights fp32, NULL for ones:
+ * the gradient of the gather), summed in fp32 in the slots' order and rounded
+ * once; a dropped slot adds nothing, and its weight is not read. */
+int qconv_moe_combine(const qconv_moe_rows_desc* d, const void* rows, const int32_t* place, const float* weights,
+                      void* y, void* stream);
+
+/* From gy[tokens][width] (row stride ld_tokens) and the forward's inputs:
+ *   grows[place[t][s]] = weights[t][s] gy[t] (row stride ld_grows),
+ *   gweights[t][s] = sum over the width of gy[t] rows[place[t][s]] (fp32, 0 where dropped).
+ * grows or gweights may be NULL; rows is read for gweights alone. */
+int qconv_moe_combine_backward(const qconv_moe_rows_desc* d, const void* gy, const void* rows, const int32_t* place,
+                               const float* weights, void* grows, int64_t ld_grows, float* gweights, void* stream);
+
+typedef struct {
+  int rows, groups, k, f;   /* rows of all groups, groups, inputs, outputs (hidden features) */
+  int dtype;                /* QCONV_F16 or QCONV_BF16: every tensor but pre */
+  int act;                  /* qconv_act (gated products)                    */
+  int64_t ld_x, ld_w, ld_h; /* row strides of x, of the weights, of h and gh */
+} qconv_moe_desc;
+
+/* The experts' products.  x[rows][k]; weights [groups][f][k], one group's rows
+ * right after the other's (row (g, i) at w + (g * f + i) * ld_w).  Rows of no
+ * group are not read and their results not written.  Otherwise as
+ * qconv_ffn_forward and qconv_ffn_backward for each group: pre is
+ * [rows][2][fp] (qconv_ffn_pre_floats(rows, f)), gx and the weight gradients
+ * [groups][f][k] are contiguous, those of a group without rows zero. */
+size_t qconv_moe_forward_bytes(const qconv_moe_desc* d, int gated);
+int qconv_moe_gated_forward(const qconv_moe_desc* d, const void* x, const void* w_gate, const void* w_up,
+                            const int32_t* offsets, void* h, float* pre, void* workspace, size_t workspace_bytes,
+                            void* stream);
+/* y = x w^T for each group's rows. */
+int qconv_moe_linear_forward(const qconv_moe_desc* d, const void* x, const void* w, const int32_t* offsets, void* y,
+                             void* workspace, size_t workspace_bytes, void* stream);
+size_t qconv_moe_backward_bytes(const qconv_moe_desc* d, int gated);
+int qconv_moe_gated_backward(const qconv_moe_desc* d, const void* x, const void* w_gate, const void* w_up,
+                             const int32_t* offsets, const float* pre, const void* gh, void* gx, void* gw_gate,
+                             void* gw_up, void* workspace, size_t workspace_bytes, void* stream);
+/* gx = gy w, gw = gy^T x for each group's rows; gx or gw may be NULL. */
+int qconv_moe_linear_backward(const qconv_moe_desc* d, const void* x, const void* w, const int32_t* offsets,
+                              const void* gy, void* gx, void* gw, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* The norm over all gradients of a model, and clipping by it                */
 /* ------------------------------------------------------------------------ */
 

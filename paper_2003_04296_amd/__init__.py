@@ -39,6 +39,9 @@ EXPORTED = (
     "qconv_ffn_pre_floats", "qconv_ffn_forward_bytes", "qconv_ffn_forward", "qconv_ffn_backward_bytes", "qconv_ffn_backward",
     "qconv_q4_code_bytes", "qconv_q4_scale_bytes", "qconv_q4_pack", "qconv_q4_workspace_bytes", "qconv_q4_linear",
     "qconv_q4_gated", "aqe_grad_norm_bytes", "aqe_grad_norm", "aqe_clip_grads",
+    "qconv_moe_sort_bytes", "qconv_moe_sort", "qconv_moe_gather", "qconv_moe_combine", "qconv_moe_combine_backward",
+    "qconv_moe_forward_bytes", "qconv_moe_gated_forward", "qconv_moe_linear_forward", "qconv_moe_backward_bytes",
+    "qconv_moe_gated_backward", "qconv_moe_linear_backward",
 )
 
 
@@ -68,6 +71,16 @@ class qconv_ffn_desc(ctypes.Structure):
 class qconv_q4_desc(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int) for name in ("m", "n", "k", "group", "dtype")] + \
                [(name, ctypes.c_int64) for name in ("ld_x", "ld_y")]
+
+
+class qconv_moe_rows_desc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("tokens", "slots", "width", "dtype")] + \
+               [(name, ctypes.c_int64) for name in ("ld_tokens", "ld_rows")]
+
+
+class qconv_moe_desc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("rows", "groups", "k", "f", "dtype", "act")] + \
+               [(name, ctypes.c_int64) for name in ("ld_x", "ld_w", "ld_h")]
 
 
 _lib = None
@@ -126,6 +139,20 @@ def lib() -> ctypes.CDLL:
     L.qconv_q4_workspace_bytes.argtypes = [q4, i32]
     L.qconv_q4_linear.argtypes = [q4] + [vp] * 6 + [sz, vp]
     L.qconv_q4_gated.argtypes = [q4] + [vp] * 5 + [i32] + [vp] * 2 + [sz, vp]
+    L.qconv_moe_sort_bytes.restype = sz
+    L.qconv_moe_sort_bytes.argtypes = [i32] * 3
+    L.qconv_moe_sort.argtypes = [vp] + [i32] * 3 + [i64, i32] + [vp] * 4 + [sz, vp]
+    rows = moe = vp
+    L.qconv_moe_gather.argtypes = [rows] + [vp] * 4
+    L.qconv_moe_combine.argtypes = [rows] + [vp] * 5
+    L.qconv_moe_combine_backward.argtypes = [rows] + [vp] * 5 + [i64, vp, vp]
+    for gated in (L.qconv_moe_forward_bytes, L.qconv_moe_backward_bytes):
+        gated.restype = sz
+        gated.argtypes = [moe, i32]
+    L.qconv_moe_gated_forward.argtypes = [moe] + [vp] * 7 + [sz, vp]
+    L.qconv_moe_linear_forward.argtypes = [moe] + [vp] * 5 + [sz, vp]
+    L.qconv_moe_gated_backward.argtypes = [moe] + [vp] * 10 + [sz, vp]
+    L.qconv_moe_linear_backward.argtypes = [moe] + [vp] * 7 + [sz, vp]
     L.aqe_grad_norm_bytes.restype = sz
     L.aqe_grad_norm_bytes.argtypes = [i32, vp]
     L.aqe_grad_norm.argtypes = [i32] + [vp] * 5 + [sz, vp]
@@ -549,6 +576,251 @@ def q4_gated(x, gate_codes, gate_scales, up_codes, up_scales, act: int = ACT_SIL
                             up_scales.data_ptr(), act, y.data_ptr(), _ptr(ws), nbytes, _stream(stream)),
            "qconv_q4_gated")
     return y
+
+
+# ---------------------------------------------------------------------------
+# Rows that go to different weights: tokens sorted by expert and back, the
+# experts' products, adapters of many requests.  Which rows belong to which
+# weight stays on the device (offsets); no call waits for it.
+# ---------------------------------------------------------------------------
+
+_ROWS_DESC = struct.Struct("4i2q")
+_MOE_DESC = struct.Struct("6i3q")
+
+
+def _indices(t, like, what: str, numel=None):
+    """An index tensor: contiguous int32 on the device of `like`."""
+    import torch
+
+    if t.dtype is not torch.int32 or t.get_device() != like.get_device() or not t.is_contiguous() or \
+            (numel is not None and t.numel() != numel):
+        raise ValueError(f"{what}: contiguous int32{'' if numel is None else f' of {numel} values'} on {like.device}")
+    return t
+
+
+def moe_sort(ids, groups: int, out=None, workspace=None, stream=None):
+    """The order that brings the rows of each group together.  ids [tokens] or
+    [tokens][slots], int32 or int64: an assignment's group (expert, adapter), or
+    a value outside [0, groups) for none -> int32 (offsets [groups + 1]: where
+    each group's rows start; order [tokens * slots]: the assignments by group,
+    stably, those of none last; place, of ids' shape: an assignment's row, -1 for
+    none).  groups is at most 4096."""
+    import torch
+
+    _on_gpu(ids, "moe_sort", stream)
+    if ids.dim() not in (1, 2) or ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError("moe_sort: ids are int32 or int64, [tokens] or [tokens][slots]")
+    tokens, slots = ids.shape if ids.dim() == 2 else (ids.shape[0], 1)
+    if slots < 1:
+        raise ValueError("moe_sort: ids have at least one slot")
+    if ids.dim() == 2:
+        ld = _ld(ids, (tokens, slots), "moe_sort")
+    else:
+        ld = ids.stride(0) if tokens > 1 else 1
+        if ld < 1:
+            raise ValueError("moe_sort: ids share memory")
+    n = _int(tokens * slots)
+    shapes = (groups + 1,), (n,), tuple(ids.shape)
+    if out is None:
+        if groups < 1:
+            raise QconvError(QCONV_EINVAL, "moe_sort")
+        out = tuple(_new(s, torch.int32, ids, stream) for s in shapes)
+    elif any(tuple(_indices(t, ids, "moe_sort out").shape) != s for t, s in zip(out, shapes, strict=True)):
+        raise ValueError(f"moe_sort: out has the shapes {shapes}")
+    offsets, order, place = out
+    L = lib()
+    ws, nbytes = _workspace(workspace, L.qconv_moe_sort_bytes(tokens, slots, groups), ids, "moe_sort", stream)
+    _check(L.qconv_moe_sort(ids.data_ptr(), ids.dtype is torch.int64, tokens, slots, ld, groups, offsets.data_ptr(),
+                            order.data_ptr(), place.data_ptr(), _ptr(ws), nbytes, _stream(stream)), "qconv_moe_sort")
+    return offsets, order, place
+
+
+def _place(place, tokens, like, what):
+    """(slots, place's address)."""
+    if place.dim() not in (1, 2) or place.shape[0] != tokens:
+        raise ValueError(f"{what}: place is [{tokens}] or [{tokens}][slots], got {tuple(place.shape)}")
+    _indices(place, like, what + " place")
+    return place.shape[1] if place.dim() == 2 else 1
+
+
+def _weights(weights, place, like, what):
+    import torch
+
+    if weights is not None and (weights.dtype is not torch.float32 or weights.shape != place.shape or
+                                weights.get_device() != like.get_device() or not weights.is_contiguous()):
+        raise ValueError(f"{what}: weights are contiguous fp32 of place's shape on {like.device}")
+    return _ptr(weights)
+
+
+def _matrix(t, what, stream):
+    if t.dim() != 2:
+        raise ValueError(f"{what}: a matrix, got {tuple(t.shape)}")
+    _on_gpu(t, what, stream)
+    return t.shape
+
+
+def moe_gather(x, place, out=None, stream=None):
+    """rows [tokens * slots][width] of x [tokens][width] by place (moe_sort):
+    rows[place[t][s]] = x[t].  fp32 or 16-bit; rows that no place names are left
+    as they are."""
+    tokens, width = _matrix(x, "moe_gather", stream)
+    slots = _place(place, tokens, x, "moe_gather")
+    n = tokens * slots
+    ld = width if out is None else _rows(out, n, width, x, "moe_gather out")
+    d = _ROWS_DESC.pack(_int(tokens), _int(slots), _int(width), _dtypes[x.dtype], _ld(x, (tokens, width), "moe_gather"), ld)
+    rows = _new((n, width), x.dtype, x, stream) if out is None else out
+    _check(lib().qconv_moe_gather(d, x.data_ptr(), place.data_ptr(), rows.data_ptr(), _stream(stream)),
+           "qconv_moe_gather")
+    return rows
+
+
+def moe_combine(rows, place, weights=None, out=None, stream=None):
+    """y [tokens][width] = the rows of each token's slots times weights (fp32 of
+    place's shape; None: ones), summed in fp32 and rounded once."""
+    n, width = _matrix(rows, "moe_combine", stream)
+    tokens = place.shape[0] if place.dim() else 0
+    slots = _place(place, tokens, rows, "moe_combine")
+    if n != tokens * slots:
+        raise ValueError(f"moe_combine: {n} rows for {tokens} x {slots} places")
+    w = _weights(weights, place, rows, "moe_combine")
+    ld = width if out is None else _rows(out, tokens, width, rows, "moe_combine out")
+    d = _ROWS_DESC.pack(_int(tokens), _int(slots), _int(width), _dtypes[rows.dtype], ld, _ld(rows, (n, width), "moe_combine"))
+    y = _new((tokens, width), rows.dtype, rows, stream) if out is None else out
+    _check(lib().qconv_moe_combine(d, rows.data_ptr(), place.data_ptr(), w, y.data_ptr(), _stream(stream)),
+           "qconv_moe_combine")
+    return y
+
+
+def moe_gather_backward(grows, place, out=None, stream=None):
+    """The gradient of moe_gather's x: each token's rows of grows, summed."""
+    return moe_combine(grows, place, None, out, stream)
+
+
+def moe_combine_backward(gy, rows, place, weights=None, need_rows: bool = True, need_w: bool = True, out=None,
+                         stream=None):
+    """From gy [tokens][width] -> (the gradient of moe_combine's rows, of its
+    weights: fp32 of place's shape); None for what need_rows / need_w leave out.
+    Gradients of rows that no place names are left as they are.  out: tensors (or
+    None) to write instead of new ones."""
+    import torch
+
+    tokens, width = _matrix(gy, "moe_combine_backward", stream)
+    slots = _place(place, tokens, gy, "moe_combine_backward")
+    n = tokens * slots
+    ld_rows = _rows(rows, n, width, gy, "moe_combine_backward rows")
+    w = _weights(weights, place, gy, "moe_combine_backward")
+    grows, gw = out if out is not None else (None, None)
+    ld = width if grows is None else _rows(grows, n, width, gy, "moe_combine_backward out")
+    if gw is not None:
+        _weights(gw, place, gy, "moe_combine_backward out")
+    d = _ROWS_DESC.pack(_int(tokens), _int(slots), _int(width), _dtypes[gy.dtype],
+                        _ld(gy, (tokens, width), "moe_combine_backward"), ld_rows)
+    grows = (_new((n, width), gy.dtype, gy, stream) if grows is None else grows) if need_rows else None
+    gw = (_new(place.shape, torch.float32, gy, stream) if gw is None else gw) if need_w else None
+    _check(lib().qconv_moe_combine_backward(d, gy.data_ptr(), rows.data_ptr(), place.data_ptr(), w, _ptr(grows), ld,
+                                            _ptr(gw), _stream(stream)), "qconv_moe_combine_backward")
+    return grows, gw
+
+
+def _expert_weights(w, k, like, what):
+    """(groups, f, row stride) of weights [groups][f][k], one group's rows right after the other's."""
+    s = w.shape
+    if len(s) != 3 or s[2] != k or w.dtype is not like.dtype or w.get_device() != like.get_device():
+        raise ValueError(f"{what}: weights are [groups][f][{k}] {like.dtype} on {like.device}, got {tuple(s)} {w.dtype}")
+    step, ld, unit = w.stride()
+    groups, f = s[0], s[1]
+    if f == 1 and groups > 1:
+        ld = step  # one row a group
+    elif f <= 1:
+        ld = k
+    if (unit != 1 and k > 1) or ld < k or (groups > 1 and step != f * ld):
+        raise ValueError(f"{what}: columns are contiguous and one group's rows follow the other's (strides {w.stride()})")
+    return groups, f, ld
+
+
+def _moe_args(x, ws, offsets, act, what, stream, out):
+    """(rows, k, groups, f, descriptor) of an experts' product; out: [rows][f] or None."""
+    rows, k = _matrix(x, what, stream)
+    groups, f, ld_w = _expert_weights(ws[0], k, x, what)
+    if len(ws) == 2 and (_expert_weights(ws[1], k, x, what) != (groups, f, ld_w)):
+        raise ValueError(f"{what}: w_gate and w_up have different shapes or strides")
+    _indices(offsets, x, what + " offsets", groups + 1)
+    ld_h = f if out is None else _rows(out, rows, f, x, what)
+    return rows, k, groups, f, _MOE_DESC.pack(_int(rows), groups, _int(k), _int(f), _dtypes[x.dtype], act,
+                                              _ld(x, (rows, k), what), ld_w, ld_h)
+
+
+def moe_gated_forward(x, w_gate, w_up, offsets, act: int = ACT_SILU, keep_pre: bool = False, pre=None, out=None,
+                      workspace=None, stream=None):
+    """ffn_forward with the weights [groups][f][k] of each row's group: rows
+    offsets[g] .. offsets[g + 1] of x [rows][k] are group g's -> (h [rows][f],
+    pre).  Rows of no group are left as they are."""
+    rows, k, groups, f, d = _moe_args(x, (w_gate, w_up), offsets, act, "moe_gated_forward", stream, out)
+    L = lib()
+    h = _new((rows, f), x.dtype, x, stream) if out is None else out
+    if pre is not None:
+        _check_pre(pre, rows, f, x, "moe_gated_forward")
+    elif keep_pre:
+        import torch
+
+        pre = _new((L.qconv_ffn_pre_floats(rows, f),), torch.float32, x, stream)
+    ws, nbytes = _workspace(workspace, L.qconv_moe_forward_bytes(d, 1), x, "moe_gated_forward", stream)
+    _check(L.qconv_moe_gated_forward(d, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), offsets.data_ptr(),
+                                     h.data_ptr(), _ptr(pre), _ptr(ws), nbytes, _stream(stream)),
+           "qconv_moe_gated_forward")
+    return h, pre
+
+
+def moe_linear_forward(x, w, offsets, out=None, workspace=None, stream=None):
+    """y [rows][f] = x w_g^T with the weights [groups][f][k] of each row's group."""
+    rows, k, groups, f, d = _moe_args(x, (w,), offsets, 0, "moe_linear_forward", stream, out)
+    L = lib()
+    y = _new((rows, f), x.dtype, x, stream) if out is None else out
+    ws, nbytes = _workspace(workspace, L.qconv_moe_forward_bytes(d, 0), x, "moe_linear_forward", stream)
+    _check(L.qconv_moe_linear_forward(d, x.data_ptr(), w.data_ptr(), offsets.data_ptr(), y.data_ptr(), _ptr(ws), nbytes,
+                                      _stream(stream)), "qconv_moe_linear_forward")
+    return y
+
+
+def _grad_outs(out, shapes, needs, like, what, stream):
+    """The gradients to write: those of `out` (contiguous) or new ones, None where not needed."""
+    out = (None,) * len(shapes) if out is None else out
+    for t, s in zip(out, shapes, strict=True):
+        if t is not None and (tuple(t.shape) != s or t.dtype is not like.dtype or not t.is_contiguous() or
+                              t.get_device() != like.get_device()):
+            raise ValueError(f"{what}: out tensors are contiguous {like.dtype} on {like.device}, of the shapes {shapes}")
+    return [(_new(s, like.dtype, like, stream) if t is None else t) if need else None
+            for t, s, need in zip(out, shapes, needs)]
+
+
+def moe_gated_backward(x, w_gate, w_up, offsets, pre, gh, act: int = ACT_SILU, need_x: bool = True, need_w: bool = True,
+                       out=None, workspace=None, stream=None):
+    """From gh [rows][f] and the forward's pre -> (gx [rows][k], gw_gate and
+    gw_up [groups][f][k]) in x's type; None for what need_x / need_w leave out.
+    out: contiguous tensors (or None) to write instead of new ones.  Rows of no
+    group are left as they are, weights of no row get zeros."""
+    rows, k, groups, f, d = _moe_args(x, (w_gate, w_up), offsets, act, "moe_gated_backward", stream, gh)
+    _check_pre(pre, rows, f, x, "moe_gated_backward")
+    gx, gg, gu = _grad_outs(out, ((rows, k), (groups, f, k), (groups, f, k)), (need_x, need_w, need_w), x,
+                            "moe_gated_backward", stream)
+    L = lib()
+    ws, nbytes = _workspace(workspace, L.qconv_moe_backward_bytes(d, 1), x, "moe_gated_backward", stream)
+    _check(L.qconv_moe_gated_backward(d, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), offsets.data_ptr(),
+                                      pre.data_ptr(), gh.data_ptr(), _ptr(gx), _ptr(gg), _ptr(gu), _ptr(ws), nbytes,
+                                      _stream(stream)), "qconv_moe_gated_backward")
+    return gx, gg, gu
+
+
+def moe_linear_backward(x, w, offsets, gy, need_x: bool = True, need_w: bool = True, out=None, workspace=None,
+                        stream=None):
+    """From gy [rows][f] -> (gx [rows][k], gw [groups][f][k]), as moe_gated_backward."""
+    rows, k, groups, f, d = _moe_args(x, (w,), offsets, 0, "moe_linear_backward", stream, gy)
+    gx, gw = _grad_outs(out, ((rows, k), (groups, f, k)), (need_x, need_w), x, "moe_linear_backward", stream)
+    L = lib()
+    ws, nbytes = _workspace(workspace, L.qconv_moe_backward_bytes(d, 0), x, "moe_linear_backward", stream)
+    _check(L.qconv_moe_linear_backward(d, x.data_ptr(), w.data_ptr(), offsets.data_ptr(), gy.data_ptr(), _ptr(gx),
+                                       _ptr(gw), _ptr(ws), nbytes, _stream(stream)), "qconv_moe_linear_backward")
+    return gx, gw
 
 
 def _dense(t) -> bool:

@@ -524,22 +524,29 @@ __device__ __forceinline__ void multiply_groups(v4f (&sums)[H][NR], const GemmAr
   }
 }
 
+// Which tile of C a block takes: its row and column tile, numbered over both halves.
+struct TileAt {
+  uint32_t r, c;
+};
+// Workgroups go to the 8 dies in turn; each die gets a run of tiles that share
+// operands in its L2: 8 tile rows at a time, column after column.
+__device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t rows, uint32_t cols) {
+  const uint32_t all = rows * cols, group = 8 * cols, die = id & 7;
+  const uint32_t tile = die * (all / 8) + (die < all % 8 ? die : all % 8) + id / 8;
+  const uint32_t first = tile / group * 8, some = rows - first < 8 ? rows - first : 8;
+  return {first + tile % group % some, tile % group / some};
+}
+
+// The products of part `part` of a.parts of one tile.
 template <class T, class SR, class SC, int OUT, int BR, int BC>
-__device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds) {
+__device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds, const TileAt at, uint32_t part) {
   constexpr int KS = SR::KS, NR = BR / 32, PAIR = OUT == OUT_GATED;
   constexpr int LR = BR * SR::CPR, LC = BC * SR::CPR, STAGE = LR + LC, CHUNKS = SR::CH + SC::CH;
   constexpr int LOADS = (SR::DIRECT ? SR::CH : 0) + (SC::DIRECT ? SC::CH : 0);  // into LDS, per stage and thread
   constexpr bool REGS = !SR::DIRECT || !SC::DIRECT;                             // some pass through registers
-  // Workgroups go to the 8 dies in turn; each die gets a run of tiles that
-  // share operands in its L2: 8 tile rows at a time, column after column.
-  const uint32_t trs = a.tiles_r * a.halves, all = trs * a.tiles_c, group = 8 * a.tiles_c;
-  const uint32_t id = blockIdx.x % all, part = blockIdx.x / all, die = id & 7;
-  const uint32_t tile = die * (all / 8) + (die < all % 8 ? die : all % 8) + id / 8;
-  const uint32_t first = tile / group * 8, some = trs - first < 8 ? trs - first : 8;
-  const uint32_t tr = first + tile % group % some, tc = tile % group / some;
-  const int half = tr >= (uint32_t)a.tiles_r;
-  const int64_t r0 = (int64_t)(tr - half * a.tiles_r) * BR;
-  const int64_t c0 = (int64_t)tc * (PAIR ? BC / 2 : BC);
+  const int half = at.r >= (uint32_t)a.tiles_r;
+  const int64_t r0 = (int64_t)(at.r - half * a.tiles_r) * BR;
+  const int64_t c0 = (int64_t)at.c * (PAIR ? BC / 2 : BC);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
   const int wr = (wave & 1) * (BR / 2), wc = (wave >> 1) * 64;
   v4f acc[4][NR];  // [column group][row group]: lane holds row lane % 16, columns (lane / 16) * 4 + 0..3
@@ -720,7 +727,8 @@ __global__ __launch_bounds__(BC / 64 * 128) void dense_gemm_kernel(GemmArgs a) {
   static_assert(SR::KS == SC::KS, "one ring");
   [[maybe_unused]] __shared__ v4u lds[STAGES<SR::KS> * (BR + BC) * SR::CPR];
 #ifdef __HIP_DEVICE_COMPILE__  // the host has no LDS pointers
-  gemm_tile<T, SR, SC, OUT, BR, BC>(a, (lds_v4u*)lds);
+  const uint32_t rows = a.tiles_r * a.halves, all = rows * a.tiles_c;
+  gemm_tile<T, SR, SC, OUT, BR, BC>(a, (lds_v4u*)lds, tile_at(blockIdx.x % all, rows, a.tiles_c), blockIdx.x / all);
 #endif
 }
 

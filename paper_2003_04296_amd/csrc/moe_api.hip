@@ -1,0 +1,168 @@
+// moe_api.hip -- the C ABI of the operators for rows that go to different
+// weights (include/qconv.h): argument validation only.  Nothing here allocates or
+// synchronises; every launch goes to the caller's stream.
+#include "dense.h"
+#include "moe.h"
+
+using namespace qc;
+
+namespace {
+
+bool half_type(int t) { return t == QCONV_F16 || t == QCONV_BF16; }
+bool any_type(int t) { return t >= QCONV_F32 && t <= QCONV_BF16; }
+bool at(const void* p, uintptr_t align) { return ((uintptr_t)p & (align - 1)) == 0; }
+constexpr int64_t MAX_LD = (int64_t)1 << 40;
+constexpr int MOST = 0x7fffff00;  // padded sizes of every kind stay inside an int
+
+static_assert(QCONV_MOE_GROUPS_MOST == MOE_GROUPS_MOST, "one limit");
+
+int check_groups(int groups) {
+  if (groups < 1) return QCONV_EINVAL;
+  return groups > MOE_GROUPS_MOST ? QCONV_EUNSUPPORTED : QCONV_OK;
+}
+
+int check_sort(int tokens, int slots, int groups) {
+  if (tokens < 0 || slots < 1) return QCONV_EINVAL;
+  if ((int64_t)tokens * slots > MOST) return QCONV_EUNSUPPORTED;
+  return check_groups(groups);
+}
+
+int check_rows(const qconv_moe_rows_desc* d) {
+  if (!d || d->tokens < 0 || d->slots < 1 || d->width < 1 || !any_type(d->dtype) || d->ld_tokens < d->width ||
+      d->ld_rows < d->width || d->ld_tokens > MAX_LD || d->ld_rows > MAX_LD)
+    return QCONV_EINVAL;
+  if ((int64_t)d->tokens * d->slots > MOST || d->width > MOST) return QCONV_EUNSUPPORTED;
+  return QCONV_OK;
+}
+
+int check_moe(const qconv_moe_desc* d) {
+  if (!d || d->rows < 0 || d->k < 1 || d->f < 1 || d->act < QCONV_ACT_SILU || d->act > QCONV_ACT_RELU ||
+      !any_type(d->dtype) || d->ld_x < d->k || d->ld_w < d->k || d->ld_h < d->f || d->ld_x > MAX_LD ||
+      d->ld_w > MAX_LD || d->ld_h > MAX_LD)
+    return QCONV_EINVAL;
+  const int rc = check_groups(d->groups);
+  if (rc) return rc;
+  if (!half_type(d->dtype) || d->rows > MOST || d->k > MOST || d->f > 0x3fffff00) return QCONV_EUNSUPPORTED;
+  return QCONV_OK;
+}
+
+// What both forms of the experts' products have in common.
+int check_forward(const qconv_moe_desc* d, bool gated, const void* x, const void* w, const int32_t* offsets,
+                  const void* h, const void* workspace, size_t workspace_bytes) {
+  if (!w || !offsets || (d->rows > 0 && (!x || !h)) || !at(x, 2) || !at(w, 2) || !at(h, 2) || !at(offsets, 4) ||
+      !at(workspace, 16))
+    return QCONV_EINVAL;
+  const size_t need = moe_forward_bytes(*d, gated);
+  if (need && !workspace) return QCONV_EINVAL;
+  return workspace_bytes < need ? QCONV_EWORKSPACE : QCONV_OK;
+}
+int check_backward(const qconv_moe_desc* d, bool gated, const void* x, const void* w, const int32_t* offsets,
+                   const void* gh, const void* gx, const void* gw, const void* workspace, size_t workspace_bytes) {
+  if (!w || !offsets || (d->rows > 0 && (!x || !gh)) || !at(x, 2) || !at(w, 2) || !at(gh, 2) || !at(gx, 2) ||
+      !at(gw, 2) || !at(offsets, 4) || !at(workspace, 16))
+    return QCONV_EINVAL;
+  const size_t need = moe_backward_bytes(*d, gated);
+  if (need && !workspace) return QCONV_EINVAL;
+  return workspace_bytes < need ? QCONV_EWORKSPACE : QCONV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t qconv_moe_sort_bytes(int tokens, int slots, int groups) {
+  return check_sort(tokens, slots, groups) ? 0 : moe_sort_bytes(tokens * slots, groups);
+}
+
+int qconv_moe_sort(const void* ids, int wide, int tokens, int slots, int64_t ld, int groups, int32_t* offsets,
+                   int32_t* order, int32_t* place, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_sort(tokens, slots, groups);
+  if (rc) return rc;
+  if (!offsets || (tokens > 0 && (!ids || !order || !place)) || ld < slots || ld > MAX_LD || !at(ids, wide ? 8 : 4) ||
+      !at(offsets, 4) || !at(order, 4) || !at(place, 4) || !at(workspace, 16))
+    return QCONV_EINVAL;
+  const size_t need = moe_sort_bytes(tokens * slots, groups);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  return launch_moe_sort(ids, wide != 0, tokens, slots, ld, groups, offsets, order, place, workspace,
+                         (hipStream_t)stream);
+}
+
+int qconv_moe_gather(const qconv_moe_rows_desc* d, const void* x, const int32_t* place, void* rows, void* stream) {
+  const int rc = check_rows(d);
+  if (rc) return rc;
+  const int a = d->dtype == QCONV_F32 ? 4 : 2;
+  if ((d->tokens > 0 && (!x || !place || !rows)) || !at(x, a) || !at(rows, a) || !at(place, 4)) return QCONV_EINVAL;
+  return launch_moe_gather(*d, x, place, rows, (hipStream_t)stream);
+}
+
+int qconv_moe_combine(const qconv_moe_rows_desc* d, const void* rows, const int32_t* place, const float* weights,
+                      void* y, void* stream) {
+  const int rc = check_rows(d);
+  if (rc) return rc;
+  const int a = d->dtype == QCONV_F32 ? 4 : 2;
+  if ((d->tokens > 0 && (!rows || !place || !y)) || !at(rows, a) || !at(y, a) || !at(place, 4) || !at(weights, 4))
+    return QCONV_EINVAL;
+  return launch_moe_combine(*d, rows, place, weights, y, (hipStream_t)stream);
+}
+
+int qconv_moe_combine_backward(const qconv_moe_rows_desc* d, const void* gy, const void* rows, const int32_t* place,
+                               const float* weights, void* grows, int64_t ld_grows, float* gweights, void* stream) {
+  const int rc = check_rows(d);
+  if (rc) return rc;
+  const int a = d->dtype == QCONV_F32 ? 4 : 2;
+  if ((d->tokens > 0 && (!gy || !place || (gweights && !rows))) || (grows && (ld_grows < d->width || ld_grows > MAX_LD)) ||
+      !at(gy, a) || !at(rows, a) || !at(grows, a) || !at(place, 4) || !at(weights, 4) || !at(gweights, 4))
+    return QCONV_EINVAL;
+  return launch_moe_combine_back(*d, gy, rows, place, weights, grows, ld_grows, gweights, (hipStream_t)stream);
+}
+
+size_t qconv_moe_forward_bytes(const qconv_moe_desc* d, int gated) {
+  return check_moe(d) ? 0 : moe_forward_bytes(*d, gated != 0);
+}
+
+int qconv_moe_gated_forward(const qconv_moe_desc* d, const void* x, const void* w_gate, const void* w_up,
+                            const int32_t* offsets, void* h, float* pre, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  int rc = check_moe(d);
+  if (rc) return rc;
+  if (!w_up || !at(w_up, 2) || !at(pre, 16)) return QCONV_EINVAL;
+  rc = check_forward(d, true, x, w_gate, offsets, h, workspace, workspace_bytes);
+  return rc ? rc : launch_moe_forward(*d, x, w_gate, w_up, offsets, h, pre, workspace, (hipStream_t)stream);
+}
+
+int qconv_moe_linear_forward(const qconv_moe_desc* d, const void* x, const void* w, const int32_t* offsets, void* y,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_moe(d);
+  if (rc) return rc;
+  rc = check_forward(d, false, x, w, offsets, y, workspace, workspace_bytes);
+  return rc ? rc : launch_moe_forward(*d, x, w, nullptr, offsets, y, nullptr, workspace, (hipStream_t)stream);
+}
+
+size_t qconv_moe_backward_bytes(const qconv_moe_desc* d, int gated) {
+  return check_moe(d) ? 0 : moe_backward_bytes(*d, gated != 0);
+}
+
+int qconv_moe_gated_backward(const qconv_moe_desc* d, const void* x, const void* w_gate, const void* w_up,
+                             const int32_t* offsets, const float* pre, const void* gh, void* gx, void* gw_gate,
+                             void* gw_up, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_moe(d);
+  if (rc) return rc;
+  if (!w_up || (d->rows > 0 && !pre) || !gw_gate != !gw_up || !at(w_up, 2) || !at(gw_up, 2) || !at(pre, 16))
+    return QCONV_EINVAL;
+  rc = check_backward(d, true, x, w_gate, offsets, gh, gx, gw_gate, workspace, workspace_bytes);
+  return rc ? rc : launch_moe_backward(*d, x, w_gate, w_up, offsets, pre, gh, gx, gw_gate, gw_up, workspace,
+                                       (hipStream_t)stream);
+}
+
+int qconv_moe_linear_backward(const qconv_moe_desc* d, const void* x, const void* w, const int32_t* offsets,
+                              const void* gy, void* gx, void* gw, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  int rc = check_moe(d);
+  if (rc) return rc;
+  rc = check_backward(d, false, x, w, offsets, gy, gx, gw, workspace, workspace_bytes);
+  return rc ? rc : launch_moe_backward(*d, x, w, nullptr, offsets, nullptr, gy, gx, gw, nullptr, workspace,
+                                       (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,74 @@
+// moe_groups.h -- which rows of a batch belong to which weight: offsets[g] ..
+// offsets[g + 1] are the rows of group g, known to the device alone.
+#pragma once
+
+#include "dense.h"
+
+namespace qc {
+
+struct Groups {
+  const int* offsets;  // [n + 1]
+  int n;
+  int rows;  // rows there are: whatever offsets says, none past them are touched
+};
+
+struct GroupRows {
+  int first, count;
+};
+__device__ __forceinline__ GroupRows group_rows(const Groups& g, int e) {
+  const int lo = g.offsets[e], hi = g.offsets[e + 1];
+  const int first = lo < 0 ? 0 : lo < g.rows ? lo : g.rows, last = hi < g.rows ? hi : g.rows;
+  return {first, last > first ? last - first : 0};
+}
+
+// Inclusive sums over the wave's lanes.
+__device__ __forceinline__ int wave_sums(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+// The pieces of `size` rows that the groups' rows fall into, numbered group
+// after group: the host, which does not know the offsets, launches most() of them
+// and a block looks its piece up by itself (each wave; a load and a sum over the
+// lanes for every 64 groups, about 1 us).
+struct GroupPieces {
+  static int64_t most(int rows, int groups, int size) { return rows / size + (groups < rows ? groups : rows); }
+
+  int size, per;  // groups per lane
+  int upto;       // pieces of the groups up to and with this lane's
+  int total;
+
+  __device__ __forceinline__ int of(const Groups& g, int e) const {
+    return e < g.n ? (group_rows(g, e).count + size - 1) / size : 0;
+  }
+  __device__ __forceinline__ GroupPieces(const Groups& g, int size_) : size(size_) {
+    const int lane = threadIdx.x & 63;
+    per = (g.n + 63) / 64;
+    int mine = 0;
+    for (int i = 0; i < per; ++i) mine += of(g, lane * per + i);
+    upto = wave_sums(mine);
+    total = __builtin_amdgcn_readlane(upto, 63);
+  }
+  // The group of piece p < total, and the piece's number in it.
+  __device__ __forceinline__ void find(const Groups& g, int p, int& group, int& piece) const {
+    const int lane = threadIdx.x & 63;
+    int l = __popcll(__ballot(upto <= p));
+    int before = l ? __builtin_amdgcn_readlane(upto, l - 1) : 0;
+    group = l;
+    if (per > 1) {  // at most 64 groups of that lane's, one in each
+      const int e = l * per + lane, sums = wave_sums(lane < per ? of(g, e) : 0);
+      const int in = __popcll(__ballot(before + sums <= p));
+      before += in ? __builtin_amdgcn_readlane(sums, in - 1) : 0;
+      group = l * per + in;
+    }
+    group = __builtin_amdgcn_readfirstlane(group);
+    piece = __builtin_amdgcn_readfirstlane(p - before);
+  }
+};
+
+}  // namespace qc

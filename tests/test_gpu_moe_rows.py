@@ -1,0 +1,247 @@
+"""Rows sorted by group and back (moe_sort, moe_gather, moe_combine and their
+gradients) against their definitions (run with -m gpu).
+
+moe_sort and moe_gather are exact.  Bounds of the others, with u half a step of
+the tensors' type (2^-11 fp16, 2^-8 bf16, 2^-24 fp32; half the smallest subnormal
+absolutely): a sum of s products in fp32 is off by (s + 1) 2^-24 of the sum of
+their magnitudes, a result by u of itself more; a gradient of a weight, summed
+over `width` products in fp32, by (width + 1) 2^-24 of the sum of their magnitudes.
+"""
+import pytest
+import torch
+
+import paper_2003_04296_amd as q
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+U = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+TINY = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134, torch.float32: 2.0 ** -126}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    q.lib()
+    return torch.device("cuda:0")
+
+
+def _gen(dev, seed):
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    return gen
+
+
+def plan(ids, groups):
+    """(offsets, order, place) by Python lists."""
+    flat = ids.reshape(-1).tolist()
+    lists = [[] for _ in range(groups + 1)]
+    for i, e in enumerate(flat):
+        lists[e if 0 <= e < groups else groups].append(i)
+    offsets, place = [0], [-1] * len(flat)
+    for some in lists[:groups]:
+        for j, i in enumerate(some):
+            place[i] = offsets[-1] + j
+        offsets.append(offsets[-1] + len(some))
+    order = [i for some in lists for i in some]
+    t = lambda v: torch.tensor(v, dtype=torch.int32)
+    return t(offsets), t(order), t(place).view(ids.shape)
+
+
+def _check_sort(ids, groups, **kw):
+    got, want = q.moe_sort(ids, groups, **kw), plan(ids.cpu(), groups)
+    for g, w, what in zip(got, want, ("offsets", "order", "place")):
+        assert g.dtype is torch.int32 and g.shape == w.shape and torch.equal(g.cpu(), w), what
+    return got
+
+
+# one id, one wave, its ends, one block and its end, many blocks; groups on both sides of the kernels' forms
+@pytest.mark.parametrize("wide", [torch.int32, torch.int64])
+@pytest.mark.parametrize("tokens,slots,groups", [
+    (1, 1, 1), (1, 8, 64), (3, 2, 1), (16, 4, 64), (63, 1, 7), (64, 1, 63), (65, 1, 64), (1000, 3, 17), (1024, 1, 255),
+    (1025, 1, 256), (513, 2, 1023), (700, 3, 1024), (300, 1, 4096), (8192, 1, 8), (8193, 1, 8), (4097, 5, 129),
+    (33000, 2, 300), (20000, 1, 4096), (9000, 1, 1500)])
+def test_sort(dev, tokens, slots, groups, wide):
+    gen = _gen(dev, tokens + groups)
+    ids = torch.randint(-1 if tokens % 2 else 0, groups + (tokens % 3 == 0), (tokens, slots), generator=gen, device=dev)
+    _check_sort(ids.to(wide), groups)
+
+
+@pytest.mark.parametrize("tokens", [50, 40000])
+@pytest.mark.parametrize("what", ["one", "none", "falling", "last", "far"])
+def test_sort_of_unequal_groups(dev, tokens, what):
+    groups = 37
+    i = torch.arange(tokens, device=dev)
+    ids = {"one": torch.full_like(i, 5), "none": torch.full_like(i, -1), "falling": groups - 1 - i * groups // tokens,
+           "last": torch.full_like(i, groups - 1), "far": torch.where(i % 3 == 0, i % groups, (1 << 33) + i % groups)}[what]
+    _check_sort(ids, groups)
+    _check_sort(ids.clamp(max=1 << 30).int(), groups)
+
+
+def test_sort_of_wider_rows_and_into_tensors(dev):
+    gen = _gen(dev, 3)
+    wide = torch.randint(0, 9, (5000, 7), generator=gen, device=dev, dtype=torch.int32)
+    _check_sort(wide[:, 2:5], 9)
+    _check_sort(wide[:, 3], 9)  # one column of rows of seven
+    out = (torch.empty(10, dtype=torch.int32, device=dev), torch.empty(15000, dtype=torch.int32, device=dev),
+           torch.empty((5000, 3), dtype=torch.int32, device=dev))
+    got = _check_sort(wide[:, 2:5], 9, out=out)
+    assert all(a is b for a, b in zip(got, out))
+
+
+def test_sort_of_nothing(dev):
+    offsets, order, place = q.moe_sort(torch.empty((0, 4), dtype=torch.int32, device=dev), 5)
+    assert offsets.tolist() == [0] * 6 and order.shape == (0,) and place.shape == (0, 4)
+
+
+def _problem(dev, tokens, slots, width, dtype, drop, seed=0, wide=0):
+    gen = _gen(dev, seed + tokens * 7 + width)
+    ids = torch.randint(0, 5, (tokens, slots), generator=gen, device=dev)
+    if drop:
+        ids[torch.rand(ids.shape, generator=gen, device=dev) < drop] = -1
+        ids[tokens // 2] = -1  # a token without any
+    _, _, place = q.moe_sort(ids, 5)
+    draw = lambda n: torch.randn((n, width + wide), generator=gen, device=dev).to(dtype)[:, :width]
+    weights = torch.rand((tokens, slots), generator=gen, device=dev) - 0.2
+    return place, draw(tokens), draw(tokens * slots), draw(tokens), weights
+
+
+def _taken(rows, place):
+    v = rows.double()[place.clamp_min(0).long()]
+    return torch.where((place >= 0).unsqueeze(-1), v, torch.zeros((), dtype=torch.float64, device=v.device))
+
+
+def _near(got, want, bound, what):
+    assert got.shape == want.shape, what
+    bad = ~((got.double() - want).abs() <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} values off, worst {float(((got.double() - want).abs() / bound).max()):.3g}"
+
+
+SIZES = [(1, 1, 1), (1, 8, 4096), (2, 3, 7), (5, 1, 8), (17, 2, 63), (64, 4, 64), (33, 5, 129), (7, 9, 515), (100, 6, 1000),
+         (3, 2, 2051), (257, 2, 1024), (9, 3, 9000)]
+
+
+@pytest.mark.parametrize("drop", [0.0, 0.3])
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("tokens,slots,width", SIZES)
+def test_rows(dev, tokens, slots, width, dtype, drop):
+    t = TYPES[dtype]
+    place, x, rows, gy, weights = _problem(dev, tokens, slots, width, t, drop)
+    flat, keep = place.reshape(-1).long(), place.reshape(-1) >= 0
+    some = flat[keep]
+    # gather: the rows that places name, the others as they were
+    base = torch.full((tokens * slots, width), 7.0, dtype=t, device=dev)
+    want = base.clone()
+    want[some] = x.repeat_interleave(slots, 0)[keep]
+    assert torch.equal(q.moe_gather(x, place, out=base), want)
+    assert torch.equal(q.moe_gather(x, place)[some], want[some])
+    v = _taken(rows, place)
+    # its gradient
+    got = q.moe_gather_backward(rows, place)
+    assert got.dtype is t
+    _near(got, v.sum(1), (slots + 1) * 2.0 ** -24 * v.abs().sum(1) + U[t] * v.sum(1).abs() * 1.01 + TINY[t], "gx")
+    # combine; a NaN weight or row of a dropped slot counts for nothing
+    w = torch.where(place >= 0, weights, torch.full_like(weights, float("nan")))
+    unnamed = torch.ones(tokens * slots, dtype=torch.bool, device=dev)
+    unnamed[some] = False
+    rows = rows.clone()
+    rows[unnamed] = float("nan")
+    p = v * weights.double().unsqueeze(-1)
+    y = q.moe_combine(rows, place, w)
+    _near(y, p.sum(1), (slots + 1) * 2.0 ** -24 * p.abs().sum(1) + U[t] * p.sum(1).abs() * 1.01 + TINY[t], "y")
+    # its gradients
+    base = torch.full((tokens * slots, width), 7.0, dtype=t, device=dev)
+    gr, gw = q.moe_combine_backward(gy, rows, place, w, out=(base, None))
+    assert gr is base and bool((gr[unnamed] == 7.0).all())
+    want = (gy.double().unsqueeze(1) * weights.double().unsqueeze(-1)).expand(-1, slots, -1).reshape(-1, width)[keep]
+    _near(gr[some], want, (U[t] * 1.01 + 2.0 ** -24) * want.abs() + TINY[t], "grows")
+    d = v * gy.double().unsqueeze(1)
+    _near(gw, d.sum(-1), (width + 1) * 2.0 ** -24 * d.abs().sum(-1) + 1e-37, "gw")
+    # each of them alone is the same
+    only_r, none = q.moe_combine_backward(gy, rows, place, w, need_w=False)
+    assert none is None and torch.equal(only_r[some], gr[some])
+    none, only_w = q.moe_combine_backward(gy, rows, place, w, need_rows=False)
+    assert none is None and torch.equal(only_w, gw)
+    # no weights: ones
+    assert torch.equal(q.moe_combine(rows, place), got)
+    assert torch.equal(q.moe_combine_backward(gy, rows, place)[0][some], gy.repeat_interleave(slots, 0)[keep])
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_rows_of_wider_tensors(dev, dtype):
+    """Row strides past the width, at addresses that only a value has, and what lies beside the rows left as it was."""
+    t, tokens, slots, width = TYPES[dtype], 21, 3, 133
+    place, x, rows, gy, w = _problem(dev, tokens, slots, width, t, 0.2, wide=3)
+    plain = [v.contiguous() for v in (x, rows, gy)]
+
+    def into(n):
+        b = torch.full((n, width + 5), 7.0, dtype=t, device=dev)
+        return b, b[:, 1:1 + width]
+
+    for call, want in ((lambda o: q.moe_gather(x, place, out=o), q.moe_gather(plain[0], place)),
+                       (lambda o: q.moe_combine(rows, place, w, out=o), q.moe_combine(plain[1], place, w)),
+                       (lambda o: q.moe_combine_backward(gy, rows, place, w, out=(o, None))[0],
+                        q.moe_combine_backward(plain[2], plain[1], place, w)[0])):
+        b, o = into(len(want))
+        got = call(o)
+        assert got is o
+        named = torch.zeros(len(want), dtype=torch.bool, device=dev)
+        named[place[place >= 0].long() if len(want) > tokens else slice(None)] = True
+        assert torch.equal(got[named], want[named])
+        assert bool((b[:, 0] == 7.0).all()) and bool((b[:, 1 + width:] == 7.0).all()) and bool((got[~named] == 7.0).all())
+
+
+def test_places_outside_the_rows_are_passed_over(dev):
+    place, x, rows, gy, w = _problem(dev, 6, 2, 40, torch.float32, 0.0)
+    bad = place.clone()
+    bad[0, 0], bad[1, 1], bad[2, 0], bad[5, 1] = 12, -7, 0x7fffffff, -0x80000000
+    held = torch.where((bad < 0) | (bad >= 12), torch.full_like(bad, -1), bad)
+    base = torch.zeros((12, 40), device=dev)
+    assert torch.equal(q.moe_gather(x, bad, out=base.clone()), q.moe_gather(x, held, out=base.clone()))
+    assert torch.equal(q.moe_combine(rows, bad, w), q.moe_combine(rows, held, w))
+    for a, b in zip(q.moe_combine_backward(gy, rows, bad, w, out=(base.clone(), None)),
+                    q.moe_combine_backward(gy, rows, held, w, out=(base.clone(), None))):
+        assert torch.equal(a, b)
+
+
+def test_no_tokens(dev):
+    place = torch.empty((0, 2), dtype=torch.int32, device=dev)
+    x = torch.empty((0, 16), dtype=torch.bfloat16, device=dev)
+    assert q.moe_gather(x, place).shape == (0, 16) and q.moe_combine(x, place).shape == (0, 16)
+    gr, gw = q.moe_combine_backward(x, x, place)
+    assert gr.shape == (0, 16) and gw.shape == (0, 2)
+
+
+def test_infinities_and_nan(dev):
+    """They come through where a place names them, and only there."""
+    place, x, rows, gy, w = _problem(dev, 8, 2, 24, torch.bfloat16, 0.0)
+    rows = rows.clone()
+    r = int(place[3, 1])
+    rows[r, 5], rows[r, 6] = float("inf"), float("nan")
+    y = q.moe_combine(rows, place, w.abs() + 0.1)
+    assert torch.isinf(y[3, 5]) and torch.isnan(y[3, 6])
+    assert int((~torch.isfinite(y)).sum()) == 2
+
+
+def test_gradients_against_differences(dev):
+    """sum(c combine(gather(x) * v, w)): the chain's gradients along random directions, by central differences in 64 bits."""
+    place, x, v, c, w = _problem(dev, 12, 3, 20, torch.float32, 0.2)
+    gy = c
+    rows = q.moe_gather(x, place, out=torch.zeros((36, 20), device=dev)) * v
+    gr, gw = q.moe_combine_backward(gy, rows, place, w, out=(torch.zeros((36, 20), device=dev), None))
+    gx = q.moe_gather_backward(gr * v, place)
+
+    def loss(xd, wd):
+        keep = place >= 0
+        r = xd.unsqueeze(1) * _taken(v, place)
+        return (torch.where(keep.unsqueeze(-1), r * wd.unsqueeze(-1), torch.zeros_like(r)).sum(1) * c.double()).sum()
+
+    gen, h = _gen(dev, 1), 1e-4
+    for which, got in ((0, gx), (1, gw)):
+        args = [x.double(), w.double()]
+        d = torch.randn(args[which].shape, generator=gen, device=dev, dtype=torch.float64)
+        hi, lo = ([a + s * h * d if j == which else a for j, a in enumerate(args)] for s in (1, -1))
+        slope = float(loss(*hi) - loss(*lo)) / (2 * h)  # the loss is linear in each
+        # every value of the gradient carries roundings of at most 30 x 2^-24 of it or of its terms
+        assert abs(float((got.double() * d).sum()) - slope) <= 1e-5 * float(got.double().norm() * d.norm()) + 1e-9, which

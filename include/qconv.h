@@ -461,6 +461,45 @@ int qconv_moe_linear_backward(const qconv_moe_desc* d, const void* x, const void
                               const void* gy, void* gx, void* gw, void* workspace, size_t workspace_bytes,
                               void* stream);
 
+/* The largest rank of an adapter. */
+#define QCONV_LORA_RANK_MOST 256
+
+typedef struct {
+  int m, groups, rank, k, n;    /* tokens, adapters, their rank, inputs, outputs      */
+  int dtype;                    /* QCONV_F16 or QCONV_BF16: every tensor but mid      */
+  int64_t ld_x, ld_y, ld_out;   /* row strides of x, of y and gy, of out              */
+} qconv_lora_desc;
+
+/* Floats of the `mid` buffer: a row of rank (rounded up to 4) values per token. */
+size_t qconv_lora_mid_floats(int m, int rank);
+
+/* Low-rank adapters beside a shared projection: for a token t of adapter g
+ *   out[t] = y[t] + scale[g] (x[t] a_g^T) b_g^T,   out[t] = y[t] for one of none.
+ * x[m][k], y[m][n] (the projection's result), a[groups][rank][k] and
+ * b[groups][n][rank] contiguous, scale[groups] fp32 (NULL for ones).  The tokens of
+ * adapter g are order[offsets[g]] .. order[offsets[g + 1] - 1], those after
+ * offsets[groups] have none (qconv_moe_sort of each token's adapter, one slot); a
+ * token is named once.  out may be y itself (ld_out == ld_y) or overlap no input.
+ * x a^T stays in fp32 (the leading 16 bits of each value enter the second
+ * product); the result is rounded once.  An infinity among the operands may give
+ * a NaN in its place.  mid (NULL to leave it out) receives x a^T in order's order
+ * for the backward pass. */
+size_t qconv_lora_forward_bytes(const qconv_lora_desc* d, int keep_mid);
+int qconv_lora_forward(const qconv_lora_desc* d, const void* x, const void* a, const void* b, const int32_t* offsets,
+                       const int32_t* order, const float* scale, const void* y, void* out, float* mid,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* From gy[m][n] (the gradient of out; y's is the same) and the forward's mid:
+ *   gx[m][k] = scale[g] (gy b_g) a_g, zeros for a token of no adapter,
+ *   ga[groups][rank][k] = scale[g] sum over its tokens of (gy b_g)^T x,
+ *   gb[groups][n][rank] = scale[g] sum over its tokens of gy^T (x a_g^T),
+ * contiguous, zeros for an adapter without tokens.  gx, and ga together with gb,
+ * may be NULL to leave them out.  ld_out is not used. */
+size_t qconv_lora_backward_bytes(const qconv_lora_desc* d);
+int qconv_lora_backward(const qconv_lora_desc* d, const void* x, const void* a, const void* b, const int32_t* offsets,
+                        const int32_t* order, const float* scale, const float* mid, const void* gy, void* gx, void* ga,
+                        void* gb, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* The norm over all gradients of a model, and clipping by it                */
 /* ------------------------------------------------------------------------ */

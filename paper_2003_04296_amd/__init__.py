@@ -42,6 +42,8 @@ EXPORTED = (
     "qconv_moe_sort_bytes", "qconv_moe_sort", "qconv_moe_gather", "qconv_moe_combine", "qconv_moe_combine_backward",
     "qconv_moe_forward_bytes", "qconv_moe_gated_forward", "qconv_moe_linear_forward", "qconv_moe_backward_bytes",
     "qconv_moe_gated_backward", "qconv_moe_linear_backward",
+    "qconv_lora_mid_floats", "qconv_lora_forward_bytes", "qconv_lora_forward", "qconv_lora_backward_bytes",
+    "qconv_lora_backward",
 )
 
 
@@ -81,6 +83,11 @@ class qconv_moe_rows_desc(ctypes.Structure):
 class qconv_moe_desc(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int) for name in ("rows", "groups", "k", "f", "dtype", "act")] + \
                [(name, ctypes.c_int64) for name in ("ld_x", "ld_w", "ld_h")]
+
+
+class qconv_lora_desc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("m", "groups", "rank", "k", "n", "dtype")] + \
+               [(name, ctypes.c_int64) for name in ("ld_x", "ld_y", "ld_out")]
 
 
 _lib = None
@@ -153,6 +160,15 @@ def lib() -> ctypes.CDLL:
     L.qconv_moe_linear_forward.argtypes = [moe] + [vp] * 5 + [sz, vp]
     L.qconv_moe_gated_backward.argtypes = [moe] + [vp] * 10 + [sz, vp]
     L.qconv_moe_linear_backward.argtypes = [moe] + [vp] * 7 + [sz, vp]
+    lora = vp
+    L.qconv_lora_mid_floats.restype = sz
+    L.qconv_lora_mid_floats.argtypes = [i32] * 2
+    L.qconv_lora_forward_bytes.restype = sz
+    L.qconv_lora_forward_bytes.argtypes = [lora, i32]
+    L.qconv_lora_forward.argtypes = [lora] + [vp] * 10 + [sz, vp]
+    L.qconv_lora_backward_bytes.restype = sz
+    L.qconv_lora_backward_bytes.argtypes = [lora]
+    L.qconv_lora_backward.argtypes = [lora] + [vp] * 12 + [sz, vp]
     L.aqe_grad_norm_bytes.restype = sz
     L.aqe_grad_norm_bytes.argtypes = [i32, vp]
     L.aqe_grad_norm.argtypes = [i32] + [vp] * 5 + [sz, vp]
@@ -586,6 +602,7 @@ def q4_gated(x, gate_codes, gate_scales, up_codes, up_scales, act: int = ACT_SIL
 
 _ROWS_DESC = struct.Struct("4i2q")
 _MOE_DESC = struct.Struct("6i3q")
+_LORA_DESC = struct.Struct("6i3q")
 
 
 def _indices(t, like, what: str, numel=None):
@@ -821,6 +838,78 @@ def moe_linear_backward(x, w, offsets, gy, need_x: bool = True, need_w: bool = T
     _check(L.qconv_moe_linear_backward(d, x.data_ptr(), w.data_ptr(), offsets.data_ptr(), gy.data_ptr(), _ptr(gx),
                                        _ptr(gw), _ptr(ws), nbytes, _stream(stream)), "qconv_moe_linear_backward")
     return gx, gw
+
+
+def _lora_args(x, a, b, offsets, order, scale, y, out, what, stream):
+    """(m, groups, rank, k, n, descriptor) of an adapters' call."""
+    import torch
+
+    m, k = _matrix(x, what, stream)
+    dev = x.get_device()
+    sa, sb = a.shape, b.shape
+    if len(sa) != 3 or len(sb) != 3 or sa[2] != k or sb[0] != sa[0] or sb[2] != sa[1] or a.dtype is not x.dtype or \
+            b.dtype is not x.dtype or a.get_device() != dev or b.get_device() != dev or not a.is_contiguous() or \
+            not b.is_contiguous():
+        raise ValueError(f"{what}: a is [adapters][rank][{k}] and b [adapters][n][rank], contiguous {x.dtype} on {x.device}")
+    groups, rank, n = sa[0], sa[1], sb[1]
+    _indices(offsets, x, what + " offsets", groups + 1)
+    _indices(order, x, what + " order", m)
+    if scale is not None and (scale.dtype is not torch.float32 or scale.shape != (groups,) or scale.get_device() != dev or
+                              not scale.is_contiguous()):
+        raise ValueError(f"{what}: scale is a contiguous fp32 vector of {groups} on {x.device}")
+    ld_y = _rows(y, m, n, x, what)
+    return m, groups, rank, k, n, _LORA_DESC.pack(_int(m), groups, rank, _int(k), _int(n), _dtypes[x.dtype],
+                                                  _ld(x, (m, k), what), ld_y,
+                                                  ld_y if out is None else _rows(out, m, n, x, what + " out"))
+
+
+def _check_mid(mid, m, rank, like, what):
+    import torch
+
+    if mid.dtype is not torch.float32 or mid.get_device() != like.get_device() or not mid.is_contiguous() or \
+            mid.numel() < lib().qconv_lora_mid_floats(m, rank):
+        raise ValueError(f"{what}: mid holds at least {lib().qconv_lora_mid_floats(m, rank)} contiguous fp32 values")
+
+
+def lora_forward(y, x, a, b, offsets, order, scale=None, keep_mid: bool = False, mid=None, out=None, workspace=None,
+                 stream=None):
+    """Adds to y [m][n], a shared projection's result for x [m][k], each token's
+    low-rank adapter: y[t] + scale[g] (x[t] a_g^T) b_g^T with a [adapters][rank][k],
+    b [adapters][n][rank], scale fp32 [adapters] (None: ones) -> (out, mid).  In
+    place, or into `out`.  offsets and order are moe_sort's of the tokens' adapters
+    (ids [m]); a token of none keeps its y.  keep_mid (or a buffer `mid` of a former
+    call) keeps what lora_backward needs, else mid is None.  rank is at most 256."""
+    m, groups, rank, k, n, d = _lora_args(x, a, b, offsets, order, scale, y, out, "lora_forward", stream)
+    L = lib()
+    if mid is not None:
+        _check_mid(mid, m, rank, x, "lora_forward")
+    elif keep_mid:
+        import torch
+
+        mid = _new((L.qconv_lora_mid_floats(m, rank),), torch.float32, x, stream)
+    to = y if out is None else out
+    ws, nbytes = _workspace(workspace, L.qconv_lora_forward_bytes(d, mid is not None), x, "lora_forward", stream)
+    _check(L.qconv_lora_forward(d, x.data_ptr(), a.data_ptr(), b.data_ptr(), offsets.data_ptr(), order.data_ptr(),
+                                _ptr(scale), y.data_ptr(), to.data_ptr(), _ptr(mid), _ptr(ws), nbytes, _stream(stream)),
+           "qconv_lora_forward")
+    return to, mid
+
+
+def lora_backward(x, a, b, offsets, order, mid, gy, scale=None, need_x: bool = True, need_w: bool = True, out=None,
+                  workspace=None, stream=None):
+    """From gy [m][n] and the forward's mid -> (gx [m][k]: the adapters' part of
+    x's gradient, ga, gb) in x's type; None for what need_x / need_w leave out.
+    out: contiguous tensors (or None) to write instead of new ones."""
+    m, groups, rank, k, n, d = _lora_args(x, a, b, offsets, order, scale, gy, None, "lora_backward", stream)
+    _check_mid(mid, m, rank, x, "lora_backward")
+    gx, ga, gb = _grad_outs(out, ((m, k), (groups, rank, k), (groups, n, rank)), (need_x, need_w, need_w), x,
+                            "lora_backward", stream)
+    L = lib()
+    ws, nbytes = _workspace(workspace, L.qconv_lora_backward_bytes(d), x, "lora_backward", stream)
+    _check(L.qconv_lora_backward(d, x.data_ptr(), a.data_ptr(), b.data_ptr(), offsets.data_ptr(), order.data_ptr(),
+                                 _ptr(scale), mid.data_ptr(), gy.data_ptr(), _ptr(gx), _ptr(ga), _ptr(gb), _ptr(ws),
+                                 nbytes, _stream(stream)), "qconv_lora_backward")
+    return gx, ga, gb
 
 
 def _dense(t) -> bool:

@@ -1,0 +1,707 @@
+// lora.hip -- low-rank adapters of many requests beside a shared projection, and
+// their gradients.  Token t of adapter g:
+//   mid[t] = x[t] a_g^T            (rank values, fp32)
+//   out[t] = y[t] + s_g mid[t] b_g^T
+//   p[t]   = gy[t] b_g             (rank values, fp32)
+//   gx[t]  = s_g p[t] a_g,  ga_g = s_g sum_t p[t] x[t],  gb_g = s_g sum_t gy[t] mid[t]
+// An adapter's tokens are order[offsets[g]] .. order[offsets[g + 1] - 1], wherever
+// they lie in the batch: a block takes 16 or 32 of them ("piece") and reads their
+// rows in place.  Bound by HBM: the tokens' rows and the adapters in use are read
+// once, which the matrix instructions keep up with at every rank.
+//
+// mid and p stay in fp32 between the passes.  Where they are an operand they enter
+// as two bf16 parts, the leading 16 bits of each value: rounding them to the
+// tensors' type would lose half of a 16-bit result's accuracy again, and in fp16
+// overflow past 65504.  fp16 tensors that meet them are split, too, exactly: 11
+// bits are a bf16 and a rest of 3.  The third product of that (of both rests) is
+// below 2^-17 of the first and left out.
+#include "dense_gemm.h"
+#include "moe.h"
+#include "moe_groups.h"
+
+#include "qconv_internal.h"
+
+namespace qc {
+
+namespace {
+
+// A weight of each group, inner dimension contiguous.
+struct GroupWeight {
+  const uint16_t* p;
+  int64_t ld, step;  // of rows and of groups
+};
+
+struct LoraArgs {
+  Groups g;
+  const int* order;
+  const float* scale;  // [groups] or NULL
+  int rank, len;       // len: the tokens' row length
+  const uint16_t* x;   // rows of tokens: the operand (shrink, grad), what is added to or NULL (expand)
+  int64_t ld_x;
+  GroupWeight w;       // shrink [rank][len], expand [len][rank]
+  float* mid;          // [parts][rows][ld_mid]
+  int ld_mid, parts;
+  int tiles;           // shrink: of ranks; expand and grad: of columns
+  uint16_t* out;       // expand: rows of tokens; grad: [groups][rank][len] or [groups][len][rank]
+  int64_t ld_out;
+  float* part;         // grad: sums of pieces
+  int64_t ld_part;
+  int size;            // grad: rows of a piece
+};
+
+// The token of row r of the order; `m` tokens exist.
+__device__ __forceinline__ int token_at(const LoraArgs& a, int r) {
+  const int t = a.order[r];
+  return (uint32_t)t < (uint32_t)a.g.rows ? t : -1;
+}
+
+// ---------------------------------------------------------------------------
+// mid (and p): sums over a row's length
+// ---------------------------------------------------------------------------
+
+// A block takes MR * 16 tokens by RT * 16 ranks; its waves, and the blocks of a
+// split product, take every so many-th 128 values of the rows, and are joined
+// through LDS (splits by whoever reads mid).
+template <class T, int MR, int RT, int NW>
+__global__ __launch_bounds__(NW * 64) void lora_shrink_kernel(LoraArgs a) {
+  constexpr int R = MR * 16, C = RT * 16;
+  __shared__ v4f part[NW][R][C / 4];
+  const GroupPieces pieces(a.g, R);
+  const int split = blockIdx.x % a.parts, tile = blockIdx.x / a.parts % a.tiles, p = blockIdx.x / a.parts / a.tiles;
+  if (p >= pieces.total) return;
+  int e, piece;
+  pieces.find(a.g, p, e, piece);
+  const GroupRows rows = group_rows(a.g, e);
+  const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, o = lane >> 4;
+  // in place of rows past the piece its first one, of ranks past the last that one: their sums go nowhere
+  const uint16_t *x[MR], *w[RT];
+#pragma unroll
+  for (int j = 0; j < MR; ++j) {
+    const int t = token_at(a, first + (j * 16 + r < here ? j * 16 + r : 0));
+    x[j] = a.x + (int64_t)(t < 0 ? 0 : t) * a.ld_x + o * 8;
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const int c = tile * C + i * 16 + r;
+    w[i] = a.w.p + e * a.w.step + (c < a.rank ? c : a.rank - 1) * a.w.ld + o * 8;
+  }
+  v4f acc[MR][RT];
+#pragma unroll
+  for (int j = 0; j < MR; ++j)
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  const int blocks = a.len / 128, step = a.parts * NW;
+  int b = split * NW + wave;
+  for (; b < blocks; b += step) {
+    v4u xf[MR][4], wf[RT][4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+#pragma unroll
+      for (int j = 0; j < MR; ++j) xf[j][s] = load8(x[j] + (int64_t)b * 128 + s * 32);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) wf[i][s] = load8(w[i] + (int64_t)b * 128 + s * 32);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int j = 0; j < MR; ++j)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) acc[j][i] = T::mfma(wf[i][s], xf[j][s], acc[j][i]);
+  }
+  if (b == blocks && a.len % 128) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int k = blocks * 128 + s * 32, left = a.len - k - o * 8;
+      v4u xf[MR];
+#pragma unroll
+      for (int j = 0; j < MR; ++j) xf[j] = load8_first(x[j] + k, left);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const v4u wf = load8_first(w[i] + k, left);
+#pragma unroll
+        for (int j = 0; j < MR; ++j) acc[j][i] = T::mfma(wf, xf[j], acc[j][i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < MR; ++j)
+#pragma unroll
+    for (int i = 0; i < RT; ++i) part[wave][j * 16 + r][i * 4 + o] = acc[j][i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < here * (C / 4); i += NW * 64) {
+    const int row = i / (C / 4), c = i % (C / 4);
+    v4f s = part[0][row][c];
+#pragma unroll
+    for (int v = 1; v < NW; ++v) s += part[v][row][c];
+    if (tile * C + c * 4 < a.ld_mid)
+      *(v4f*)(a.mid + ((int64_t)split * a.g.rows + first + row) * a.ld_mid + tile * C + c * 4) = s;
+  }
+}
+
+// Joins the parts of mid into the first.
+__global__ __launch_bounds__(256) void lora_join_kernel(float* mid, int64_t n, int parts, float* to) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n / 4; i += (int64_t)gridDim.x * 256) {
+    v4f s = *(const v4f*)(mid + i * 4);
+    for (int p = 1; p < parts; ++p) s += *(const v4f*)(mid + p * n + i * 4);
+    *(v4f*)(to + i * 4) = s;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Two bf16 parts of a value
+// ---------------------------------------------------------------------------
+
+struct Two {
+  uint16_t hi, lo;
+};
+__device__ __forceinline__ Two two_parts(float v) {
+  const uint16_t hi = BF16::down(v);
+  // an infinity has no rest
+  return {hi, (hi & 0x7F80) == 0x7F80 ? (uint16_t)0 : BF16::down(v - BF16::up(hi))};
+}
+// Eight values of a tensor's type in bf16: itself, or a value and the rest (fp16).
+template <class T>
+__device__ __forceinline__ void in_bf16(v4u v, v4u out[2]) {
+  if constexpr (T::REST) {  // bf16
+    out[0] = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const Two a = two_parts(T::up((uint16_t)v[e])), b = two_parts(T::up((uint16_t)(v[e] >> 16)));
+      out[0][e] = a.hi | (uint32_t)b.hi << 16;
+      out[1][e] = a.lo | (uint32_t)b.lo << 16;
+    }
+  }
+}
+template <class T>
+constexpr int BF16_PARTS = T::REST ? 1 : 2;
+
+// ---------------------------------------------------------------------------
+// out = y + s mid w^T
+// ---------------------------------------------------------------------------
+
+// A block takes MR * 16 tokens; a wave 64 columns at a time.  The 16 rows of
+// operand i are columns (q / 4) * 16 + i * 4 + q % 4 of the 64, so that a lane
+// ends up with 16 columns in a row, which it reads and writes 16 bytes at a time.
+template <class T, int MR>
+__global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
+  constexpr int R = MR * 16;
+  extern __shared__ v4u lds[];  // [R][ranks of hi, then of lo, in chunks of 8, and one to spread the banks]
+  const GroupPieces pieces(a.g, R);
+  const int tile = blockIdx.x % a.tiles, p = blockIdx.x / a.tiles;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, o = lane >> 4;
+  const int chunks = (a.len + 63) / 64;
+  if (p >= pieces.total) {
+    // tokens of no adapter: a copy, or zeros
+    const int end = a.g.offsets[a.g.n], begin = end < 0 ? 0 : end;
+    const int64_t row0 = (int64_t)begin + (int64_t)(p - pieces.total) * R;
+    if (row0 >= a.g.rows || a.x == a.out) return;
+    for (int c = tile * 4 + wave; c < chunks; c += a.tiles * 4)
+      for (int j = 0; j < R; j += 8) {
+        const int row = j + lane / 8, col = c * 64 + lane % 8 * 8;
+        if (row0 + row >= a.g.rows || col >= a.len) continue;
+        const int t = token_at(a, (int)row0 + row);
+        if (t < 0) continue;
+        const v4u v = a.x ? load8_first(a.x + t * a.ld_x + col, a.len - col) : v4u{0, 0, 0, 0};
+        uint16_t* to = a.out + t * a.ld_out + col;
+        if (col + 8 <= a.len) {
+          reinterpret_cast<U128*>(to)->v = v;
+        } else {
+          for (int q = 0; col + q < a.len; ++q) to[q] = (uint16_t)(v[q / 2] >> (16 * (q & 1)));
+        }
+      }
+    return;
+  }
+  int e, piece;
+  pieces.find(a.g, p, e, piece);
+  const GroupRows rows = group_rows(a.g, e);
+  const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
+  const int steps = (a.rank + 31) / 32, ld = steps * 8 + 1;  // in chunks
+  // mid's rows: summed over its parts, zeros past the rank
+  for (int i = threadIdx.x; i < R * steps * 8; i += 256) {
+    const int row = i / (steps * 8), c = i % (steps * 8) * 4;
+    v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (row < here && c < a.rank) {
+      const float* m = a.mid + (int64_t)(first + row) * a.ld_mid + c;
+      s = *(const v4f*)m;
+      for (int q = 1; q < a.parts; ++q) s += *(const v4f*)(m + (int64_t)q * a.g.rows * a.ld_mid);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (c + q >= a.rank) s[q] = 0.0f;
+    }
+    const Two t[4] = {two_parts(s[0]), two_parts(s[1]), two_parts(s[2]), two_parts(s[3])};
+    v2u* to = (v2u*)(lds + row * ld) + i % (steps * 8);
+    to[0] = v2u{t[0].hi | (uint32_t)t[1].hi << 16, t[2].hi | (uint32_t)t[3].hi << 16};
+    to[steps * 8] = v2u{t[0].lo | (uint32_t)t[1].lo << 16, t[2].lo | (uint32_t)t[3].lo << 16};
+  }
+  __syncthreads();
+  const float scale = a.scale ? a.scale[e] : 1.0f;
+  int token[MR];
+#pragma unroll
+  for (int j = 0; j < MR; ++j) token[j] = j * 16 + r < here ? token_at(a, first + j * 16 + r) : -1;
+  const uint16_t* wp = a.w.p + e * a.w.step;
+  for (int ch = tile * 4 + wave; ch < chunks; ch += a.tiles * 4) {
+    const int c0 = ch * 64, mine = c0 + o * 16;  // of the results
+    v4u y[MR][2];
+#pragma unroll
+    for (int j = 0; j < MR; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int left = token[j] >= 0 && a.x ? a.len - mine - h * 8 : 0;
+        y[j][h] = load8_first(left > 0 ? a.x + token[j] * a.ld_x + mine + h * 8 : a.x, left);
+      }
+    v4f acc[MR][4];
+#pragma unroll
+    for (int j = 0; j < MR; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < steps; ++k) {
+      v4u wf[4][2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = c0 + (r >> 2) * 16 + i * 4 + (r & 3);
+        in_bf16<T>(load8_first(wp + (c < a.len ? c : a.len - 1) * a.w.ld + k * 32 + o * 8, a.rank - k * 32 - o * 8), wf[i]);
+      }
+#pragma unroll
+      for (int j = 0; j < MR; ++j) {
+        const v4u* s = lds + (j * 16 + r) * ld + k * 4 + o;
+        const v4u hi = s[0], lo = s[steps * 4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[j][i] = BF16::mfma(wf[i][0], hi, acc[j][i]);
+          acc[j][i] = BF16::mfma(wf[i][0], lo, acc[j][i]);
+          if constexpr (BF16_PARTS<T> == 2) acc[j][i] = BF16::mfma(wf[i][1], hi, acc[j][i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < MR; ++j) {
+      if (token[j] < 0) continue;
+      uint16_t* to = a.out + token[j] * a.ld_out + mine;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint16_t v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          v[q] = T::down(fmaf(scale, acc[j][h * 2 + q / 4][q % 4], T::up((uint16_t)(y[j][h][q / 2] >> (16 * (q & 1))))));
+        if (mine + h * 8 + 8 <= a.len) {
+          reinterpret_cast<U128*>(to + h * 8)->v =
+              v4u{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
+                  v[6] | (uint32_t)v[7] << 16};
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (mine + h * 8 + q < a.len) to[h * 8 + q] = v[q];
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Weight gradients: sums over an adapter's tokens
+// ---------------------------------------------------------------------------
+
+// Rows of an adapter are taken `size` at a time; a block has 256 columns of a
+// piece and 64 ranks.  The sums of an adapter with one piece (or none: zeros) are
+// results; others go to part, where the piece that starts at row s has its place
+// by s: pieces of one adapter start `size` rows apart, so at most two of several
+// start in the same `size` rows, and of these one is an adapter's first.
+__device__ __forceinline__ int pieces_of(const GroupRows& r, int size) {
+  return r.count > size ? (r.count + size - 1) / size : 1;
+}
+__device__ __forceinline__ int64_t part_at(int first, int piece, int size) {
+  return 2 * ((int64_t)first / size + piece) + (piece == 0 ? 1 : 0);
+}
+
+// Writes 4 values of a row of a gradient.
+template <class T>
+__device__ __forceinline__ void put_grad(const LoraArgs& a, int e, int rows, int cols, int row, int col, v4f v) {
+  const float s = a.scale ? a.scale[e] : 1.0f;
+  uint16_t* to = a.out + ((int64_t)e * rows + row) * cols + col;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (col + q < cols) to[q] = T::down(s * v[q]);
+}
+
+// Results [rank][len] (ga), or with FLIP [len][rank] (gb).  Both operands run down
+// their columns: they pass through registers into LDS rows of one token and are
+// read transposed.
+template <class T, int RT, bool FLIP>
+__global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
+  constexpr int C = 256, XP = BF16_PARTS<T>, XCH = 32 * C / 8, SCH = 32 * 128 / 8, STAGE = XCH * XP + SCH;
+  [[maybe_unused]] __shared__ v4u store[2 * STAGE];
+#ifdef __HIP_DEVICE_COMPILE__
+  lds_v4u* const lds = (lds_v4u*)store;
+  const GroupPieces pieces(a.g, a.size, true);
+  const int rts = (a.rank + 63) / 64;
+  const int tile = blockIdx.x % a.tiles, rt = blockIdx.x / a.tiles % rts, p = blockIdx.x / a.tiles / rts;
+  if (p >= pieces.total) return;
+  int e, piece;
+  pieces.find(a.g, p, e, piece);
+  const GroupRows rows = group_rows(a.g, e);
+  const int first = rows.first + piece * a.size;
+  const int here = rows.count - piece * a.size < a.size ? rows.count - piece * a.size : a.size;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c0 = tile * C, r0 = rt * 64;
+  v4f acc[4][RT];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  // A stage: 32 tokens.  Of x a thread has 4 chunks of 8 columns, of mid 2 x 4 ranks.
+  v4u xr[4];
+  v4f sr[2];
+  const int xc = threadIdx.x % 32, sc = threadIdx.x % 16 * 4;
+  auto load = [&](int at) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = at + threadIdx.x / 32 + i * 8, col = c0 + xc * 8;
+      const int t = k < here ? token_at(a, first + k) : -1;
+      xr[i] = load8_first(t >= 0 ? a.x + t * a.ld_x + col : a.x, t >= 0 ? a.len - col : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = at + threadIdx.x / 16 + i * 16;
+      // a token that is none counts for nothing
+      const bool on = k < here && r0 + sc < a.rank && token_at(a, first + k) >= 0;
+      sr[i] = on ? *(const v4f*)(a.mid + (int64_t)(first + k) * a.ld_mid + r0 + sc) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  };
+  auto put = [&](lds_v4u* to) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = threadIdx.x / 32 + i * 8;
+      v4u v[2];
+      in_bf16<T>(xr[i], v);
+#pragma unroll
+      for (int q = 0; q < XP; ++q) to[q * XCH + k * (C / 8) + (xc ^ swz_col(k))] = v[q];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = threadIdx.x / 16 + i * 16;
+      const Two t[4] = {two_parts(sr[i][0]), two_parts(sr[i][1]), two_parts(sr[i][2]), two_parts(sr[i][3])};
+      lds_v4u* const row = to + XP * XCH + k * 16;
+      typedef __attribute__((address_space(3))) v2u* half;
+      ((half)(row + ((sc / 8) ^ swz_col(k))))[sc / 4 & 1] =
+          v2u{t[0].hi | (uint32_t)t[1].hi << 16, t[2].hi | (uint32_t)t[3].hi << 16};
+      ((half)(row + ((sc / 8 + 8) ^ swz_col(k))))[sc / 4 & 1] =
+          v2u{t[0].lo | (uint32_t)t[1].lo << 16, t[2].lo | (uint32_t)t[3].lo << 16};
+    }
+  };
+  if (here > 0) {
+    load(0);
+    put(lds);
+  }
+  for (int at = 0, b = 0; at < here; at += 32, b ^= 1) {
+    __syncthreads();
+    const lds_v4u* now = lds + b * STAGE;
+    const bool more = at + 32 < here;
+    if (more) load(at + 32);
+    v4u s[2][RT];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < RT; ++j) s[h][j] = fragment<32, 128, true>(now + XP * XCH, h * 64 + j * 16, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v4u x[XP];
+#pragma unroll
+      for (int q = 0; q < XP; ++q) x[q] = fragment<32, C, true>(now + q * XCH, wave * 64 + i * 16, 0);
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        auto add = [&](v4u xf, v4u sf) {
+          acc[i][j] = FLIP ? BF16::mfma(sf, xf, acc[i][j]) : BF16::mfma(xf, sf, acc[i][j]);
+        };
+        add(x[0], s[0][j]);
+        add(x[0], s[1][j]);
+        if constexpr (XP == 2) add(x[1], s[0][j]);
+      }
+    }
+    if (more) put(lds + (b ^ 1) * STAGE);
+  }
+  const bool whole = rows.count <= a.size;
+  const int nr = FLIP ? a.len : a.rank, nc = FLIP ? a.rank : a.len;
+  float* const to = a.part + part_at(rows.first, piece, a.size) * nr * a.ld_part;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+      const int x = c0 + wave * 64 + i * 16, s = r0 + j * 16;  // the first column and rank
+      const int row = (FLIP ? x : s) + (lane & 15), col = (FLIP ? s : x) + (lane >> 4) * 4;
+      if (row >= nr || col >= nc) continue;
+      if (whole) put_grad<T>(a, e, nr, nc, row, col, acc[i][j]);
+      else *(v4f*)(to + (int64_t)row * a.ld_part + col) = acc[i][j];
+    }
+#endif
+}
+
+// Joins the pieces of the adapters that have several: the y-th of them.
+template <class T, bool FLIP>
+__global__ __launch_bounds__(256) void lora_grad_join_kernel(LoraArgs a) {
+  const GroupPieces several(a.g, a.size, true, true);
+  if ((int)blockIdx.y >= several.total) return;
+  int e, unused;
+  several.find(a.g, blockIdx.y, e, unused);
+  const GroupRows rows = group_rows(a.g, e);
+  const int n = pieces_of(rows, a.size);
+  const int nr = FLIP ? a.len : a.rank, nc = FLIP ? a.rank : a.len, per = (int)(a.ld_part / 4);
+  const int64_t all = (int64_t)nr * per, plane = nr * a.ld_part;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int row = (int)(i / per), col = (int)(i % per) * 4;
+    v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) s += *(const v4f*)(a.part + part_at(rows.first, p, a.size) * plane + row * a.ld_part + col);
+    put_grad<T>(a, e, nr, nc, row, col, s);
+  }
+}
+
+// The transposed copy of each group's matrix [rows][cols] in rows of ld_out.
+__global__ __launch_bounds__(256) void lora_transpose_kernel(const uint16_t* w, int rows, int cols, uint16_t* out,
+                                                             int64_t ld_out, int tiles_r, int tiles_c) {
+  __shared__ uint16_t t[64][66];
+  const int tc = blockIdx.x % tiles_c, tr = blockIdx.x / tiles_c % tiles_r;
+  const int64_t g = blockIdx.x / tiles_c / tiles_r;
+  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  for (int i = y; i < 64; i += 4) {
+    const int r = tr * 64 + i, c = tc * 64 + x;
+    if (r < rows && c < cols) t[i][x] = w[(g * rows + r) * cols + c];
+  }
+  __syncthreads();
+  for (int i = y; i < 64; i += 4) {
+    const int r = tr * 64 + x, c = tc * 64 + i;
+    if (r < rows && c < cols) out[(g * cols + c) * ld_out + r] = t[x][i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+
+int ld_mid(const qconv_lora_desc& d) { return (int)round_up(d.rank, 4); }
+size_t mid_bytes(const qconv_lora_desc& d) { return (size_t)round_up((int64_t)d.m * ld_mid(d) * 4, 16); }
+
+// Tokens of a piece: 32 where that makes enough pieces for the chip, else 16.
+int piece_rows(const qconv_lora_desc& d) { return d.m >= 32 * 128 ? 32 : 16; }
+
+// Blocks that share the sums over a row of `len` values: until there are about
+// 512 of them, as long as each wave has 128 values.
+int shrink_parts(const qconv_lora_desc& d, int len) {
+  const int R = piece_rows(d);
+  const int64_t blocks = GroupPieces::most(d.m, d.groups, R) * ceil_div(d.rank, 64);
+  int64_t parts = 512 / (blocks > 0 ? blocks : 1);
+  if (parts > len / 1024) parts = len / 1024;
+  return parts < 1 ? 1 : parts > 8 ? 8 : (int)parts;
+}
+
+constexpr int NW = 8;
+
+template <class T, int MR, int RT>
+int run_shrink_t(LoraArgs& a, hipStream_t s) {
+  a.tiles = ceil_div(a.rank, RT * 16);
+  const int64_t blocks = GroupPieces::most(a.g.rows, a.g.n, MR * 16) * a.tiles * a.parts;
+  if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;  // 2^31 threads
+  lora_shrink_kernel<T, MR, RT, NW><<<(unsigned)blocks, NW * 64, 0, s>>>(a);
+  return hip_status();
+}
+template <class T>
+int run_shrink(LoraArgs& a, int rows, hipStream_t s) {
+  if (rows == 32)
+    return a.rank <= 16 ? run_shrink_t<T, 2, 1>(a, s) : a.rank <= 32 ? run_shrink_t<T, 2, 2>(a, s) : run_shrink_t<T, 2, 4>(a, s);
+  return a.rank <= 16 ? run_shrink_t<T, 1, 1>(a, s) : a.rank <= 32 ? run_shrink_t<T, 1, 2>(a, s) : run_shrink_t<T, 1, 4>(a, s);
+}
+
+template <class T>
+int run_expand(LoraArgs& a, int rows, hipStream_t s) {
+  const int64_t pieces = a.g.rows / rows + (a.g.n + 1 < a.g.rows ? a.g.n + 1 : a.g.rows);
+  // a block per 256 columns until there are about 1024
+  const int64_t most = ceil_div(a.len, 256), want = 1024 / pieces;
+  a.tiles = (int)(want < 1 ? 1 : want < most ? want : most);
+  if (pieces * a.tiles >= (1 << 23)) return QCONV_EUNSUPPORTED;
+  const size_t lds = (size_t)rows * (ceil_div(a.rank, 32) * 8 + 1) * 16;
+  const unsigned blocks = (unsigned)(pieces * a.tiles);
+  if (rows == 32) lora_expand_kernel<T, 2><<<blocks, 256, lds, s>>>(a);
+  else lora_expand_kernel<T, 1><<<blocks, 256, lds, s>>>(a);
+  return hip_status();
+}
+
+// Tokens of a piece of a weight gradient.
+constexpr int GRAD_ROWS = 512;
+size_t grad_bytes(const qconv_lora_desc& d) {
+  const int64_t a = (int64_t)d.rank * round_up(d.k, 4), b = (int64_t)d.n * round_up(d.rank, 4);
+  return d.m > GRAD_ROWS ? (size_t)2 * ceil_div(d.m, GRAD_ROWS) * (a > b ? a : b) * 4 : 0;
+}
+template <class T, int RT, bool FLIP>
+int run_grad_t(LoraArgs& a, hipStream_t s) {
+  a.size = GRAD_ROWS;
+  a.tiles = ceil_div(a.len, 256);
+  a.ld_part = round_up(FLIP ? a.rank : a.len, 4);
+  const int64_t blocks = ((int64_t)a.g.rows / GRAD_ROWS + a.g.n) * a.tiles * ceil_div(a.rank, 64);
+  if (blocks >= (1 << 23)) return QCONV_EUNSUPPORTED;
+  lora_grad_kernel<T, RT, FLIP><<<(unsigned)blocks, 256, 0, s>>>(a);
+  if (a.g.rows > GRAD_ROWS) {
+    const int64_t n = (FLIP ? a.len : a.rank) * a.ld_part / 4;
+    const int several = a.g.rows / GRAD_ROWS < a.g.n ? a.g.rows / GRAD_ROWS : a.g.n;
+    const dim3 grid((unsigned)(n < (1 << 16) ? (n + 255) / 256 : 256), several);
+    lora_grad_join_kernel<T, FLIP><<<grid, 256, 0, s>>>(a);
+  }
+  return hip_status();
+}
+template <class T, bool FLIP>
+int run_grad(LoraArgs& a, hipStream_t s) {
+  return a.rank <= 16 ? run_grad_t<T, 1, FLIP>(a, s) : a.rank <= 32 ? run_grad_t<T, 2, FLIP>(a, s) : run_grad_t<T, 4, FLIP>(a, s);
+}
+
+int run_transpose(const void* w, int groups, int rows, int cols, uint16_t* out, int64_t ld_out, hipStream_t s) {
+  const int tr = ceil_div(rows, 64), tc = ceil_div(cols, 64);
+  const int64_t blocks = (int64_t)groups * tr * tc;
+  if (blocks >= (1 << 23)) return QCONV_EUNSUPPORTED;
+  lora_transpose_kernel<<<(unsigned)blocks, 256, 0, s>>>((const uint16_t*)w, rows, cols, out, ld_out, tr, tc);
+  return hip_status();
+}
+
+int run_join(float* parts, int n_parts, const qconv_lora_desc& d, float* to, hipStream_t s) {
+  const int64_t n = (int64_t)d.m * ld_mid(d);
+  lora_join_kernel<<<(unsigned)(n < (1 << 20) ? (n / 4 + 255) / 256 : 1024), 256, 0, s>>>(parts, n, n_parts, to);
+  return hip_status();
+}
+
+template <class T>
+int forward(const qconv_lora_desc& d, LoraArgs a, const void* x, const void* wa, const void* wb, const void* y, void* out,
+            float* mid, void* ws, hipStream_t s) {
+  const int rows = piece_rows(d);
+  a.parts = shrink_parts(d, d.k);
+  a.len = d.k;
+  a.x = (const uint16_t*)x;
+  a.ld_x = d.ld_x;
+  a.w = {(const uint16_t*)wa, d.k, (int64_t)d.rank * d.k};
+  a.mid = a.parts == 1 && mid ? mid : (float*)ws;
+  int rc = run_shrink<T>(a, rows, s);
+  if (rc == QCONV_OK && mid && a.parts > 1) {
+    rc = run_join(a.mid, a.parts, d, mid, s);
+    a.mid = mid;
+    a.parts = 1;
+  }
+  a.len = d.n;
+  a.x = (const uint16_t*)y;
+  a.ld_x = d.ld_y;
+  a.w = {(const uint16_t*)wb, d.rank, (int64_t)d.n * d.rank};
+  a.out = (uint16_t*)out;
+  a.ld_out = d.ld_out;
+  return rc ? rc : run_expand<T>(a, rows, s);
+}
+
+struct BackBytes {
+  size_t bt, at, parts, p, grad;
+};
+BackBytes back_bytes(const qconv_lora_desc& d) {
+  BackBytes b;
+  b.bt = (size_t)round_up((int64_t)d.groups * d.rank * round_up(d.n, 8) * 2, 16);
+  b.at = (size_t)round_up((int64_t)d.groups * d.k * round_up(d.rank, 8) * 2, 16);
+  const int parts = shrink_parts(d, d.n);
+  b.parts = parts > 1 ? parts * mid_bytes(d) : 0;
+  b.p = mid_bytes(d);
+  b.grad = grad_bytes(d);
+  return b;
+}
+
+template <class T>
+int backward(const qconv_lora_desc& d, LoraArgs a, const void* x, const void* wa, const void* wb, const float* mid,
+             const void* gy, void* gx, void* ga, void* gb, void* ws, hipStream_t s) {
+  const BackBytes b = back_bytes(d);
+  uint16_t* bt = (uint16_t*)ws;
+  uint16_t* at = (uint16_t*)((char*)bt + b.bt);
+  float* parts = (float*)((char*)at + b.at);
+  float* p = (float*)((char*)parts + b.parts);
+  a.part = (float*)((char*)p + b.p);
+  int rc = QCONV_OK;
+  if (d.m > 0) {
+    const int64_t ld_bt = round_up(d.n, 8), ld_at = round_up(d.rank, 8);
+    rc = run_transpose(wb, d.groups, d.n, d.rank, bt, ld_bt, s);
+    if (rc) return rc;
+    a.parts = shrink_parts(d, d.n);
+    a.len = d.n;
+    a.x = (const uint16_t*)gy;
+    a.ld_x = d.ld_y;
+    a.w = {bt, ld_bt, (int64_t)d.rank * ld_bt};
+    a.mid = a.parts > 1 ? parts : p;
+    rc = run_shrink<T>(a, piece_rows(d), s);
+    if (rc) return rc;
+    if (a.parts > 1) rc = run_join(parts, a.parts, d, p, s);
+    if (rc) return rc;
+    a.mid = p;
+    a.parts = 1;
+    if (gx) {
+      rc = run_transpose(wa, d.groups, d.rank, d.k, at, ld_at, s);
+      if (rc) return rc;
+      a.len = d.k;
+      a.x = nullptr;
+      a.w = {at, ld_at, (int64_t)d.k * ld_at};
+      a.out = (uint16_t*)gx;
+      a.ld_out = d.k;
+      rc = run_expand<T>(a, piece_rows(d), s);
+      if (rc) return rc;
+    }
+  }
+  if (ga) {
+    a.mid = p;
+    a.len = d.k;
+    a.x = (const uint16_t*)x;
+    a.ld_x = d.ld_x;
+    a.out = (uint16_t*)ga;
+    rc = run_grad<T, false>(a, s);
+    if (rc) return rc;
+    a.mid = (float*)mid;
+    a.len = d.n;
+    a.x = (const uint16_t*)gy;
+    a.ld_x = d.ld_y;
+    a.out = (uint16_t*)gb;
+    rc = run_grad<T, true>(a, s);
+  }
+  return rc;
+}
+
+LoraArgs lora_args(const qconv_lora_desc& d, const int* offsets, const int* order, const float* scale) {
+  LoraArgs a = {};
+  a.g = {offsets, d.groups, d.m};
+  a.order = order;
+  a.scale = scale;
+  a.rank = d.rank;
+  a.ld_mid = ld_mid(d);
+  a.parts = 1;
+  return a;
+}
+
+}  // namespace
+
+size_t lora_forward_bytes(const qconv_lora_desc& d, bool keep_mid) {
+  const int parts = shrink_parts(d, d.k);
+  return keep_mid && parts == 1 ? 0 : parts * mid_bytes(d);
+}
+
+int launch_lora_forward(const qconv_lora_desc& d, const void* x, const void* wa, const void* wb, const int* offsets,
+                        const int* order, const float* scale, const void* y, void* out, float* mid, void* ws,
+                        hipStream_t s) {
+  if (d.m == 0) return QCONV_OK;
+  const LoraArgs a = lora_args(d, offsets, order, scale);
+  return d.dtype == QCONV_F16 ? forward<F16>(d, a, x, wa, wb, y, out, mid, ws, s)
+                              : forward<BF16>(d, a, x, wa, wb, y, out, mid, ws, s);
+}
+
+size_t lora_backward_bytes(const qconv_lora_desc& d) {
+  const BackBytes b = back_bytes(d);
+  return b.bt + b.at + b.parts + b.p + b.grad;
+}
+
+int launch_lora_backward(const qconv_lora_desc& d, const void* x, const void* wa, const void* wb, const int* offsets,
+                         const int* order, const float* scale, const float* mid, const void* gy, void* gx, void* ga,
+                         void* gb, void* ws, hipStream_t s) {
+  const LoraArgs a = lora_args(d, offsets, order, scale);
+  return d.dtype == QCONV_F16 ? backward<F16>(d, a, x, wa, wb, mid, gy, gx, ga, gb, ws, s)
+                              : backward<BF16>(d, a, x, wa, wb, mid, gy, gx, ga, gb, ws, s);
+}
+
+}  // namespace qc

@@ -28,4 +28,13 @@ size_t moe_backward_bytes(const qconv_moe_desc& d, bool gated);
 int launch_moe_backward(const qconv_moe_desc& d, const void* x, const void* wg, const void* wu, const int* offsets,
                         const float* pre, const void* gh, void* gx, void* gwg, void* gwu, void* ws, hipStream_t s);
 
+size_t lora_forward_bytes(const qconv_lora_desc& d, bool keep_mid);
+int launch_lora_forward(const qconv_lora_desc& d, const void* x, const void* wa, const void* wb, const int* offsets,
+                        const int* order, const float* scale, const void* y, void* out, float* mid, void* ws,
+                        hipStream_t s);
+size_t lora_backward_bytes(const qconv_lora_desc& d);
+int launch_lora_backward(const qconv_lora_desc& d, const void* x, const void* wa, const void* wb, const int* offsets,
+                         const int* order, const float* scale, const float* mid, const void* gy, void* gx, void* ga,
+                         void* gb, void* ws, hipStream_t s);
+
 }  // namespace qc

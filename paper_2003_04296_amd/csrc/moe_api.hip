@@ -66,6 +66,23 @@ int check_backward(const qconv_moe_desc* d, bool gated, const void* x, const voi
   return workspace_bytes < need ? QCONV_EWORKSPACE : QCONV_OK;
 }
 
+int check_lora(const qconv_lora_desc* d, bool out) {
+  if (!d || d->m < 0 || d->rank < 1 || d->k < 1 || d->n < 1 || !any_type(d->dtype) || d->ld_x < d->k ||
+      d->ld_y < d->n || (out && d->ld_out < d->n) || d->ld_x > MAX_LD || d->ld_y > MAX_LD || (out && d->ld_out > MAX_LD))
+    return QCONV_EINVAL;
+  const int rc = check_groups(d->groups);
+  if (rc) return rc;
+  if (!half_type(d->dtype) || d->rank > QCONV_LORA_RANK_MOST || d->m > MOST || d->k > MOST || d->n > MOST)
+    return QCONV_EUNSUPPORTED;
+  return QCONV_OK;
+}
+// Adapters, their tokens and scales.
+bool lora_inputs(const qconv_lora_desc* d, const void* x, const void* a, const void* b, const int32_t* offsets,
+                 const int32_t* order, const float* scale, const void* y) {
+  return a && b && offsets && (d->m == 0 || (x && order && y)) && at(x, 2) && at(a, 2) && at(b, 2) && at(y, 2) &&
+         at(offsets, 4) && at(order, 4) && at(scale, 4);
+}
+
 }  // namespace
 
 extern "C" {
@@ -163,6 +180,45 @@ int qconv_moe_linear_backward(const qconv_moe_desc* d, const void* x, const void
   rc = check_backward(d, false, x, w, offsets, gy, gx, gw, workspace, workspace_bytes);
   return rc ? rc : launch_moe_backward(*d, x, w, nullptr, offsets, nullptr, gy, gx, gw, nullptr, workspace,
                                        (hipStream_t)stream);
+}
+
+size_t qconv_lora_mid_floats(int m, int rank) {
+  if (m < 0 || rank < 1 || rank > QCONV_LORA_RANK_MOST) return 0;
+  return (size_t)m * round_up(rank, 4);
+}
+
+size_t qconv_lora_forward_bytes(const qconv_lora_desc* d, int keep_mid) {
+  return check_lora(d, true) ? 0 : lora_forward_bytes(*d, keep_mid != 0);
+}
+
+int qconv_lora_forward(const qconv_lora_desc* d, const void* x, const void* a, const void* b, const int32_t* offsets,
+                       const int32_t* order, const float* scale, const void* y, void* out, float* mid,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_lora(d, true);
+  if (rc) return rc;
+  if (!lora_inputs(d, x, a, b, offsets, order, scale, y) || (d->m > 0 && !out) || !at(out, 2) || !at(mid, 16) ||
+      !at(workspace, 16) || (out && out == y && d->ld_out != d->ld_y))
+    return QCONV_EINVAL;
+  const size_t need = lora_forward_bytes(*d, mid != nullptr);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  return launch_lora_forward(*d, x, a, b, offsets, order, scale, y, out, mid, workspace, (hipStream_t)stream);
+}
+
+size_t qconv_lora_backward_bytes(const qconv_lora_desc* d) { return check_lora(d, false) ? 0 : lora_backward_bytes(*d); }
+
+int qconv_lora_backward(const qconv_lora_desc* d, const void* x, const void* a, const void* b, const int32_t* offsets,
+                        const int32_t* order, const float* scale, const float* mid, const void* gy, void* gx, void* ga,
+                        void* gb, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_lora(d, false);
+  if (rc) return rc;
+  if (!lora_inputs(d, x, a, b, offsets, order, scale, gy) || !ga != !gb || (d->m > 0 && ga && !mid) || !at(gx, 2) ||
+      !at(ga, 2) || !at(gb, 2) || !at(mid, 16) || !at(workspace, 16))
+    return QCONV_EINVAL;
+  const size_t need = lora_backward_bytes(*d);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  return launch_lora_backward(*d, x, a, b, offsets, order, scale, mid, gy, gx, ga, gb, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

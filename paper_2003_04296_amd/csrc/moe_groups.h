@@ -35,18 +35,24 @@ __device__ __forceinline__ int wave_sums(int v) {
 // The pieces of `size` rows that the groups' rows fall into, numbered group
 // after group: the host, which does not know the offsets, launches most() of them
 // and a block looks its piece up by itself (each wave; a load and a sum over the
-// lanes for every 64 groups, about 1 us).
+// lanes for every 64 groups, about 1 us).  With `empty` a group without rows has a
+// piece, too; with `several` only groups of more than one piece count, as one.
 struct GroupPieces {
   static int64_t most(int rows, int groups, int size) { return rows / size + (groups < rows ? groups : rows); }
 
   int size, per;  // groups per lane
+  bool empty, several;
   int upto;       // pieces of the groups up to and with this lane's
   int total;
 
   __device__ __forceinline__ int of(const Groups& g, int e) const {
-    return e < g.n ? (group_rows(g, e).count + size - 1) / size : 0;
+    if (e >= g.n) return 0;
+    const int rows = group_rows(g, e).count;
+    if (several) return rows > size ? 1 : 0;
+    return rows > 0 ? (int)(((int64_t)rows + size - 1) / size) : empty ? 1 : 0;
   }
-  __device__ __forceinline__ GroupPieces(const Groups& g, int size_) : size(size_) {
+  __device__ __forceinline__ GroupPieces(const Groups& g, int size_, bool empty_ = false, bool several_ = false)
+      : size(size_), empty(empty_), several(several_) {
     const int lane = threadIdx.x & 63;
     per = (g.n + 63) / 64;
     int mine = 0;

@@ -124,3 +124,61 @@ def test_host_tensors_are_refused():
                 lambda: q.moe_gated_backward(x, w, w, offsets, pre, h), lambda: q.moe_linear_backward(x, w, offsets, h)):
         with pytest.raises(ValueError):
             bad()
+
+
+def _lora(m=4, groups=3, rank=8, k=16, n=24, dtype=q.DT_BF16, ld_x=16, ld_y=24, ld_out=24):
+    return ctypes.byref(q.qconv_lora_desc(m, groups, rank, k, n, dtype, ld_x, ld_y, ld_out))
+
+
+@pytest.mark.parametrize("bad", [dict(m=-1), dict(groups=0), dict(rank=0), dict(k=0), dict(n=0), dict(dtype=3), dict(ld_x=15),
+                                 dict(ld_y=23), dict(ld_x=1 << 62)])
+def test_lora_descriptors(bad):
+    L, d = q.lib(), _lora(**bad)
+    assert L.qconv_lora_forward(d, P, P, P, P, P, P, P, P, P, P, 1 << 40, None) == q.QCONV_EINVAL
+    assert L.qconv_lora_backward(d, P, P, P, P, P, P, P, P, P, P, P, P, 1 << 40, None) == q.QCONV_EINVAL
+    assert L.qconv_lora_forward_bytes(d, 0) == 0 and L.qconv_lora_backward_bytes(d) == 0
+
+
+def test_lora_pointers_and_sizes():
+    L = q.lib()
+    for bad in (dict(dtype=q.DT_F32), dict(rank=257), dict(groups=4097)):
+        assert L.qconv_lora_forward(_lora(**bad), P, P, P, P, P, P, P, P, P, P, 1 << 40, None) == q.QCONV_EUNSUPPORTED, bad
+        assert L.qconv_lora_backward(_lora(**bad), P, P, P, P, P, P, P, P, P, P, P, P, 1 << 40, None) == q.QCONV_EUNSUPPORTED
+    ok = [P] * 9  # x, a, b, offsets, order, scale, y, out, mid
+    for i in range(9):
+        for v in (None, P + 1):
+            if v is None and i in (5, 8):
+                continue
+            a = list(ok)
+            a[i] = v
+            assert L.qconv_lora_forward(_lora(), *a, P, 1 << 40, None) == q.QCONV_EINVAL, (i, v)
+    assert L.qconv_lora_forward(_lora(ld_out=25), *ok, P, 1 << 40, None) == q.QCONV_EINVAL  # y itself, by another stride
+    assert L.qconv_lora_forward(_lora(ld_out=23), *ok, P, 1 << 40, None) == q.QCONV_EINVAL
+    need = L.qconv_lora_forward_bytes(_lora(), 0)
+    assert need > 0
+    assert L.qconv_lora_forward(_lora(), *ok[:8], None, P, need - 1, None) == q.QCONV_EWORKSPACE
+    assert L.qconv_lora_forward(_lora(), *ok[:8], None, None, need, None) == q.QCONV_EINVAL
+    assert L.qconv_lora_forward(_lora(), *ok[:8], None, P + 8, need, None) == q.QCONV_EINVAL
+    ok = [P] * 11  # x, a, b, offsets, order, scale, mid, gy, gx, ga, gb
+    for i in range(11):
+        for v in (None, P + 1):
+            if v is None and i in (5, 8):
+                continue
+            a = list(ok)
+            a[i] = v
+            assert L.qconv_lora_backward(_lora(), *a, P, 1 << 40, None) == q.QCONV_EINVAL, (i, v)
+    need = L.qconv_lora_backward_bytes(_lora())
+    assert need > 0 and L.qconv_lora_backward(_lora(), *ok, P, need - 1, None) == q.QCONV_EWORKSPACE
+    assert L.qconv_lora_backward(_lora(), *ok, None, need, None) == q.QCONV_EINVAL
+    assert L.qconv_lora_forward(_lora(m=0), None, P, P, P, None, None, None, None, None, None, 0, None) == q.QCONV_OK
+    assert L.qconv_lora_mid_floats(3, 9) == 36 and L.qconv_lora_mid_floats(-1, 9) == 0 and L.qconv_lora_mid_floats(3, 300) == 0
+
+
+def test_lora_host_tensors_are_refused():
+    x, y = torch.zeros((4, 16), dtype=torch.float16), torch.zeros((4, 24), dtype=torch.float16)
+    a, b = torch.zeros((3, 8, 16), dtype=torch.float16), torch.zeros((3, 24, 8), dtype=torch.float16)
+    ids = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        q.lora_forward(y, x, a, b, ids, ids)
+    with pytest.raises(ValueError):
+        q.lora_backward(x, a, b, ids, ids, torch.zeros(32), y)

@@ -46,11 +46,10 @@ template <class T, class SR, class SC, int B>
 __global__ __launch_bounds__(B / 64 * 128) void moe_gemm_w_kernel(GemmArgs a, Groups g, int64_t step_out) {
   [[maybe_unused]] __shared__ v4u lds[STAGES<SR::KS> * (B + B) * SR::CPR];
 #ifdef __HIP_DEVICE_COMPILE__
-  // the tile rows of one expert follow those of another
-  const uint32_t per = a.tiles_r * a.halves;
-  TileAt at = tile_at(blockIdx.x, per * g.n, a.tiles_c);
-  const int e = at.r / per;
-  at.r -= e * per;
+  // one expert after the other, each over all dies: the experts' sums differ in length
+  const uint32_t per = a.tiles_r * a.halves, all = per * a.tiles_c;
+  const int e = blockIdx.x / all;
+  const TileAt at = tile_at(blockIdx.x % all, per, a.tiles_c);
   const GroupRows rows = group_rows(g, e);
   const int64_t first = __builtin_amdgcn_readfirstlane(rows.first);
 #pragma unroll

@@ -27,7 +27,7 @@ struct SortArgs {
   int64_t ld;
   int n, groups;
   int chunk;        // ids per block
-  int* hist;        // [blocks][groups + 1]
+  int* hist;        // [groups + 1][blocks]: ids of each key in each block
   int *offsets, *order, *place;
 };
 
@@ -89,21 +89,21 @@ __global__ __launch_bounds__(1024) void moe_count_kernel(SortArgs a) {
   const int64_t b = (int64_t)blockIdx.x * a.chunk, e = b + a.chunk < a.n ? b + a.chunk : a.n;
   for (int64_t i = b + threadIdx.x; i < e; i += 1024) atomicAdd(&cnt[sort_key(a, (int)i)], 1);
   __syncthreads();
-  int* h = a.hist + (int64_t)blockIdx.x * (a.groups + 1);
-  for (int g = threadIdx.x; g <= a.groups; g += 1024) h[g] = cnt[g];
+  for (int g = threadIdx.x; g <= a.groups; g += 1024) a.hist[(int64_t)g * gridDim.x + blockIdx.x] = cnt[g];
 }
 
 // Ranks a block's ids and writes order, place and (the first block) offsets.
 // Each wave owns a run of the ids and counts of its own in LDS, so that ranks
 // follow the ids' order whatever the waves' timing: the sums over earlier blocks
-// (from their counts, which every block reads: at most 2^17 words), earlier
+// (from their counts, which every block reads: at most 2^17 words, a key's in a
+// row), earlier
 // waves and smaller keys are the start of a wave's rows of a key.
 // Bound by latency: 32768 x 8 ids move 4 MB.
 template <int NW, int BUCKETS>
 __global__ __launch_bounds__(NW * 64) void moe_rank_kernel(SortArgs a) {
   constexpr int NT = NW * 64;
   __shared__ int cnt[NW][BUCKETS];
-  __shared__ int base[BUCKETS];
+  __shared__ int base[BUCKETS], start[BUCKETS];
   __shared__ int tmp[NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int buckets = a.groups + 1, bits = 32 - __clz(a.groups);
@@ -116,28 +116,48 @@ __global__ __launch_bounds__(NW * 64) void moe_rank_kernel(SortArgs a) {
   const int b = wave * run < here ? wave * run : here, e = b + run < here ? b + run : here;
   for (int i = b + lane; i < e; i += 64) atomicAdd(&cnt[wave][sort_key(a, (int)first + i)], 1);
   __syncthreads();
-  // per key: the rows of earlier waves; in base all rows of the key
-  for (int g = threadIdx.x; g < buckets; g += NT) {
-    int before = 0, total = 0;
-    if (a.hist) {
-      const int blocks = gridDim.x;
-      for (int k = 0; k < blocks; ++k) {
-        const int h = a.hist[(int64_t)k * buckets + g];
+  // per key: in base all its rows, in start those of earlier blocks.  `span`
+  // lanes sum the blocks' counts of one key.
+  if (a.hist) {
+    const int blocks = gridDim.x;
+    int span = 8;
+    while (span < 64 && span < blocks) span *= 2;
+    const int in = lane & (span - 1);
+    for (int g0 = wave * (64 / span); g0 < buckets; g0 += NT / span) {
+      const int g = g0 + lane / span;
+      int before = 0, total = 0;
+      for (int k = in; k < blocks; k += span) {
+        const int h = g < buckets ? a.hist[(int64_t)g * blocks + k] : 0;
         before += k < (int)blockIdx.x ? h : 0;
         total += h;
       }
+      for (int d = 1; d < span; d <<= 1) {
+        before += __shfl_xor(before, d);
+        total += __shfl_xor(total, d);
+      }
+      if (in == 0 && g < buckets) {
+        base[g] = total;
+        start[g] = before;
+      }
     }
-    for (int w = 0; w < NW; ++w) {
-      const int c = cnt[w][g];
-      cnt[w][g] = before;
-      before += c;
+  } else {
+    for (int g = threadIdx.x; g < buckets; g += NT) {
+      int total = 0;
+      for (int w = 0; w < NW; ++w) total += cnt[w][g];
+      base[g] = total;
+      start[g] = 0;
     }
-    base[g] = a.hist ? total : before;
   }
   __syncthreads();
   block_scan<NT>(base, buckets, tmp);
-  for (int g = threadIdx.x; g < buckets; g += NT)
-    for (int w = 0; w < NW; ++w) cnt[w][g] += base[g];
+  for (int g = threadIdx.x; g < buckets; g += NT) {
+    int at = base[g] + start[g];
+    for (int w = 0; w < NW; ++w) {
+      const int c = cnt[w][g];
+      cnt[w][g] = at;
+      at += c;
+    }
+  }
   if (blockIdx.x == 0)
     for (int g = threadIdx.x; g < buckets; g += NT) a.offsets[g] = base[g];
   __syncthreads();
@@ -435,7 +455,7 @@ int launch_moe_sort(const void* ids, int wide, int tokens, int slots, int64_t ld
   else if (groups < 1024)
     moe_rank_kernel<16, 1024><<<blocks, 1024, 0, s>>>(a);
   else
-    moe_rank_kernel<8, MOE_GROUPS_MOST + 1><<<blocks, 512, 0, s>>>(a);
+    moe_rank_kernel<4, MOE_GROUPS_MOST + 1><<<blocks, 256, 0, s>>>(a);
   return hip_status();
 }
 

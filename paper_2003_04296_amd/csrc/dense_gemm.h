@@ -54,10 +54,11 @@ struct GemmArgs {
   int ld_pre;
   int act;
   // the products of a tile split over `parts` blocks: fp32 sums go to
-  // part[parts][2 or halves][rows][ld_part], joined by dense_join_kernel
+  // part[parts][2 or halves][part_rows][ld_part] (NULL: to out), joined by
+  // dense_join_kernel
   int parts;
   float* part;
-  int ld_part;
+  int part_rows, ld_part;
 };
 
 // LDS holds chunks of 16 bytes; a stage holds KS products (32 or 64) of every
@@ -666,11 +667,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, lds_v4u* const lds,
   auto put = [&](auto act, int i, int j, v4f v[2]) {
     const int64_t r = r0 + wr + j * 16 + (lane & 15), c = c1 + i * 16;
     if (r >= a.rows || c >= a.cols) return;
-    if (a.parts > 1) {
+    if (a.part) {
 #pragma unroll
       for (int h = 0; h < H; ++h) {
         const int64_t plane = (int64_t)part * (PAIR ? 2 : a.halves) + (PAIR ? h : half);
-        *(v4f*)(a.part + (plane * a.rows + r) * a.ld_part + c) = v[h];
+        *(v4f*)(a.part + (plane * a.part_rows + r) * a.ld_part + c) = v[h];
       }
     } else {
       finish4<T, OUT, decltype(act)::value>(a, half, r, c, v);
@@ -742,7 +743,7 @@ __device__ __forceinline__ void join(const GemmArgs& a) {
     const int64_t row = i / q;  // of both halves
     const int half = row >= a.rows;
     const int64_t c = i % q * 4;
-    const int64_t plane = (int64_t)a.rows * a.ld_part, step = plane * (OUT == OUT_GATED ? 2 : a.halves);
+    const int64_t plane = (int64_t)a.part_rows * a.ld_part, step = plane * (OUT == OUT_GATED ? 2 : a.halves);
     v4f v[2] = {};
 #pragma unroll
     for (int h = 0; h < H; ++h) {
@@ -875,6 +876,8 @@ int run_gemm_tiles(GemmArgs& a, hipStream_t s) {
   a.tiles_c = ceil_div(a.cols, OUT == OUT_GATED ? B / 2 : B);
   const int64_t blocks = (int64_t)a.tiles_r * a.tiles_c * a.halves * a.parts;
   if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;  // 2^31 threads
+  if (a.parts == 1) a.part = nullptr;
+  a.part_rows = a.rows;
   a.ld_part = (int)round_up(a.cols, 4);
   a.wide_out = a.ld_out % 4 == 0 && ((uintptr_t)a.out[0] & 7) == 0 && ((uintptr_t)a.out[1] & 7) == 0;
   dense_gemm_kernel<T, SR, SC, OUT, B, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a);

@@ -185,17 +185,14 @@ struct RowsBlock {
 // A pass is NW blocks of 128 inputs, one per wave.  Its x lies in LDS, put
 // there by all waves in whole rows; the next pass's x and weights are on their
 // way into registers while it is multiplied.
+constexpr int rows_ld(int nw) { return nw * 128 + 8; }  // + 8: the tokens' values in different banks
+// Output tile nt and token tile mt; xs: 16 * MT rows of LDS, at the end the waves' sums.
 template <class T, class W, int H, int MT, int NW>
-__global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
-  constexpr int PASS = NW * 128, LD = PASS + 8, WPT = PASS / 512, STEP = NW / WPT, PER = 16 * MT / STEP;
-  __shared__ v4u xs[16 * MT * LD / 8];  // at the end: the waves' sums
+__device__ __forceinline__ void dense_rows_tile(const RowsArgs& a, v4u (&xs)[16 * MT * rows_ld(NW) / 8], int nt, int mt) {
+  constexpr int PASS = NW * 128, LD = rows_ld(NW), WPT = PASS / 512, STEP = NW / WPT, PER = 16 * MT / STEP;
   static_assert(sizeof(xs) >= sizeof(float) * NW * H * MT * 256, "sums fit");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, o = lane >> 4;
-  // workgroups go to the 8 dies in turn: the token tiles of one set of outputs
-  // follow each other on one die, whose L2 then holds their weights
-  const int nt = blockIdx.x / (8 * a.tiles_m) * 8 + blockIdx.x % 8, mt = blockIdx.x / 8 % a.tiles_m;
-  if (nt >= a.tiles_n) return;
   const int n0 = nt * 16, m0 = mt * 16 * MT;
   const int64_t row = n0 + r < a.n ? n0 + r : 0;
   v4f acc[H][MT];
@@ -262,6 +259,16 @@ __global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
     }
     a.y[(int64_t)m * a.ld_y + n] = T::down(y);
   }
+}
+
+template <class T, class W, int H, int MT, int NW>
+__global__ __launch_bounds__(NW * 64) void dense_rows_kernel(RowsArgs a) {
+  __shared__ v4u xs[16 * MT * rows_ld(NW) / 8];
+  // workgroups go to the 8 dies in turn: the token tiles of one set of outputs
+  // follow each other on one die, whose L2 then holds their weights
+  const int nt = blockIdx.x / (8 * a.tiles_m) * 8 + blockIdx.x % 8, mt = blockIdx.x / 8 % a.tiles_m;
+  if (nt >= a.tiles_n) return;
+  dense_rows_tile<T, W, H, MT, NW>(a, xs, nt, mt);
 }
 
 // The end of the kernels for at most 4 tokens: thread i < M * 16 joins the

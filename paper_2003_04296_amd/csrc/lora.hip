@@ -307,16 +307,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
 
 // Rows of an adapter are taken `size` at a time; a block has 256 columns of a
 // piece and 64 ranks.  The sums of an adapter with one piece (or none: zeros) are
-// results; others go to part, where the piece that starts at row s has its place
-// by s: pieces of one adapter start `size` rows apart, so at most two of several
-// start in the same `size` rows, and of these one is an adapter's first.
-__device__ __forceinline__ int pieces_of(const GroupRows& r, int size) {
-  return r.count > size ? (r.count + size - 1) / size : 1;
-}
-__device__ __forceinline__ int64_t part_at(int first, int piece, int size) {
-  return 2 * ((int64_t)first / size + piece) + (piece == 0 ? 1 : 0);
-}
-
+// results; others go to part.
 // Writes 4 values of a row of a gradient.
 template <class T>
 __device__ __forceinline__ void put_grad(const LoraArgs& a, int e, int rows, int cols, int row, int col, v4f v) {
@@ -425,7 +416,7 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
   }
   const bool whole = rows.count <= a.size;
   const int nr = FLIP ? a.len : a.rank, nc = FLIP ? a.rank : a.len;
-  float* const to = a.part + part_at(rows.first, piece, a.size) * nr * a.ld_part;
+  float* const to = a.part + group_part(rows.first, piece, a.size) * nr * a.ld_part;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -442,19 +433,19 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
 // Joins the pieces of the adapters that have several: the y-th of them.
 template <class T, bool FLIP>
 __global__ __launch_bounds__(256) void lora_grad_join_kernel(LoraArgs a) {
-  const GroupPieces several(a.g, a.size, true, true);
+  const GroupPieces several(a.g, a.size, false, true);
   if ((int)blockIdx.y >= several.total) return;
   int e, unused;
   several.find(a.g, blockIdx.y, e, unused);
   const GroupRows rows = group_rows(a.g, e);
-  const int n = pieces_of(rows, a.size);
+  const int n = (rows.count - 1) / a.size + 1;
   const int nr = FLIP ? a.len : a.rank, nc = FLIP ? a.rank : a.len, per = (int)(a.ld_part / 4);
   const int64_t all = (int64_t)nr * per, plane = nr * a.ld_part;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int row = (int)(i / per), col = (int)(i % per) * 4;
     v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int p = 0; p < n; ++p) s += *(const v4f*)(a.part + part_at(rows.first, p, a.size) * plane + row * a.ld_part + col);
+    for (int p = 0; p < n; ++p) s += *(const v4f*)(a.part + group_part(rows.first, p, a.size) * plane + row * a.ld_part + col);
     put_grad<T>(a, e, nr, nc, row, col, s);
   }
 }

@@ -5,6 +5,7 @@
 // One launch per product for all experts, on the tiles of dense_gemm.h: a block
 // finds its expert and rows from the offsets, which stay on the device.
 #include "dense_ffn.h"
+#include "dense_rows.h"
 #include "moe.h"
 #include "moe_groups.h"
 
@@ -20,8 +21,11 @@ __global__ __launch_bounds__(B / 64 * 128) void moe_gemm_kernel(GemmArgs a, Grou
   [[maybe_unused]] __shared__ v4u lds[STAGES<SR::KS> * (B + B) * SR::CPR];
 #ifdef __HIP_DEVICE_COMPILE__  // the host has no LDS pointers
   const GroupPieces pieces(g, B);
-  if (blockIdx.x >= (uint64_t)pieces.total * a.tiles_c) return;
-  TileAt at = tile_at(blockIdx.x, pieces.total, a.tiles_c);
+  const uint32_t all = (uint32_t)pieces.total * a.tiles_c;
+  // the parts of one tile lie `blocks` launched tiles apart
+  const uint32_t blocks = gridDim.x / a.parts, part = blockIdx.x / blocks, id = blockIdx.x % blocks;
+  if (id >= all) return;
+  TileAt at = tile_at(id, pieces.total, a.tiles_c);
   int e, piece;
   pieces.find(g, at.r, e, piece);
   const GroupRows rows = group_rows(g, e);
@@ -34,94 +38,228 @@ __global__ __launch_bounds__(B / 64 * 128) void moe_gemm_kernel(GemmArgs a, Grou
   a.rows = __builtin_amdgcn_readfirstlane(rows.count);
   a.out[0] = (uint16_t*)a.out[0] + first * a.ld_out;
   if (OUT == OUT_GATED && a.pre) a.pre += first * 2 * a.ld_pre;
+  if (a.part) a.part += first * a.ld_part;
   at.r = piece;
   a.tiles_r = 0x7fffffff;  // one half
-  gemm_tile<T, SR, SC, OUT, B, B>(a, (lds_v4u*)lds, at, 0);
+  gemm_tile<T, SR, SC, OUT, B, B>(a, (lds_v4u*)lds, at, part);
 #endif
 }
 
+// The join of split products, for the rows that groups have.
+template <class T, int OUT>
+__global__ __launch_bounds__(256) void moe_join_kernel(GemmArgs a, Groups g) {
+  const int first = g.offsets[0] < 0 ? 0 : g.offsets[0], end = g.offsets[g.n] < g.rows ? g.offsets[g.n] : g.rows;
+  a.rows = end - first;
+  a.part += (int64_t)first * a.ld_part;
+  a.out[0] = (uint16_t*)a.out[0] + first * a.ld_out;
+  if (OUT == OUT_GATED && a.pre) a.pre += (int64_t)first * 2 * a.ld_pre;
+  with_act(OUT == OUT_GATED ? a.act : 0, [&](auto act) { join<T, OUT, decltype(act)::value>(a); });
+}
+
 // The products over the batch's rows (weight gradients): a.rows and a.cols are
-// the weight's.
+// the weight's.  An expert's rows are taken `size` at a time, so that experts of
+// unequal share, or few of them, fill the chip; sums of an expert with several such
+// pieces go to a.part.
 template <class T, class SR, class SC, int B>
-__global__ __launch_bounds__(B / 64 * 128) void moe_gemm_w_kernel(GemmArgs a, Groups g, int64_t step_out) {
+__global__ __launch_bounds__(B / 64 * 128) void moe_gemm_w_kernel(GemmArgs a, Groups g, int size, int uncut, int64_t step_out) {
   [[maybe_unused]] __shared__ v4u lds[STAGES<SR::KS> * (B + B) * SR::CPR];
 #ifdef __HIP_DEVICE_COMPILE__
-  // one expert after the other, each over all dies: the experts' sums differ in length
+  // one piece after the other, each over all dies: their sums differ in length
   const uint32_t per = a.tiles_r * a.halves, all = per * a.tiles_c;
-  const int e = blockIdx.x / all;
+  size = group_size(g, size, uncut);
+  const GroupPieces pieces(g, size, true);
+  const int p = blockIdx.x / all;
+  if (p >= pieces.total) return;
   const TileAt at = tile_at(blockIdx.x % all, per, a.tiles_c);
+  int e, piece;
+  pieces.find(g, p, e, piece);
   const GroupRows rows = group_rows(g, e);
-  const int64_t first = __builtin_amdgcn_readfirstlane(rows.first);
+  const int64_t begin = (int64_t)piece * size, first = __builtin_amdgcn_readfirstlane(rows.first) + begin;
+  const int count = __builtin_amdgcn_readfirstlane(rows.count);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     a.r[i].p += first * a.r[i].ld;
     a.out[i] = (uint16_t*)a.out[i] + e * step_out;
   }
   a.c[0].p += first * a.c[0].ld;
-  a.k = __builtin_amdgcn_readfirstlane(rows.count);
+  a.k = count - begin < size ? count - (int)begin : size;
+  a.part = count > size ? a.part + group_part(first - begin, piece, size) * a.halves * a.part_rows * a.ld_part : nullptr;
   gemm_tile<T, SR, SC, OUT_PLAIN, B, B>(a, (lds_v4u*)lds, at, 0);
 #endif
+}
+
+// The join of the experts' pieces: blockIdx.y counts the experts with several.
+template <class T>
+__global__ __launch_bounds__(256) void moe_join_w_kernel(GemmArgs a, Groups g, int size, int uncut, int64_t step_out) {
+  size = group_size(g, size, uncut);
+  const GroupPieces several(g, size, false, true);
+  if ((int)blockIdx.y >= several.total) return;
+  int e, unused;
+  several.find(g, blockIdx.y, e, unused);
+  const GroupRows rows = group_rows(g, e);
+  const int n = (rows.count - 1) / size + 1, q = a.ld_part / 4;
+  const int64_t plane = (int64_t)a.part_rows * a.ld_part;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.halves * a.part_rows * q; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / q;  // of both halves
+    const int half = row >= a.part_rows, c = (int)(i % q) * 4;
+    v4f v[2] = {};
+#pragma unroll 4
+    for (int p = 0; p < n; ++p)
+      v[0] += *(const v4f*)(a.part + group_part(rows.first, p, size) * a.halves * plane + row * a.ld_part + c);
+    GemmArgs b = a;
+    b.out[0] = (uint16_t*)a.out[half] + e * step_out;
+    finish4<T, OUT_PLAIN, 0>(b, 0, row - half * (int64_t)a.part_rows, c, v);
+  }
+}
+
+// Few rows: the form of dense_rows.h, a block for 16 outputs and 16 rows of one
+// expert.
+template <class T, int H, int NW>
+__global__ __launch_bounds__(NW * 64) void moe_rows_kernel(RowsArgs a, Groups g, int64_t step_w) {
+  __shared__ v4u xs[16 * rows_ld(NW) / 8];
+  const GroupPieces pieces(g, 16);
+  // as in dense_rows_kernel, the pieces in place of the token tiles
+  const int many = pieces.total, nt = many ? blockIdx.x / (8 * many) * 8 + blockIdx.x % 8 : a.tiles_n;
+  if (nt >= a.tiles_n) return;
+  int e, piece;
+  pieces.find(g, blockIdx.x / 8 % many, e, piece);
+  const GroupRows rows = group_rows(g, e);
+  const int64_t first = __builtin_amdgcn_readfirstlane(rows.first);
+  a.m = __builtin_amdgcn_readfirstlane(rows.count);
+  a.x += first * a.ld_x;
+  a.y += first * a.ld_y;
+  if (a.pre) a.pre += first * 2 * a.ld_pre;
+#pragma unroll
+  for (int h = 0; h < H; ++h) a.w[h] = (const uint16_t*)a.w[h] + e * step_w;
+  dense_rows_tile<T, Dense16, H, 1, NW>(a, xs, nt, piece);
+}
+
+template <class T, int H>
+int run_few(RowsArgs& a, const Groups& g, int64_t step_w, hipStream_t s) {
+  constexpr int NW = 8;
+  a.tiles_n = ceil_div(a.n, 16);
+  const int64_t blocks = (int64_t)(a.tiles_n + 7) / 8 * 8 * GroupPieces::most(g.rows, g.n, 16);
+  if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;
+  moe_rows_kernel<T, H, NW><<<(unsigned)blocks, NW * 64, 0, s>>>(a, g, step_w);
+  return hip_status();
 }
 
 template <class T, class SR, class SC, int OUT, int B>
 int run_tiles(GemmArgs& a, const Groups& g, int64_t step_c, hipStream_t s) {
   a.tiles_c = ceil_div(a.cols, OUT == OUT_GATED ? B / 2 : B);
-  const int64_t blocks = GroupPieces::most(g.rows, g.n, B) * a.tiles_c;
+  const int64_t blocks = GroupPieces::most(g.rows, g.n, B) * a.tiles_c * a.parts;
   if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;  // 2^31 threads
+  a.rows = a.part_rows = g.rows;
+  a.ld_part = (int)round_up(a.cols, 4);
+  if (a.parts == 1) a.part = nullptr;
   a.wide_out = a.ld_out % 4 == 0 && ((uintptr_t)a.out[0] & 7) == 0;
   moe_gemm_kernel<T, SR, SC, OUT, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a, g, step_c);
+  if (a.parts > 1) {
+    const int64_t n = (int64_t)g.rows * (a.ld_part / 4);
+    moe_join_kernel<T, OUT><<<(unsigned)(n < (1 << 20) ? (n + 255) / 256 : 4096), 256, 0, s>>>(a, g);
+  }
   return hip_status();
 }
 template <class T, class SR, class SC, int B>
-int run_tiles_w(GemmArgs& a, const Groups& g, int64_t step_out, hipStream_t s) {
+int run_tiles_w(GemmArgs& a, const Groups& g, int size, int64_t step_out, hipStream_t s) {
+  // with a tile for each compute unit, an expert twice as long as a piece is not worth cutting
+  const int uncut = size < 0x3fffff00 && (int64_t)ceil_div(a.rows, 256) * ceil_div(a.cols, 256) * a.halves * g.n >= 256 ? 2 * size : size;
   a.tiles_r = ceil_div(a.rows, B);
   a.tiles_c = ceil_div(a.cols, B);
-  const int64_t blocks = (int64_t)a.tiles_r * a.halves * a.tiles_c * g.n;
+  const int64_t blocks = ((int64_t)g.rows / size + g.n) * a.tiles_r * a.halves * a.tiles_c;
   if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;
+  a.part_rows = a.rows;
+  a.ld_part = (int)round_up(a.cols, 4);
   a.wide_out = a.ld_out % 4 == 0 && ((uintptr_t)a.out[0] & 7) == 0 && ((uintptr_t)a.out[1] & 7) == 0;
-  moe_gemm_w_kernel<T, SR, SC, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a, g, step_out);
+  moe_gemm_w_kernel<T, SR, SC, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a, g, size, uncut, step_out);
+  if (g.rows > size) {
+    const int64_t n = (int64_t)a.halves * a.rows * (a.ld_part / 4);
+    const int several = g.rows / size < g.n ? g.rows / size : g.n;
+    moe_join_w_kernel<T><<<dim3((unsigned)(n < (1 << 17) ? (n + 255) / 256 : 512), several), 256, 0, s>>>(a, g, size, uncut, step_out);
+  }
   return hip_status();
 }
 
 // Rows of the batch by the weights' rows (CCOL false) or columns.
 template <class T, bool CCOL, int OUT>
-int run_rows_t(GemmArgs& a, const Groups& g, int64_t step_c, int tile, bool aligned, hipStream_t s) {
+int run_rows_t(GemmArgs& a, const Groups& g, int64_t step_c, const GemmPlan& p, bool aligned, hipStream_t s) {
+  a.parts = p.parts;
   constexpr bool PAIR = OUT == OUT_GATED;
   constexpr int KS = CCOL ? 32 : 64;
   if (!aligned)
     return run_tiles<T, Stage16<KS, 128, 256, 0, false, false, false>, Stage16<KS, 128, 256, 1, CCOL, false, PAIR>, OUT,
                      128>(a, g, step_c, s);
-  if (tile == 256)
+  if (p.tile == 256)
     return run_tiles<T, Stage16<KS, 256, 512, 0, false, true, false>, Stage16<KS, 256, 512, 1, CCOL, true, PAIR>, OUT,
                      256>(a, g, step_c, s);
   return run_tiles<T, Stage16<KS, 128, 256, 0, false, true, false>, Stage16<KS, 128, 256, 1, CCOL, true, PAIR>, OUT,
                    128>(a, g, step_c, s);
 }
 template <bool CCOL, int OUT>
-int run_rows(int dtype, GemmArgs& a, const Groups& g, int64_t step_c, int tile, bool aligned, hipStream_t s) {
-  return dtype == QCONV_F16 ? run_rows_t<F16, CCOL, OUT>(a, g, step_c, tile, aligned, s)
-                            : run_rows_t<BF16, CCOL, OUT>(a, g, step_c, tile, aligned, s);
+int run_rows(int dtype, GemmArgs& a, const Groups& g, int64_t step_c, const GemmPlan& p, bool aligned, hipStream_t s) {
+  return dtype == QCONV_F16 ? run_rows_t<F16, CCOL, OUT>(a, g, step_c, p, aligned, s)
+                            : run_rows_t<BF16, CCOL, OUT>(a, g, step_c, p, aligned, s);
 }
 template <class T>
-int run_weights_t(GemmArgs& a, const Groups& g, int64_t step_out, int tile, bool aligned, hipStream_t s) {
+int run_weights_t(GemmArgs& a, const Groups& g, int64_t step_out, int tile, int size, bool aligned, hipStream_t s) {
   if (!aligned)
     return run_tiles_w<T, Stage16<32, 128, 256, 0, true, false, false>, Stage16<32, 128, 256, 1, true, false, false>,
-                       128>(a, g, step_out, s);
+                       128>(a, g, size, step_out, s);
   if (tile == 256)
     return run_tiles_w<T, Stage16<32, 256, 512, 0, true, true, false>, Stage16<32, 256, 512, 1, true, true, false>,
-                       256>(a, g, step_out, s);
+                       256>(a, g, size, step_out, s);
   return run_tiles_w<T, Stage16<32, 128, 256, 0, true, true, false>, Stage16<32, 128, 256, 1, true, true, false>, 128>(
-      a, g, step_out, s);
+      a, g, size, step_out, s);
 }
 
-// Tiles of 256 x 256 where the experts' rows fill most of them and there are
-// enough for the 256 compute units, else 128 x 128.
-int tile_rows(const qconv_moe_desc& d, int cols, bool gated) {
-  const int64_t across = gated ? 128 : 256;
-  return d.rows >= 512 * (int64_t)d.groups && d.rows / 256 * ((cols + across - 1) / across) >= 256 ? 256 : 128;
+// The products whose rows are the batch's: tiles of 256 x 256 where there are
+// enough for the 256 compute units and the experts' rows, on average, fill three
+// quarters of one, else 128 x 128; few of those are split as in gemm_plan.
+GemmPlan plan_rows(const qconv_moe_desc& d, int cols, int64_t products, bool gated, bool aligned) {
+  auto tiles = [&](int b) {
+    const int64_t n = GroupPieces::most(d.rows, d.groups, b) * ceil_div(cols, gated ? b / 2 : b);
+    return n > 0 ? n : 1;
+  };
+  if (aligned && d.rows >= 192 * (int64_t)d.groups && tiles(256) >= 256) return {256, 1, 0};
+  const int64_t small = tiles(128);
+  int64_t parts = small >= 192 ? 1 : 256 / small;
+  if (parts > products / 512) parts = products / 512;
+  if (parts <= 1) return {128, 1, 0};
+  return {128, (int)parts, (size_t)parts * (gated ? 2 : 1) * d.rows * round_up(cols, 4) * 4};
 }
-int tile_weights(const qconv_moe_desc& d, int halves) {
-  return (int64_t)ceil_div(d.f, 256) * ceil_div(d.k, 256) * halves * d.groups >= 256 ? 256 : 128;
+
+// Weight gradients: the tile, and the rows of a piece.  Enough tiles: an expert's rows
+// are one piece.  Otherwise pieces make about twice as many tiles as fit the chip, or
+// more where experts are uneven, and are long enough to be worth their sums' way
+// through memory (8192 rows of 8 experts, 2048 -> 2048: 105 us whole, 121 in pieces of
+// 1536 rows; 32768 rows of 16, the largest with a fourth of them, 1024 -> 1024: 304 us
+// whole, 121 in pieces of 1536).
+struct PlanW {
+  int tile, size;
+  size_t bytes;
+};
+PlanW plan_weights(const qconv_moe_desc& d, bool gated, bool aligned) {
+  const int halves = gated ? 2 : 1;
+  auto tiles = [&](int b) { return (int64_t)ceil_div(d.f, b) * ceil_div(d.k, b) * halves; };
+  const int tile = aligned && tiles(256) * d.groups >= 256 ? 256 : 128;
+  const int64_t per = tiles(tile), slots = tile == 256 ? 256 : 512;
+  if (per * d.groups >= 4 * slots) return {tile, 0x7fffff00, 0};
+  int64_t size = round_up(d.rows * per / (2 * slots), 64);
+  const int least = tile == 256 ? 1536 : 512;
+  size = size < least ? least : size < 0x7fffff00 ? size : 0x7fffff00;
+  return {tile, (int)size, d.rows > size ? (size_t)(2 * ((d.rows + size - 1) / size) * halves * d.f * round_up(d.k, 4) * 4) : 0};
+}
+
+// The rows that go forward without tiles.  Tiles read the same weights through LDS
+// and are slower at it while there is less than a tile of rows for each expert; the
+// blocks without tiles read x for every 16 outputs.  us here and there, gated, weights
+// from memory (both with 10 us of a call's own):
+//   16 experts 2048 -> 4096   99 and 128 at 32 rows, 109 and 132 at 128, 136 and 132 at 256
+//   64 experts 2048 -> 1024   73 and 101 at 64, 106 and 131 at 256, 141 and 134 at 1024
+//   64 experts 512 -> 512     12.4 and 15.5 at 32, 17.4 and 16.6 at 64, 24 and 19 at 256
+bool few_rows(const qconv_moe_desc& d) {
+  const int many = d.k < 1024 ? 32 : 4 * d.groups;
+  return d.rows <= (d.k >= 1024 && many < 64 ? 64 : many);
 }
 
 // Operands off 16-byte rows are copied as in ffn.hip; the copies of all experts'
@@ -143,12 +281,34 @@ size_t factor_bytes(const qconv_moe_desc& d, bool gated) {
 
 }  // namespace
 
-size_t moe_forward_bytes(const qconv_moe_desc& d, bool gated) { return copies_bytes(d, gated, true); }
+size_t moe_forward_bytes(const qconv_moe_desc& d, bool gated) {
+  if (few_rows(d)) return 0;
+  const size_t p = plan_rows(d, d.f, d.k, gated, false).bytes, q = plan_rows(d, d.f, d.k, gated, true).bytes;
+  return copies_bytes(d, gated, true) + (p > q ? p : q);
+}
 
 int launch_moe_forward(const qconv_moe_desc& d, const void* x, const void* wg, const void* wu, const int* offsets,
                        void* h, float* pre, void* ws, hipStream_t s) {
   if (d.rows == 0) return QCONV_OK;
   const Groups g = {offsets, d.groups, d.rows};
+  if (few_rows(d)) {
+    RowsArgs r = {};
+    r.x = (const uint16_t*)x;
+    r.ld_x = d.ld_x;
+    r.ld_w = d.ld_w;
+    r.ld_y = d.ld_h;
+    r.w[0] = wg;
+    r.w[1] = wu;
+    r.y = (uint16_t*)h;
+    r.pre = pre;
+    r.ld_pre = (int)round_up(d.f, 8);
+    r.n = d.f;
+    r.k = d.k;
+    r.act = d.act;
+    const int64_t step = (int64_t)d.f * d.ld_w;
+    if (wu) return d.dtype == QCONV_F16 ? run_few<F16, 2>(r, g, step, s) : run_few<BF16, 2>(r, g, step, s);
+    return d.dtype == QCONV_F16 ? run_few<F16, 1>(r, g, step, s) : run_few<BF16, 1>(r, g, step, s);
+  }
   GemmArgs a = {};
   a.r[0] = a.r[1] = {(const uint16_t*)x, d.ld_x};
   a.c[0] = {(const uint16_t*)wg, d.ld_w};
@@ -177,12 +337,21 @@ int launch_moe_forward(const qconv_moe_desc& d, const void* x, const void* wg, c
   }
   const bool aligned = aligned_rows(a.r[0]) && aligned_rows(a.c[0]) && aligned_rows(a.c[1]) && a.k % 8 == 0;
   const int64_t step = (int64_t)d.f * a.c[0].ld;
-  if (wu) return run_rows<false, OUT_GATED>(d.dtype, a, g, step, tile_rows(d, d.f, true), aligned, s);
-  return run_rows<false, OUT_PLAIN>(d.dtype, a, g, step, tile_rows(d, d.f, false), aligned, s);
+  const GemmPlan p = plan_rows(d, d.f, d.k, wu, aligned);
+  a.part = (float*)((char*)ws + copies_bytes(d, wu, true));
+  return wu ? run_rows<false, OUT_GATED>(d.dtype, a, g, step, p, aligned, s)
+            : run_rows<false, OUT_PLAIN>(d.dtype, a, g, step, p, aligned, s);
 }
 
 size_t moe_backward_bytes(const qconv_moe_desc& d, bool gated) {
-  return copies_bytes(d, gated, false) + factor_bytes(d, gated);
+  size_t most = 0;
+  for (bool aligned : {false, true}) {
+    const size_t p = plan_rows(d, d.k, (gated ? 2 : 1) * (int64_t)d.f, false, aligned).bytes;
+    const size_t q = plan_weights(d, gated, aligned).bytes;
+    most = p > most ? p : most;
+    most = q > most ? q : most;
+  }
+  return copies_bytes(d, gated, false) + factor_bytes(d, gated) + most;
 }
 
 int launch_moe_backward(const qconv_moe_desc& d, const void* x, const void* wg, const void* wu, const int* offsets,
@@ -192,6 +361,7 @@ int launch_moe_backward(const qconv_moe_desc& d, const void* x, const void* wg, 
   Operand ox = {(const uint16_t*)x, d.ld_x}, og = {(const uint16_t*)wg, d.ld_w};
   Operand ou = wu ? Operand{(const uint16_t*)wu, d.ld_w} : og;
   uint16_t* factors = (uint16_t*)((char*)ws + copies_bytes(d, wu, false));
+  float* part = (float*)((char*)factors + factor_bytes(d, wu));
   bool whole = d.k % 8 == 0;  // rows end with 16 bytes
   int rc = QCONV_OK;
   if (copies_bytes(d, wu, false)) {
@@ -241,7 +411,9 @@ int launch_moe_backward(const qconv_moe_desc& d, const void* x, const void* wg, 
     a.out[0] = gx;
     a.ld_out = d.k;
     const bool aligned = aligned_rows(d0) && aligned_rows(og) && aligned_rows(ou) && whole && whole_h;
-    rc = run_rows<true, OUT_PLAIN>(d.dtype, a, g, (int64_t)d.f * og.ld, tile_rows(d, d.k, false), aligned, s);
+    a.part = part;
+    const GemmPlan p = plan_rows(d, d.k, a.segments * (int64_t)d.f, false, aligned);
+    rc = run_rows<true, OUT_PLAIN>(d.dtype, a, g, (int64_t)d.f * og.ld, p, aligned, s);
   }
   if (rc == QCONV_OK && gwg) {
     GemmArgs a = {};
@@ -256,10 +428,11 @@ int launch_moe_backward(const qconv_moe_desc& d, const void* x, const void* wg, 
     a.out[1] = gwu ? gwu : gwg;
     a.ld_out = d.k;
     const bool aligned = aligned_rows(d0) && aligned_rows(ox) && whole && whole_h;
-    const int tile = tile_weights(d, a.halves);
+    a.part = part;
+    const PlanW p = plan_weights(d, wu, aligned);
     const int64_t step = (int64_t)d.f * d.k;
-    rc = d.dtype == QCONV_F16 ? run_weights_t<F16>(a, g, step, tile, aligned, s)
-                              : run_weights_t<BF16>(a, g, step, tile, aligned, s);
+    rc = d.dtype == QCONV_F16 ? run_weights_t<F16>(a, g, step, p.tile, p.size, aligned, s)
+                              : run_weights_t<BF16>(a, g, step, p.tile, p.size, aligned, s);
   }
   return rc;
 }

@@ -77,4 +77,24 @@ struct GroupPieces {
   }
 };
 
+// The rows of a piece where groups of up to `most` rows need not be cut: `size`, or
+// all of them.
+__device__ __forceinline__ int group_size(const Groups& g, int size, int most) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+  for (int e = lane; e < g.n; e += 64) {
+    const int c = group_rows(g, e).count;
+    n = c > n ? c : n;
+  }
+  return __ballot(n > most) ? size : 0x7fffff00;
+}
+
+// Where the sums over piece `piece` of a group of several are kept, if the group's
+// rows start at `first`: pieces of one group start `size` rows apart, so at most two
+// of groups with several start in the same `size` rows, and of these one is its
+// group's first.  2 * ceil(rows / size) places do.
+__device__ __forceinline__ int64_t group_part(int64_t first, int piece, int size) {
+  return 2 * (first / size + piece) + (piece == 0 ? 1 : 0);
+}
+
 }  // namespace qc

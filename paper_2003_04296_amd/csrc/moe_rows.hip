@@ -116,22 +116,27 @@ __global__ __launch_bounds__(NW * 64) void moe_rank_kernel(SortArgs a) {
   const int b = wave * run < here ? wave * run : here, e = b + run < here ? b + run : here;
   for (int i = b + lane; i < e; i += 64) atomicAdd(&cnt[wave][sort_key(a, (int)first + i)], 1);
   __syncthreads();
-  // per key: in base all its rows, in start those of earlier blocks.  `span`
-  // lanes sum the blocks' counts of one key.
+  // per key: in base all its rows, in start those of earlier blocks.  Eight lanes
+  // sum the blocks' counts of one key.
   if (a.hist) {
     const int blocks = gridDim.x;
-    int span = 8;
-    while (span < 64 && span < blocks) span *= 2;
-    const int in = lane & (span - 1);
-    for (int g0 = wave * (64 / span); g0 < buckets; g0 += NT / span) {
-      const int g = g0 + lane / span;
+    const int in = lane & 7;
+    for (int g0 = wave * 8; g0 < buckets; g0 += NT / 8) {
+      const int g = g0 + lane / 8;
+      const int* h = a.hist + (int64_t)(g < buckets ? g : 0) * blocks;
       int before = 0, total = 0;
-      for (int k = in; k < blocks; k += span) {
-        const int h = g < buckets ? a.hist[(int64_t)g * blocks + k] : 0;
-        before += k < (int)blockIdx.x ? h : 0;
-        total += h;
+      for (int k0 = 0; k0 < blocks; k0 += 64) {
+        int c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = k0 + i * 8 + in < blocks ? h[k0 + i * 8 + in] : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          before += k0 + i * 8 + in < (int)blockIdx.x ? c[i] : 0;
+          total += c[i];
+        }
       }
-      for (int d = 1; d < span; d <<= 1) {
+#pragma unroll
+      for (int d = 1; d < 8; d <<= 1) {
         before += __shfl_xor(before, d);
         total += __shfl_xor(total, d);
       }

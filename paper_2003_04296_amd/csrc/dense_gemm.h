@@ -525,17 +525,23 @@ __device__ __forceinline__ void multiply_groups(v4f (&sums)[H][NR], const GemmAr
   }
 }
 
-// Which tile of C a block takes: its row and column tile, numbered over both halves.
+// A tile of C: its row and column, rows numbered over both halves.
 struct TileAt {
   uint32_t r, c;
 };
-// Workgroups go to the 8 dies in turn; each die gets a run of tiles that share
-// operands in its L2: 8 tile rows at a time, column after column.
+// Tile number t of rows x cols tiles: 8 tile rows at a time, column after column.
+__device__ __forceinline__ TileAt tile_number(uint32_t t, uint32_t rows, uint32_t cols) {
+  const uint32_t group = 8 * cols, first = t / group * 8, some = rows - first < 8 ? rows - first : 8;
+  return {first + t % group % some, t % group / some};
+}
+// Workgroups go to the 8 dies in turn; each die gets a run of the `all` tiles, which
+// share operands in its L2.
+__device__ __forceinline__ uint32_t die_tile(uint32_t id, uint32_t all) {
+  const uint32_t die = id & 7;
+  return die * (all / 8) + (die < all % 8 ? die : all % 8) + id / 8;
+}
 __device__ __forceinline__ TileAt tile_at(uint32_t id, uint32_t rows, uint32_t cols) {
-  const uint32_t all = rows * cols, group = 8 * cols, die = id & 7;
-  const uint32_t tile = die * (all / 8) + (die < all % 8 ? die : all % 8) + id / 8;
-  const uint32_t first = tile / group * 8, some = rows - first < 8 ? rows - first : 8;
-  return {first + tile % group % some, tile % group / some};
+  return tile_number(die_tile(id, rows * cols), rows, cols);
 }
 
 // The products of part `part` of a.parts of one tile.

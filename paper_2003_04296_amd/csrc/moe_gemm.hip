@@ -15,6 +15,36 @@ namespace qc {
 
 namespace {
 
+// The arguments of one expert's rows.
+template <int OUT>
+__device__ __forceinline__ void take_rows(GemmArgs& a, const GroupRows& rows) {
+  const int64_t first = __builtin_amdgcn_readfirstlane(rows.first);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) a.r[i].p += first * a.r[i].ld;
+  a.rows = __builtin_amdgcn_readfirstlane(rows.count);
+  a.out[0] = (uint16_t*)a.out[0] + first * a.ld_out;
+  if (OUT == OUT_GATED && a.pre) a.pre += first * 2 * a.ld_pre;
+}
+
+// Tiles of 256 x 256, one block of which fits a compute unit: as many as fill the
+// chip's 256 units a whole number of times are taken whole, the others' products are
+// split over the units that would be idle and joined by moe_tail_kernel (gx of 16384
+// rows of 8 experts, 4096 -> 2048, two products each: 544 tiles).
+struct Tail {
+  uint32_t full, rest;  // tiles
+  int parts;            // of each of the rest
+};
+constexpr int TAIL_TILE = 256 * 256;  // fp32 sums of a part
+__device__ __forceinline__ Tail tail_of(uint32_t all, int64_t products) {
+  Tail t;
+  t.full = all & ~255u;
+  t.rest = all - t.full;
+  int64_t parts = t.rest ? 256 / t.rest : 1;
+  if (parts > products / 512) parts = products / 512;
+  t.parts = parts > 16 ? 16 : parts > 1 ? (int)parts : 1;
+  return t;
+}
+
 // The products whose rows are the batch's (forward, gx).
 template <class T, class SR, class SC, int OUT, int B>
 __global__ __launch_bounds__(B / 64 * 128) void moe_gemm_kernel(GemmArgs a, Groups g, int64_t step_c) {
@@ -22,27 +52,78 @@ __global__ __launch_bounds__(B / 64 * 128) void moe_gemm_kernel(GemmArgs a, Grou
 #ifdef __HIP_DEVICE_COMPILE__  // the host has no LDS pointers
   const GroupPieces pieces(g, B);
   const uint32_t all = (uint32_t)pieces.total * a.tiles_c;
-  // the parts of one tile lie `blocks` launched tiles apart
-  const uint32_t blocks = gridDim.x / a.parts, part = blockIdx.x / blocks, id = blockIdx.x % blocks;
-  if (id >= all) return;
-  TileAt at = tile_at(id, pieces.total, a.tiles_c);
+  uint32_t part, tile;
+  [[maybe_unused]] float* sums = nullptr;
+  if constexpr (B == 256) {
+    const Tail tail = tail_of(all, (int64_t)a.k * a.segments);
+    part = 0;
+    if (blockIdx.x < tail.full) {
+      tile = die_tile(blockIdx.x, tail.full);
+      a.parts = 1;
+    } else {
+      const uint32_t i = (blockIdx.x - tail.full) / tail.parts;
+      if (i >= tail.rest) return;
+      tile = tail.full + i;
+      a.parts = tail.parts;
+      part = (blockIdx.x - tail.full) % tail.parts;
+      if (tail.parts > 1) sums = a.part + (int64_t)i * tail.parts * TAIL_TILE;
+    }
+  } else {
+    // the parts of one tile lie as many blocks apart as are launched for each
+    const uint32_t blocks = gridDim.x / a.parts, id = blockIdx.x % blocks;
+    part = blockIdx.x / blocks;
+    if (id >= all) return;
+    tile = die_tile(id, all);
+  }
+  TileAt at = tile_number(tile, pieces.total, a.tiles_c);
   int e, piece;
   pieces.find(g, at.r, e, piece);
   const GroupRows rows = group_rows(g, e);
-  const int64_t first = __builtin_amdgcn_readfirstlane(rows.first);
+  take_rows<OUT>(a, rows);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    a.r[i].p += first * a.r[i].ld;
-    a.c[i].p += e * step_c;
-  }
-  a.rows = __builtin_amdgcn_readfirstlane(rows.count);
-  a.out[0] = (uint16_t*)a.out[0] + first * a.ld_out;
-  if (OUT == OUT_GATED && a.pre) a.pre += first * 2 * a.ld_pre;
-  if (a.part) a.part += first * a.ld_part;
+  for (int i = 0; i < 2; ++i) a.c[i].p += e * step_c;
   at.r = piece;
+  if constexpr (B == 256) {
+    a.part = sums;
+    if (sums) {  // [parts][2 if gated][256][columns of a tile]
+      a.part_rows = 256;
+      a.ld_part = OUT == OUT_GATED ? 128 : 256;
+      a.part -= ((int64_t)at.r * 256 + at.c) * a.ld_part;
+    }
+  } else if (a.part) {
+    a.part += (int64_t)rows.first * a.ld_part;
+  }
   a.tiles_r = 0x7fffffff;  // one half
   gemm_tile<T, SR, SC, OUT, B, B>(a, (lds_v4u*)lds, at, part);
 #endif
+}
+
+// Joins the tiles that moe_gemm_kernel has split: 16 blocks a tile.
+template <class T, int OUT>
+__global__ __launch_bounds__(256) void moe_tail_kernel(GemmArgs a, Groups g) {
+  constexpr int H = OUT == OUT_GATED ? 2 : 1, COLS = 256 / H;
+  const GroupPieces pieces(g, 256);
+  const Tail tail = tail_of((uint32_t)pieces.total * a.tiles_c, (int64_t)a.k * a.segments);
+  const uint32_t i = blockIdx.x / 16;
+  if (i >= tail.rest || tail.parts == 1) return;
+  const TileAt at = tile_number(tail.full + i, pieces.total, a.tiles_c);
+  int e, piece;
+  pieces.find(g, at.r, e, piece);
+  take_rows<OUT>(a, group_rows(g, e));
+  const float* sums = a.part + (int64_t)i * tail.parts * TAIL_TILE;
+  with_act(OUT == OUT_GATED ? a.act : 0, [&](auto act) {
+    for (int q = threadIdx.x; q < 16 * COLS / 4; q += 256) {
+      const int row = blockIdx.x % 16 * 16 + q / (COLS / 4), col = q % (COLS / 4) * 4;
+      const int64_t r = (int64_t)piece * 256 + row, c = (int64_t)at.c * COLS + col;
+      if (r >= a.rows || c >= a.cols) continue;
+      v4f v[2] = {};
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        for (int p = 0; p < tail.parts; ++p)
+          v[h] += *(const v4f*)(sums + ((int64_t)(p * H + h) * 256 + row) * COLS + col);
+      finish4<T, OUT, decltype(act)::value>(a, 0, r, c, v);
+    }
+  });
 }
 
 // The join of split products, for the rows that groups have.
@@ -147,14 +228,17 @@ int run_few(RowsArgs& a, const Groups& g, int64_t step_w, hipStream_t s) {
 template <class T, class SR, class SC, int OUT, int B>
 int run_tiles(GemmArgs& a, const Groups& g, int64_t step_c, hipStream_t s) {
   a.tiles_c = ceil_div(a.cols, OUT == OUT_GATED ? B / 2 : B);
-  const int64_t blocks = GroupPieces::most(g.rows, g.n, B) * a.tiles_c * a.parts;
+  int64_t blocks = GroupPieces::most(g.rows, g.n, B) * a.tiles_c * a.parts;
+  if (B == 256) blocks += 256;  // parts of the last tiles
   if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;  // 2^31 threads
   a.rows = a.part_rows = g.rows;
   a.ld_part = (int)round_up(a.cols, 4);
-  if (a.parts == 1) a.part = nullptr;
+  if (B != 256 && a.parts == 1) a.part = nullptr;
   a.wide_out = a.ld_out % 4 == 0 && ((uintptr_t)a.out[0] & 7) == 0;
   moe_gemm_kernel<T, SR, SC, OUT, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a, g, step_c);
-  if (a.parts > 1) {
+  if (B == 256) {
+    moe_tail_kernel<T, OUT><<<128 * 16, 256, 0, s>>>(a, g);  // more tiles than 128 are not split
+  } else if (a.parts > 1) {
     const int64_t n = (int64_t)g.rows * (a.ld_part / 4);
     moe_join_kernel<T, OUT><<<(unsigned)(n < (1 << 20) ? (n + 255) / 256 : 4096), 256, 0, s>>>(a, g);
   }
@@ -220,7 +304,7 @@ GemmPlan plan_rows(const qconv_moe_desc& d, int cols, int64_t products, bool gat
     const int64_t n = GroupPieces::most(d.rows, d.groups, b) * ceil_div(cols, gated ? b / 2 : b);
     return n > 0 ? n : 1;
   };
-  if (aligned && d.rows >= 192 * (int64_t)d.groups && tiles(256) >= 256) return {256, 1, 0};
+  if (aligned && d.rows >= 192 * (int64_t)d.groups && tiles(256) >= 256) return {256, 1, (size_t)256 * TAIL_TILE * 4};
   const int64_t small = tiles(128);
   int64_t parts = small >= 192 ? 1 : 256 / small;
   if (parts > products / 512) parts = products / 512;

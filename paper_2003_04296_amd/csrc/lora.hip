@@ -92,37 +92,47 @@ __global__ __launch_bounds__(NW * 64) void lora_shrink_kernel(LoraArgs a) {
   for (int j = 0; j < MR; ++j)
 #pragma unroll
     for (int i = 0; i < RT; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  // The next 128 values are on their way while these are multiplied.  The fence
+  // keeps the loads ahead of the products: left alone, the compiler puts each right
+  // before its use to save registers, and the wave waits for one at a time.
   const int blocks = a.len / 128, step = a.parts * NW;
   int b = split * NW + wave;
-  for (; b < blocks; b += step) {
-    v4u xf[MR][4], wf[RT][4];
+  struct Block {
+    v4u x[MR][4], w[RT][4];
+  } next;
+  auto load = [&](int64_t k) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
 #pragma unroll
-      for (int j = 0; j < MR; ++j) xf[j][s] = load8(x[j] + (int64_t)b * 128 + s * 32);
+      for (int j = 0; j < MR; ++j) next.x[j][s] = load8(x[j] + k + s * 32);
 #pragma unroll
-      for (int i = 0; i < RT; ++i) wf[i][s] = load8(w[i] + (int64_t)b * 128 + s * 32);
+      for (int i = 0; i < RT; ++i) next.w[i][s] = load8(w[i] + k + s * 32);
     }
+  };
+  if (b < blocks) load((int64_t)b * 128);
+  for (; b < blocks; b += step) {
+    const Block now = next;
+    if (b + step < blocks) load((int64_t)(b + step) * 128);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int j = 0; j < MR; ++j)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) acc[j][i] = T::mfma(wf[i][s], xf[j][s], acc[j][i]);
+        for (int i = 0; i < RT; ++i) acc[j][i] = T::mfma(now.w[i][s], now.x[j][s], acc[j][i]);
   }
-  if (b == blocks && a.len % 128) {
+  if (b == blocks) {
+    for (int k = blocks * 128; k < a.len; k += 32) {
+      const int left = a.len - k - o * 8;
+      v4u xf[MR], wf[RT];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int k = blocks * 128 + s * 32, left = a.len - k - o * 8;
-      v4u xf[MR];
+      for (int j = 0; j < MR; ++j) xf[j] = a.len - k >= 32 ? load8(x[j] + k) : load8_first(x[j] + k, left);
 #pragma unroll
-      for (int j = 0; j < MR; ++j) xf[j] = load8_first(x[j] + k, left);
+      for (int i = 0; i < RT; ++i) wf[i] = a.len - k >= 32 ? load8(w[i] + k) : load8_first(w[i] + k, left);
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const v4u wf = load8_first(w[i] + k, left);
+      for (int j = 0; j < MR; ++j)
 #pragma unroll
-        for (int j = 0; j < MR; ++j) acc[j][i] = T::mfma(wf, xf[j], acc[j][i]);
-      }
+        for (int i = 0; i < RT; ++i) acc[j][i] = T::mfma(wf[i], xf[j], acc[j][i]);
     }
   }
 #pragma unroll
@@ -220,6 +230,52 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
   const GroupRows rows = group_rows(a.g, e);
   const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
   const int steps = (a.rank + 31) / 32, ld = steps * 8 + 1;  // in chunks
+  int token[MR];
+#pragma unroll
+  for (int j = 0; j < MR; ++j) token[j] = j * 16 + r < here ? token_at(a, first + j * 16 + r) : -1;
+  const uint16_t* wp = a.w.p + e * a.w.step;
+  // Loads are the same for every lane where a chunk of columns exists whole, from a
+  // row that exists where the lane has none, so that they can be under way together:
+  // those of the next 64 columns (and of the next 32 ranks) while these are multiplied.
+  v4u y[MR][2], wf[4];
+  auto load_w = [&](int ch, int k) {
+    const int c0 = ch * 64 + (r >> 2) * 16 + (r & 3), at = k * 32 + o * 8;
+    if (a.rank % 8 == 0) {
+      const bool in = at < a.rank;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = c0 + i * 4 < a.len ? c0 + i * 4 : a.len - 1;
+        wf[i] = load8(wp + c * a.w.ld + (in ? at : 0));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wf[i] = in ? wf[i] : v4u{0, 0, 0, 0};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = c0 + i * 4 < a.len ? c0 + i * 4 : a.len - 1;
+        wf[i] = load8_first(wp + c * a.w.ld + at, a.rank - at);
+      }
+    }
+  };
+  auto load_y = [&](int ch) {
+    if (!a.x) return;
+    const int c = ch * 64 + o * 16;
+#pragma unroll
+    for (int j = 0; j < MR; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint16_t* from = a.x + (token[j] < 0 ? 0 : token[j]) * a.ld_x;
+        y[j][h] = ch * 64 + 64 <= a.len ? load8(from + c + h * 8) : load8_first(from + (c < a.len ? c + h * 8 : 0), a.len - c - h * 8);
+      }
+  };
+#pragma unroll
+  for (int j = 0; j < MR; ++j) y[j][0] = y[j][1] = v4u{0, 0, 0, 0};
+  int ch = tile * 4 + wave;
+  if (ch < chunks) {
+    load_w(ch, 0);
+    load_y(ch);
+  }
+  const float scale = a.scale ? a.scale[e] : 1.0f;
   // mid's rows: summed over its parts, zeros past the rank
   for (int i = threadIdx.x; i < R * steps * 8; i += 256) {
     const int row = i / (steps * 8), c = i % (steps * 8) * 4;
@@ -227,6 +283,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
     if (row < here && c < a.rank) {
       const float* m = a.mid + (int64_t)(first + row) * a.ld_mid + c;
       s = *(const v4f*)m;
+#pragma unroll 4
       for (int q = 1; q < a.parts; ++q) s += *(const v4f*)(m + (int64_t)q * a.g.rows * a.ld_mid);
 #pragma unroll
       for (int q = 0; q < 4; ++q)
@@ -238,65 +295,66 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
     to[steps * 8] = v2u{t[0].lo | (uint32_t)t[1].lo << 16, t[2].lo | (uint32_t)t[3].lo << 16};
   }
   __syncthreads();
-  const float scale = a.scale ? a.scale[e] : 1.0f;
-  int token[MR];
+  v4f acc[MR][4];
 #pragma unroll
-  for (int j = 0; j < MR; ++j) token[j] = j * 16 + r < here ? token_at(a, first + j * 16 + r) : -1;
-  const uint16_t* wp = a.w.p + e * a.w.step;
-  for (int ch = tile * 4 + wave; ch < chunks; ch += a.tiles * 4) {
-    const int c0 = ch * 64, mine = c0 + o * 16;  // of the results
-    v4u y[MR][2];
+  for (int j = 0; j < MR; ++j)
 #pragma unroll
-    for (int j = 0; j < MR; ++j)
+    for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  v4u base[MR][2];
+  for (int k = 0; ch < chunks;) {
+    v4u w[4][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int left = token[j] >= 0 && a.x ? a.len - mine - h * 8 : 0;
-        y[j][h] = load8_first(left > 0 ? a.x + token[j] * a.ld_x + mine + h * 8 : a.x, left);
-      }
-    v4f acc[MR][4];
+    for (int i = 0; i < 4; ++i) in_bf16<T>(wf[i], w[i]);
+    if (k == 0) {
 #pragma unroll
-    for (int j = 0; j < MR; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < steps; ++k) {
-      v4u wf[4][2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = c0 + (r >> 2) * 16 + i * 4 + (r & 3);
-        in_bf16<T>(load8_first(wp + (c < a.len ? c : a.len - 1) * a.w.ld + k * 32 + o * 8, a.rank - k * 32 - o * 8), wf[i]);
-      }
-#pragma unroll
-      for (int j = 0; j < MR; ++j) {
-        const v4u* s = lds + (j * 16 + r) * ld + k * 4 + o;
-        const v4u hi = s[0], lo = s[steps * 4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[j][i] = BF16::mfma(wf[i][0], hi, acc[j][i]);
-          acc[j][i] = BF16::mfma(wf[i][0], lo, acc[j][i]);
-          if constexpr (BF16_PARTS<T> == 2) acc[j][i] = BF16::mfma(wf[i][1], hi, acc[j][i]);
-        }
-      }
+      for (int j = 0; j < MR; ++j) base[j][0] = y[j][0], base[j][1] = y[j][1];
     }
+    const int here_ch = ch, here_k = k;
+    if (++k == steps) {
+      k = 0;
+      ch += a.tiles * 4;
+    }
+    if (ch < chunks) {
+      load_w(ch, k);
+      if (k == 0) load_y(ch);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < MR; ++j) {
-      if (token[j] < 0) continue;
-      uint16_t* to = a.out + token[j] * a.ld_out + mine;
+      const v4u* s = lds + (j * 16 + r) * ld + here_k * 4 + o;
+      const v4u hi = s[0], lo = s[steps * 4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint16_t v[8];
+      for (int i = 0; i < 4; ++i) {
+        acc[j][i] = BF16::mfma(w[i][0], hi, acc[j][i]);
+        acc[j][i] = BF16::mfma(w[i][0], lo, acc[j][i]);
+        if constexpr (BF16_PARTS<T> == 2) acc[j][i] = BF16::mfma(w[i][1], hi, acc[j][i]);
+      }
+    }
+    if (k != 0) continue;
+    const int mine = here_ch * 64 + o * 16;
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          v[q] = T::down(fmaf(scale, acc[j][h * 2 + q / 4][q % 4], T::up((uint16_t)(y[j][h][q / 2] >> (16 * (q & 1))))));
-        if (mine + h * 8 + 8 <= a.len) {
-          reinterpret_cast<U128*>(to + h * 8)->v =
-              v4u{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
-                  v[6] | (uint32_t)v[7] << 16};
-        } else {
+    for (int j = 0; j < MR; ++j) {
+      if (token[j] >= 0) {
+        uint16_t* to = a.out + token[j] * a.ld_out + mine;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint16_t v[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q)
-            if (mine + h * 8 + q < a.len) to[h * 8 + q] = v[q];
+            v[q] = T::down(fmaf(scale, acc[j][h * 2 + q / 4][q % 4], T::up((uint16_t)(base[j][h][q / 2] >> (16 * (q & 1))))));
+          if (mine + h * 8 + 8 <= a.len) {
+            reinterpret_cast<U128*>(to + h * 8)->v =
+                v4u{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
+                    v[6] | (uint32_t)v[7] << 16};
+          } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              if (mine + h * 8 + q < a.len) to[h * 8 + q] = v[q];
+          }
         }
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
   }
 }
@@ -308,6 +366,8 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
 // Rows of an adapter are taken `size` at a time; a block has 256 columns of a
 // piece and 64 ranks.  The sums of an adapter with one piece (or none: zeros) are
 // results; others go to part.
+constexpr int GRAD_MOST = 512;  // rows of a piece, a multiple of 32
+
 // Writes 4 values of a row of a gradient.
 template <class T>
 __device__ __forceinline__ void put_grad(const LoraArgs& a, int e, int rows, int cols, int row, int col, v4f v) {
@@ -325,6 +385,7 @@ template <class T, int RT, bool FLIP>
 __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
   constexpr int C = 256, XP = BF16_PARTS<T>, XCH = 32 * C / 8, SCH = 32 * 128 / 8, STAGE = XCH * XP + SCH;
   [[maybe_unused]] __shared__ v4u store[2 * STAGE];
+  [[maybe_unused]] __shared__ int tokens[GRAD_MOST + 64];  // and two stages of none
 #ifdef __HIP_DEVICE_COMPILE__
   lds_v4u* const lds = (lds_v4u*)store;
   const GroupPieces pieces(a.g, a.size, true);
@@ -343,24 +404,42 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = threadIdx.x; i < GRAD_MOST + 64; i += 256) tokens[i] = i < here ? token_at(a, first + i) : -1;
+  __syncthreads();
   // A stage: 32 tokens.  Of x a thread has 4 chunks of 8 columns, of mid 2 x 4 ranks.
-  v4u xr[4];
-  v4f sr[2];
+  // Two stages are on their way while one is multiplied.
+  v4u xr[4], xr2[4];
+  v4f sr[2], sr2[2];
   const int xc = threadIdx.x % 32, sc = threadIdx.x % 16 * 4;
+  const bool whole_cols = c0 + C <= a.len, rank_in = r0 + sc < a.rank;
   auto load = [&](int at) {
+    int t[4], u[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = tokens[at + threadIdx.x / 32 + i * 8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) u[i] = tokens[at + threadIdx.x / 16 + i * 16];
+    // in place of a token that is none the first one, which then counts for nothing
+    const int col = c0 + xc * 8;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int k = at + threadIdx.x / 32 + i * 8, col = c0 + xc * 8;
-      const int t = k < here ? token_at(a, first + k) : -1;
-      xr[i] = load8_first(t >= 0 ? a.x + t * a.ld_x + col : a.x, t >= 0 ? a.len - col : 0);
+      const uint16_t* from = a.x + (t[i] < 0 ? 0 : t[i]) * a.ld_x + (whole_cols || col < a.len ? col : 0);
+      xr2[i] = whole_cols ? load8(from) : load8_first(from, a.len - col);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int k = at + threadIdx.x / 16 + i * 16;
-      // a token that is none counts for nothing
-      const bool on = k < here && r0 + sc < a.rank && token_at(a, first + k) >= 0;
-      sr[i] = on ? *(const v4f*)(a.mid + (int64_t)(first + k) * a.ld_mid + r0 + sc) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      sr2[i] = *(const v4f*)(a.mid + (int64_t)(first + (u[i] >= 0 ? k : 0)) * a.ld_mid + (rank_in ? r0 + sc : 0));
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) xr2[i] = t[i] >= 0 ? xr2[i] : v4u{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sr2[i] = u[i] >= 0 && rank_in ? sr2[i] : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  };
+  auto advance = [&] {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) xr[i] = xr2[i];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sr[i] = sr2[i];
   };
   auto put = [&](lds_v4u* to) {
 #pragma unroll
@@ -385,13 +464,16 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
   };
   if (here > 0) {
     load(0);
+    advance();
+    load(32);
     put(lds);
+    advance();
   }
   for (int at = 0, b = 0; at < here; at += 32, b ^= 1) {
     __syncthreads();
     const lds_v4u* now = lds + b * STAGE;
-    const bool more = at + 32 < here;
-    if (more) load(at + 32);
+    if (at + 64 < here) load(at + 64);
+    __builtin_amdgcn_sched_barrier(0);
     v4u s[2][RT];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -412,7 +494,8 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
         if constexpr (XP == 2) add(x[1], s[0][j]);
       }
     }
-    if (more) put(lds + (b ^ 1) * STAGE);
+    if (at + 32 < here) put(lds + (b ^ 1) * STAGE);
+    advance();
   }
   const bool whole = rows.count <= a.size;
   const int nr = FLIP ? a.len : a.rank, nc = FLIP ? a.rank : a.len;
@@ -519,23 +602,34 @@ int run_expand(LoraArgs& a, int rows, hipStream_t s) {
   return hip_status();
 }
 
-// Tokens of a piece of a weight gradient.
-constexpr int GRAD_ROWS = 512;
+// Tokens of a piece of a weight gradient: as many as make about 1024 blocks.
+int grad_rows(const LoraArgs& a, int len) {
+  const int64_t n = (int64_t)a.g.rows * ceil_div(len, 256) * ceil_div(a.rank, 64) / 1024;
+  return n < 128 ? 128 : n < GRAD_MOST ? (int)round_up(n, 32) : GRAD_MOST;
+}
 size_t grad_bytes(const qconv_lora_desc& d) {
-  const int64_t a = (int64_t)d.rank * round_up(d.k, 4), b = (int64_t)d.n * round_up(d.rank, 4);
-  return d.m > GRAD_ROWS ? (size_t)2 * ceil_div(d.m, GRAD_ROWS) * (a > b ? a : b) * 4 : 0;
+  size_t most = 0;
+  LoraArgs a = {};
+  a.g.rows = d.m;
+  a.rank = d.rank;
+  for (int len : {d.k, d.n}) {
+    const int64_t size = grad_rows(a, len), p = len == d.k ? d.rank * round_up(len, 4) : 0, q = len == d.n ? len * round_up(d.rank, 4) : 0;
+    const size_t bytes = d.m > size ? (size_t)(2 * ((d.m + size - 1) / size) * (p > q ? p : q) * 4) : 0;
+    most = bytes > most ? bytes : most;
+  }
+  return most;
 }
 template <class T, int RT, bool FLIP>
 int run_grad_t(LoraArgs& a, hipStream_t s) {
-  a.size = GRAD_ROWS;
+  a.size = grad_rows(a, a.len);
   a.tiles = ceil_div(a.len, 256);
   a.ld_part = round_up(FLIP ? a.rank : a.len, 4);
-  const int64_t blocks = ((int64_t)a.g.rows / GRAD_ROWS + a.g.n) * a.tiles * ceil_div(a.rank, 64);
+  const int64_t blocks = ((int64_t)a.g.rows / a.size + a.g.n) * a.tiles * ceil_div(a.rank, 64);
   if (blocks >= (1 << 23)) return QCONV_EUNSUPPORTED;
   lora_grad_kernel<T, RT, FLIP><<<(unsigned)blocks, 256, 0, s>>>(a);
-  if (a.g.rows > GRAD_ROWS) {
+  if (a.g.rows > a.size) {
     const int64_t n = (FLIP ? a.len : a.rank) * a.ld_part / 4;
-    const int several = a.g.rows / GRAD_ROWS < a.g.n ? a.g.rows / GRAD_ROWS : a.g.n;
+    const int several = a.g.rows / a.size < a.g.n ? a.g.rows / a.size : a.g.n;
     const dim3 grid((unsigned)(n < (1 << 16) ? (n + 255) / 256 : 256), several);
     lora_grad_join_kernel<T, FLIP><<<grid, 256, 0, s>>>(a);
   }

@@ -533,21 +533,36 @@ __global__ __launch_bounds__(256) void lora_grad_join_kernel(LoraArgs a) {
   }
 }
 
-// The transposed copy of each group's matrix [rows][cols] in rows of ld_out.
-__global__ __launch_bounds__(256) void lora_transpose_kernel(const uint16_t* w, int rows, int cols, uint16_t* out,
-                                                             int64_t ld_out, int tiles_r, int tiles_c) {
+// Transposed copies of each group's matrix [rows][cols], in rows of ld_out: of b, and
+// of a where blocks are left for it.
+struct Transpose {
+  const uint16_t* w[2];
+  uint16_t* out[2];
+  int rows[2], cols[2];
+  int64_t ld_out[2];
+  uint32_t blocks;  // of the first
+};
+__global__ __launch_bounds__(256) void lora_transpose_kernel(Transpose a) {
   __shared__ uint16_t t[64][66];
-  const int tc = blockIdx.x % tiles_c, tr = blockIdx.x / tiles_c % tiles_r;
-  const int64_t g = blockIdx.x / tiles_c / tiles_r;
+  const int which = blockIdx.x >= a.blocks;
+  const uint32_t id = blockIdx.x - (which ? a.blocks : 0);
+  const int rows = a.rows[which], cols = a.cols[which], tr_n = (rows + 63) / 64, tc_n = (cols + 63) / 64;
+  const int tc = id % tc_n, tr = id / tc_n % tr_n;
+  const int64_t g = id / tc_n / tr_n;
   const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-  for (int i = y; i < 64; i += 4) {
-    const int r = tr * 64 + i, c = tc * 64 + x;
-    if (r < rows && c < cols) t[i][x] = w[(g * rows + r) * cols + c];
+  uint16_t v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = tr * 64 + y + i * 4, c = tc * 64 + x;
+    v[i] = r < rows && c < cols ? a.w[which][(g * rows + r) * cols + c] : (uint16_t)0;
   }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t[y + i * 4][x] = v[i];
   __syncthreads();
-  for (int i = y; i < 64; i += 4) {
-    const int r = tr * 64 + x, c = tc * 64 + i;
-    if (r < rows && c < cols) out[(g * cols + c) * ld_out + r] = t[x][i];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int r = tr * 64 + x, c = tc * 64 + y + i * 4;
+    if (r < rows && c < cols) a.out[which][(g * cols + c) * a.ld_out[which] + r] = t[x][y + i * 4];
   }
 }
 
@@ -591,8 +606,8 @@ int run_shrink(LoraArgs& a, int rows, hipStream_t s) {
 template <class T>
 int run_expand(LoraArgs& a, int rows, hipStream_t s) {
   const int64_t pieces = a.g.rows / rows + (a.g.n + 1 < a.g.rows ? a.g.n + 1 : a.g.rows);
-  // a block per 256 columns until there are about 1024
-  const int64_t most = ceil_div(a.len, 256), want = 1024 / pieces;
+  // a block per 256 columns while there are at most about 2048
+  const int64_t most = ceil_div(a.len, 256), want = 2048 / pieces;
   a.tiles = (int)(want < 1 ? 1 : want < most ? want : most);
   if (pieces * a.tiles >= (1 << 23)) return QCONV_EUNSUPPORTED;
   const size_t lds = (size_t)rows * (ceil_div(a.rank, 32) * 8 + 1) * 16;
@@ -640,11 +655,12 @@ int run_grad(LoraArgs& a, hipStream_t s) {
   return a.rank <= 16 ? run_grad_t<T, 1, FLIP>(a, s) : a.rank <= 32 ? run_grad_t<T, 2, FLIP>(a, s) : run_grad_t<T, 4, FLIP>(a, s);
 }
 
-int run_transpose(const void* w, int groups, int rows, int cols, uint16_t* out, int64_t ld_out, hipStream_t s) {
-  const int tr = ceil_div(rows, 64), tc = ceil_div(cols, 64);
-  const int64_t blocks = (int64_t)groups * tr * tc;
-  if (blocks >= (1 << 23)) return QCONV_EUNSUPPORTED;
-  lora_transpose_kernel<<<(unsigned)blocks, 256, 0, s>>>((const uint16_t*)w, rows, cols, out, ld_out, tr, tc);
+int run_transpose(const Transpose& t, int groups, bool both, hipStream_t s) {
+  auto blocks = [&](int i) { return (int64_t)groups * ceil_div(t.rows[i], 64) * ceil_div(t.cols[i], 64); };
+  if (blocks(0) + blocks(1) >= (1 << 23)) return QCONV_EUNSUPPORTED;
+  Transpose a = t;
+  a.blocks = (uint32_t)blocks(0);
+  lora_transpose_kernel<<<(unsigned)(blocks(0) + (both ? blocks(1) : 0)), 256, 0, s>>>(a);
   return hip_status();
 }
 
@@ -705,7 +721,8 @@ int backward(const qconv_lora_desc& d, LoraArgs a, const void* x, const void* wa
   int rc = QCONV_OK;
   if (d.m > 0) {
     const int64_t ld_bt = round_up(d.n, 8), ld_at = round_up(d.rank, 8);
-    rc = run_transpose(wb, d.groups, d.n, d.rank, bt, ld_bt, s);
+    rc = run_transpose({{(const uint16_t*)wb, (const uint16_t*)wa}, {bt, at}, {d.n, d.rank}, {d.rank, d.k}, {ld_bt, ld_at}, 0},
+                       d.groups, gx != nullptr, s);
     if (rc) return rc;
     a.parts = shrink_parts(d, d.n);
     a.len = d.n;
@@ -720,8 +737,6 @@ int backward(const qconv_lora_desc& d, LoraArgs a, const void* x, const void* wa
     a.mid = p;
     a.parts = 1;
     if (gx) {
-      rc = run_transpose(wa, d.groups, d.rank, d.k, at, ld_at, s);
-      if (rc) return rc;
       a.len = d.k;
       a.x = nullptr;
       a.w = {at, ld_at, (int64_t)d.k * ld_at};

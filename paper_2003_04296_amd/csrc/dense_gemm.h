@@ -48,7 +48,6 @@ struct GemmArgs {
   int kp;  // codes per row
   void* out[2];
   int64_t ld_out;
-  int wide_out;  // rows of out start at 8-byte addresses
   const float* bias;
   float* pre;  // OUT_GATED: [rows][2][ld_pre] or NULL
   int ld_pre;
@@ -275,15 +274,19 @@ __device__ __forceinline__ v4u fragment(const lds_v4u* lds, int r0, int sub) {
   }
 }
 
-// Four values of one row, columns c..c + 3 of `cols`.
+// Four values of one row, columns c..c + 3 of `cols`, at any address that a value
+// may have (global stores take it).
+struct __attribute__((packed, aligned(2))) U64 {
+  v2u v;
+};
 template <class T>
-__device__ __forceinline__ void put4(void* out, int64_t row, int64_t c, int64_t cols, bool wide, v4f v) {
+__device__ __forceinline__ void put4(void* out, int64_t row, int64_t c, int64_t cols, v4f v) {
   uint16_t* p = (uint16_t*)out + row + c;
   uint16_t b[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) b[e] = T::down(v[e]);
-  if (wide && c + 4 <= cols) {
-    *(v2u*)p = v2u{b[0] | (uint32_t)b[1] << 16, b[2] | (uint32_t)b[3] << 16};
+  if (c + 4 <= cols) {
+    reinterpret_cast<U64*>(p)->v = v2u{b[0] | (uint32_t)b[1] << 16, b[2] | (uint32_t)b[3] << 16};
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -326,14 +329,14 @@ __device__ __forceinline__ void finish4(const GemmArgs& a, int half, int64_t r, 
     v4f h;
 #pragma unroll
     for (int e = 0; e < 4; ++e) h[e] = act_value<ACT>(v[0][e]) * v[1][e];
-    put4<T>(a.out[0], r * a.ld_out, c, a.cols, a.wide_out, h);
+    put4<T>(a.out[0], r * a.ld_out, c, a.cols, h);
   } else {
     if (a.bias) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (c + e < a.cols) v[0][e] += a.bias[c + e];
     }
-    put4<T>(a.out[half], r * a.ld_out, c, a.cols, a.wide_out, v[0]);
+    put4<T>(a.out[half], r * a.ld_out, c, a.cols, v[0]);
   }
 }
 
@@ -885,7 +888,6 @@ int run_gemm_tiles(GemmArgs& a, hipStream_t s) {
   if (a.parts == 1) a.part = nullptr;
   a.part_rows = a.rows;
   a.ld_part = (int)round_up(a.cols, 4);
-  a.wide_out = a.ld_out % 4 == 0 && ((uintptr_t)a.out[0] & 7) == 0 && ((uintptr_t)a.out[1] & 7) == 0;
   dense_gemm_kernel<T, SR, SC, OUT, B, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a);
   if (a.parts > 1) {
     const int64_t n = (int64_t)a.rows * (a.ld_part / 4) * (OUT == OUT_GATED ? 1 : a.halves);

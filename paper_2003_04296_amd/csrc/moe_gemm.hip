@@ -234,7 +234,6 @@ int run_tiles(GemmArgs& a, const Groups& g, int64_t step_c, hipStream_t s) {
   a.rows = a.part_rows = g.rows;
   a.ld_part = (int)round_up(a.cols, 4);
   if (B != 256 && a.parts == 1) a.part = nullptr;
-  a.wide_out = a.ld_out % 4 == 0 && ((uintptr_t)a.out[0] & 7) == 0;
   moe_gemm_kernel<T, SR, SC, OUT, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a, g, step_c);
   if (B == 256) {
     moe_tail_kernel<T, OUT><<<128 * 16, 256, 0, s>>>(a, g);  // more tiles than 128 are not split
@@ -254,7 +253,6 @@ int run_tiles_w(GemmArgs& a, const Groups& g, int size, int64_t step_out, hipStr
   if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;
   a.part_rows = a.rows;
   a.ld_part = (int)round_up(a.cols, 4);
-  a.wide_out = a.ld_out % 4 == 0 && ((uintptr_t)a.out[0] & 7) == 0 && ((uintptr_t)a.out[1] & 7) == 0;
   moe_gemm_w_kernel<T, SR, SC, B><<<(unsigned)blocks, B / 64 * 128, 0, s>>>(a, g, size, uncut, step_out);
   if (g.rows > size) {
     const int64_t n = (int64_t)a.halves * a.rows * (a.ld_part / 4);

@@ -55,6 +55,32 @@ __device__ __forceinline__ int token_at(const LoraArgs& a, int r) {
   return (uint32_t)t < (uint32_t)a.g.rows ? t : -1;
 }
 
+// Eight values without the first k of them (0 <= k <= 8), zeros behind.
+__device__ __forceinline__ v4u drop(v4u v, int k) {
+  const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+  const int s = 16 * (k & 3);
+  const uint64_t up = s ? hi << (64 - s) : 0;
+  const uint64_t a = k >= 8 ? 0 : k >= 4 ? hi >> s : lo >> s | up, b = k >= 4 ? 0 : hi >> s;
+  return v4u{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+}
+// load8_first at the end of a row of `len` values, n of which begin at p, in one load
+// (value by value, each would be waited for): the row's last eight, moved.
+__device__ __forceinline__ v4u load8_end(const uint16_t* p, int n, int len) {
+  if (len < 8) return load8_first(p, n);
+  const int64_t d = n < 8 ? 8 - (int64_t)n : 0;
+  return drop(load8(p - d), d < 8 ? (int)d : 8);
+}
+// load8_first inside contiguous memory that ends at `end`, `all` values long: what
+// follows the n values is read and cleared.
+__device__ __forceinline__ v4u load8_inside(const uint16_t* p, int n, const uint16_t* end, int64_t all) {
+  if (all < 8) return load8_first(p, n);
+  const int64_t d = p + 8 > end ? p + 8 - end : 0;
+  v4u v = drop(load8(p - d), d < 8 ? (int)d : 8);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = n >= 2 * e + 2 ? v[e] : n == 2 * e + 1 ? v[e] & 0xFFFF : 0;
+  return v;
+}
+
 // ---------------------------------------------------------------------------
 // mid (and p): sums over a row's length
 // ---------------------------------------------------------------------------
@@ -126,9 +152,9 @@ __global__ __launch_bounds__(NW * 64) void lora_shrink_kernel(LoraArgs a) {
       const int left = a.len - k - o * 8;
       v4u xf[MR], wf[RT];
 #pragma unroll
-      for (int j = 0; j < MR; ++j) xf[j] = a.len - k >= 32 ? load8(x[j] + k) : load8_first(x[j] + k, left);
+      for (int j = 0; j < MR; ++j) xf[j] = a.len - k >= 32 ? load8(x[j] + k) : load8_end(x[j] + k, left, a.len);
 #pragma unroll
-      for (int i = 0; i < RT; ++i) wf[i] = a.len - k >= 32 ? load8(w[i] + k) : load8_first(w[i] + k, left);
+      for (int i = 0; i < RT; ++i) wf[i] = a.len - k >= 32 ? load8(w[i] + k) : load8_end(w[i] + k, left, a.len);
 #pragma unroll
       for (int j = 0; j < MR; ++j)
 #pragma unroll
@@ -237,6 +263,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
   // Loads are the same for every lane where a chunk of columns exists whole, from a
   // row that exists where the lane has none, so that they can be under way together:
   // those of the next 64 columns (and of the next 32 ranks) while these are multiplied.
+  const uint16_t* w_end = a.w.p + a.g.n * a.w.step;
   v4u y[MR][2], wf[4];
   auto load_w = [&](int ch, int k) {
     const int c0 = ch * 64 + (r >> 2) * 16 + (r & 3), at = k * 32 + o * 8;
@@ -253,7 +280,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = c0 + i * 4 < a.len ? c0 + i * 4 : a.len - 1;
-        wf[i] = load8_first(wp + c * a.w.ld + at, a.rank - at);
+        wf[i] = load8_inside(wp + c * a.w.ld + (at < a.rank ? at : 0), a.rank - at, w_end, a.g.n * a.w.step);
       }
     }
   };
@@ -265,7 +292,7 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint16_t* from = a.x + (token[j] < 0 ? 0 : token[j]) * a.ld_x;
-        y[j][h] = ch * 64 + 64 <= a.len ? load8(from + c + h * 8) : load8_first(from + (c < a.len ? c + h * 8 : 0), a.len - c - h * 8);
+        y[j][h] = ch * 64 + 64 <= a.len ? load8(from + c + h * 8) : load8_end(from + c + h * 8, a.len - c - h * 8, a.len);
       }
   };
 #pragma unroll
@@ -422,8 +449,8 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
     const int col = c0 + xc * 8;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint16_t* from = a.x + (t[i] < 0 ? 0 : t[i]) * a.ld_x + (whole_cols || col < a.len ? col : 0);
-      xr2[i] = whole_cols ? load8(from) : load8_first(from, a.len - col);
+      const uint16_t* from = a.x + (t[i] < 0 ? 0 : t[i]) * a.ld_x + col;
+      xr2[i] = whole_cols ? load8(from) : load8_end(from, a.len - col, a.len);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {

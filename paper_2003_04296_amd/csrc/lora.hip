@@ -409,8 +409,8 @@ __device__ __forceinline__ void put_grad(const LoraArgs& a, int e, int rows, int
 // their columns: they pass through registers into LDS rows of one token and are
 // read transposed.
 template <class T, int RT, bool FLIP>
-__global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
-  constexpr int C = 256, XP = BF16_PARTS<T>, XCH = 32 * C / 8, SCH = 32 * 128 / 8, STAGE = XCH * XP + SCH;
+__global__ __launch_bounds__(256, RT == 4 ? 2 : 3) void lora_grad_kernel(LoraArgs a) {
+  constexpr int C = 256, XCH = 32 * C / 8, SCH = 32 * 128 / 8, STAGE = XCH + SCH;
   [[maybe_unused]] __shared__ v4u store[2 * STAGE];
   [[maybe_unused]] __shared__ int tokens[GRAD_MOST + 64];  // and two stages of none
 #ifdef __HIP_DEVICE_COMPILE__
@@ -472,16 +472,13 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int k = threadIdx.x / 32 + i * 8;
-      v4u v[2];
-      in_bf16<T>(xr[i], v);
-#pragma unroll
-      for (int q = 0; q < XP; ++q) to[q * XCH + k * (C / 8) + (xc ^ swz_col(k))] = v[q];
+      to[k * (C / 8) + (xc ^ swz_col(k))] = xr[i];
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int k = threadIdx.x / 16 + i * 16;
       const Two t[4] = {two_parts(sr[i][0]), two_parts(sr[i][1]), two_parts(sr[i][2]), two_parts(sr[i][3])};
-      lds_v4u* const row = to + XP * XCH + k * 16;
+      lds_v4u* const row = to + XCH + k * 16;
       typedef __attribute__((address_space(3))) v2u* half;
       ((half)(row + ((sc / 8) ^ swz_col(k))))[sc / 4 & 1] =
           v2u{t[0].hi | (uint32_t)t[1].hi << 16, t[2].hi | (uint32_t)t[3].hi << 16};
@@ -505,12 +502,11 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int j = 0; j < RT; ++j) s[h][j] = fragment<32, 128, true>(now + XP * XCH, h * 64 + j * 16, 0);
+      for (int j = 0; j < RT; ++j) s[h][j] = fragment<32, 128, true>(now + XCH, h * 64 + j * 16, 0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      v4u x[XP];
-#pragma unroll
-      for (int q = 0; q < XP; ++q) x[q] = fragment<32, C, true>(now + q * XCH, wave * 64 + i * 16, 0);
+      v4u x[2];
+      in_bf16<T>(fragment<32, C, true>(now, wave * 64 + i * 16, 0), x);
 #pragma unroll
       for (int j = 0; j < RT; ++j) {
         auto add = [&](v4u xf, v4u sf) {
@@ -518,7 +514,7 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraArgs a) {
         };
         add(x[0], s[0][j]);
         add(x[0], s[1][j]);
-        if constexpr (XP == 2) add(x[1], s[0][j]);
+        if constexpr (BF16_PARTS<T> == 2) add(x[1], s[0][j]);
       }
     }
     if (at + 32 < here) put(lds + (b ^ 1) * STAGE);

@@ -152,8 +152,10 @@ __global__ __launch_bounds__(B / 64 * 128) void moe_gemm_w_kernel(GemmArgs a, Gr
   const int p = blockIdx.x / all;
   if (p >= pieces.total) return;
   const TileAt at = tile_at(blockIdx.x % all, per, a.tiles_c);
-  int e, piece;
-  pieces.find(g, p, e, piece);
+  int e, piece = 0;
+  // the longest sums first: the chip is then busy to the end
+  if (g.n <= 64 && pieces.total == g.n) e = group_by_size(g, p);
+  else pieces.find(g, p, e, piece);
   const GroupRows rows = group_rows(g, e);
   const int64_t begin = (int64_t)piece * size, first = __builtin_amdgcn_readfirstlane(rows.first) + begin;
   const int count = __builtin_amdgcn_readfirstlane(rows.count);
@@ -329,6 +331,8 @@ PlanW plan_weights(const qconv_moe_desc& d, bool gated, bool aligned) {
   int64_t size = round_up(d.rows * per / (2 * slots), 64);
   const int least = tile == 256 ? 1536 : 512;
   size = size < least ? least : size < 0x7fffff00 ? size : 0x7fffff00;
+  // a tile for each unit, and even all rows in one expert would be short
+  if (per * d.groups >= slots && d.rows <= 3 * size) return {tile, 0x7fffff00, 0};
   return {tile, (int)size, d.rows > size ? (size_t)(2 * ((d.rows + size - 1) / size) * halves * d.f * round_up(d.k, 4) * 4) : 0};
 }
 

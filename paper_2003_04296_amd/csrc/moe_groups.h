@@ -89,6 +89,17 @@ __device__ __forceinline__ int group_size(const Groups& g, int size, int most) {
   return __ballot(n > most) ? size : 0x7fffff00;
 }
 
+// The p-th largest of at most 64 groups (equal ones in their order).
+__device__ __forceinline__ int group_by_size(const Groups& g, int p) {
+  const int lane = threadIdx.x & 63, mine = lane < g.n ? group_rows(g, lane).count : -1;
+  int before = 0;
+  for (int e = 0; e < g.n; ++e) {
+    const int other = __builtin_amdgcn_readlane(mine, e);
+    before += other > mine || (other == mine && e < lane) ? 1 : 0;
+  }
+  return __builtin_ctzll(__ballot(lane < g.n && before == p));
+}
+
 // Where the sums over piece `piece` of a group of several are kept, if the group's
 // rows start at `first`: pieces of one group start `size` rows apart, so at most two
 // of groups with several start in the same `size` rows, and of these one is its

@@ -388,9 +388,9 @@ int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_co
 /* Rows that go to different weights: tokens sorted by expert and back, the   */
 /* experts' products, and low-rank adapters of many requests.  Which rows     */
 /* belong to which weight is known to the device alone: offsets[groups + 1]   */
-/* (device, int32; rows offsets[g] .. offsets[g + 1] are group g's).  Nothing  */
-/* synchronises.  Whatever the device arrays hold, no call touches memory     */
-/* outside its tensors.                                                       */
+/* (device, int32, from 0 on and never falling; rows offsets[g] ..            */
+/* offsets[g + 1] - 1 are group g's).  Nothing synchronises.  Whatever the    */
+/* device arrays hold, no call touches memory outside its tensors.            */
 /* ------------------------------------------------------------------------ */
 
 /* The most groups (experts, adapters). */

@@ -87,7 +87,9 @@ __device__ __forceinline__ v4u load8_inside(const uint16_t* p, int n, const uint
 
 // A block takes MR * 16 tokens by RT * 16 ranks; its waves, and the blocks of a
 // split product, take every so many-th 128 values of the rows, and are joined
-// through LDS (splits by whoever reads mid).
+// through LDS (splits by whoever reads mid).  Bound by reading x, 8192 tokens of 4096
+// bf16 at rank 32 in 21.6 us (3.1 TB/s; 31 while each load was waited for), and by its
+// latencies at few tokens (offsets, order, rows, the join): one token 4.0 us.
 template <class T, int MR, int RT, int NW>
 __global__ __launch_bounds__(NW * 64) void lora_shrink_kernel(LoraArgs a) {
   constexpr int R = MR * 16, C = RT * 16;
@@ -221,6 +223,8 @@ constexpr int BF16_PARTS = T::REST ? 1 : 2;
 // A block takes MR * 16 tokens; a wave 64 columns at a time.  The 16 rows of
 // operand i are columns (q / 4) * 16 + i * 4 + q % 4 of the 64, so that a lane
 // ends up with 16 columns in a row, which it reads and writes 16 bytes at a time.
+// Bound by HBM: 8192 tokens x 4096 bf16 read and written in 33 us (4.1 TB/s), gx of as
+// many, written alone, in 24; by latencies at few tokens, one token 5.0 us.
 template <class T, int MR>
 __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
   constexpr int R = MR * 16;
@@ -407,7 +411,8 @@ __device__ __forceinline__ void put_grad(const LoraArgs& a, int e, int rows, int
 
 // Results [rank][len] (ga), or with FLIP [len][rank] (gb).  Both operands run down
 // their columns: they pass through registers into LDS rows of one token and are
-// read transposed.
+// read transposed.  Bound by HBM and by the sums' start: 8192 tokens x 4096 bf16 at
+// rank 32 in 27 us (2.5 TB/s), three blocks a unit.
 template <class T, int RT, bool FLIP>
 __global__ __launch_bounds__(256, RT == 4 ? 2 : 3) void lora_grad_kernel(LoraArgs a) {
   constexpr int C = 256, XCH = 32 * C / 8, SCH = 32 * 128 / 8, STAGE = XCH + SCH;
@@ -596,11 +601,15 @@ __global__ __launch_bounds__(256) void lora_transpose_kernel(Transpose a) {
 int ld_mid(const qconv_lora_desc& d) { return (int)round_up(d.rank, 4); }
 size_t mid_bytes(const qconv_lora_desc& d) { return (size_t)round_up((int64_t)d.m * ld_mid(d) * 4, 16); }
 
-// Tokens of a piece: 32 where that makes enough pieces for the chip, else 16.
-int piece_rows(const qconv_lora_desc& d) { return d.m >= 32 * 128 ? 32 : 16; }
+// Tokens of a piece.  With 32 the adapters are read half as often, with 16 twice as
+// many blocks share the chip.  us of a forward of 4096 -> 4096 with 16 and 32: rank 16,
+// 4096 tokens of 4 adapters 30.4 and 36.0, 8192 of 64 53.9 and 47.9; rank 64, 2048
+// tokens 40.9 and 31.3, 8192 96.8 and 69.4.
+int piece_rows(const qconv_lora_desc& d) { return d.m >= (d.rank > 32 ? 2048 : 8192) ? 32 : 16; }
 
 // Blocks that share the sums over a row of `len` values: until there are about
-// 512 of them, as long as each wave has 128 values.
+// 512 of them, as long as each wave has 128 values (one token of 4096 inputs: 8.5 us of
+// a forward with 4 blocks, 11.3 with one).
 int shrink_parts(const qconv_lora_desc& d, int len) {
   const int R = piece_rows(d);
   const int64_t blocks = GroupPieces::most(d.m, d.groups, R) * ceil_div(d.rank, 64);
@@ -629,8 +638,10 @@ int run_shrink(LoraArgs& a, int rows, hipStream_t s) {
 template <class T>
 int run_expand(LoraArgs& a, int rows, hipStream_t s) {
   const int64_t pieces = a.g.rows / rows + (a.g.n + 1 < a.g.rows ? a.g.n + 1 : a.g.rows);
-  // a block per 256 columns while there are at most about 2048
-  const int64_t most = ceil_div(a.len, 256), want = 2048 / pieces;
+  // a block per 256 columns while there are at most about 1024: more read an adapter's
+  // offsets and mid for fewer columns each (rank 16, 4096 -> 8192, us of a forward with
+  // 512, 1024 and 2048: 13.6, 13.0 and 14.2 for 512 tokens, 30.5, 28.3 and 29.2 for 2048)
+  const int64_t most = ceil_div(a.len, 256), want = 1024 / pieces;
   a.tiles = (int)(want < 1 ? 1 : want < most ? want : most);
   if (pieces * a.tiles >= (1 << 23)) return QCONV_EUNSUPPORTED;
   const size_t lds = (size_t)rows * (ceil_div(a.rank, 32) * 8 + 1) * 16;
@@ -640,7 +651,8 @@ int run_expand(LoraArgs& a, int rows, hipStream_t s) {
   return hip_status();
 }
 
-// Tokens of a piece of a weight gradient: as many as make about 1024 blocks.
+// Tokens of a piece of a weight gradient: as many as make about 1024 blocks (8192
+// tokens x 4096 at rank 32: 27 us and 7.6 of the join; with 600 blocks 34 and 5.7).
 int grad_rows(const LoraArgs& a, int len) {
   const int64_t n = (int64_t)a.g.rows * ceil_div(len, 256) * ceil_div(a.rank, 64) / 1024;
   return n < 128 ? 128 : n < GRAD_MOST ? (int)round_up(n, 32) : GRAD_MOST;

@@ -60,7 +60,7 @@ def _check_sort(ids, groups, **kw):
 @pytest.mark.parametrize("wide", [torch.int32, torch.int64])
 @pytest.mark.parametrize("tokens,slots,groups", [
     (1, 1, 1), (1, 8, 64), (3, 2, 1), (16, 4, 64), (63, 1, 7), (64, 1, 63), (65, 1, 64), (1000, 3, 17), (1024, 1, 255),
-    (1025, 1, 256), (513, 2, 1023), (700, 3, 1024), (300, 1, 4096), (8192, 1, 8), (8193, 1, 8), (4097, 5, 129),
+    (1025, 1, 256), (513, 2, 1023), (700, 3, 1024), (300, 1, 4096), (4096, 1, 8), (4097, 1, 8), (8193, 1, 1000), (4097, 5, 129),
     (33000, 2, 300), (20000, 1, 4096), (9000, 1, 1500)])
 def test_sort(dev, tokens, slots, groups, wide):
     gen = _gen(dev, tokens + groups)
@@ -119,7 +119,8 @@ def _near(got, want, bound, what):
 
 
 SIZES = [(1, 1, 1), (1, 8, 4096), (2, 3, 7), (5, 1, 8), (17, 2, 63), (64, 4, 64), (33, 5, 129), (7, 9, 515), (100, 6, 1000),
-         (3, 2, 2051), (257, 2, 1024), (9, 3, 9000)]
+         (3, 2, 2051), (257, 2, 1024), (9, 3, 9000),
+         (2049, 2, 500), (2048, 3, 520)]
 
 
 @pytest.mark.parametrize("drop", [0.0, 0.3])

@@ -212,8 +212,8 @@ __global__ __launch_bounds__(NW * 64) void moe_rows_kernel(RowsArgs a, Groups g,
   __shared__ v4u xs[16 * rows_ld(NW) / 8];
   const GroupPieces pieces(g, 16);
   // as in dense_rows_kernel, the pieces in place of the token tiles
-  const int many = pieces.total, nt = many ? blockIdx.x / (8 * many) * 8 + blockIdx.x % 8 : a.tiles_n;
-  if (nt >= a.tiles_n) return;
+  const uint32_t many = pieces.total, nt = many ? blockIdx.x / (8ull * many) * 8 + blockIdx.x % 8 : a.tiles_n;
+  if (nt >= (uint32_t)a.tiles_n) return;
   int e, piece;
   pieces.find(g, blockIdx.x / 8 % many, e, piece);
   const GroupRows rows = group_rows(g, e);

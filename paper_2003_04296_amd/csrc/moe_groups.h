@@ -45,11 +45,15 @@ struct GroupPieces {
   int upto;       // pieces of the groups up to and with this lane's
   int total;
 
+  // At most MOST, far above what is ever launched: sums over offsets of no order, where
+  // groups share rows, stay inside an int.
+  static constexpr int MOST = 1 << 24;
   __device__ __forceinline__ int of(const Groups& g, int e) const {
     if (e >= g.n) return 0;
     const int rows = group_rows(g, e).count;
     if (several) return rows > size ? 1 : 0;
-    return rows > 0 ? (int)(((int64_t)rows + size - 1) / size) : empty ? 1 : 0;
+    const int n = rows > 0 ? (rows - 1) / size + 1 : empty ? 1 : 0;
+    return n < MOST ? n : MOST;
   }
   __device__ __forceinline__ GroupPieces(const Groups& g, int size_, bool empty_ = false, bool several_ = false)
       : size(size_), empty(empty_), several(several_) {
@@ -57,7 +61,7 @@ struct GroupPieces {
     per = (g.n + 63) / 64;
     int mine = 0;
     for (int i = 0; i < per; ++i) mine += of(g, lane * per + i);
-    upto = wave_sums(mine);
+    upto = wave_sums(mine < MOST ? mine : MOST);
     total = __builtin_amdgcn_readlane(upto, 63);
   }
   // The group of piece p < total, and the piece's number in it.

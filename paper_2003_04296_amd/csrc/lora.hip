@@ -91,16 +91,9 @@ __device__ __forceinline__ v4u load8_inside(const uint16_t* p, int n, const uint
 // bf16 at rank 32 in 21.6 us (3.1 TB/s; 31 while each load was waited for), and by its
 // latencies at few tokens (offsets, order, rows, the join): one token 4.0 us.
 template <class T, int MR, int RT, int NW>
-__global__ __launch_bounds__(NW * 64) void lora_shrink_kernel(LoraArgs a) {
-  constexpr int R = MR * 16, C = RT * 16;
-  __shared__ v4f part[NW][R][C / 4];
-  const GroupPieces pieces(a.g, R);
-  const int split = blockIdx.x % a.parts, tile = blockIdx.x / a.parts % a.tiles, p = blockIdx.x / a.parts / a.tiles;
-  if (p >= pieces.total) return;
-  int e, piece;
-  pieces.find(a.g, p, e, piece);
-  const GroupRows rows = group_rows(a.g, e);
-  const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
+__device__ __forceinline__ void shrink(const LoraArgs& a, int e, int first, int here, int tile, int split,
+                                       v4f (&part)[NW][MR * 16][RT * 4]) {
+  constexpr int C = RT * 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, o = lane >> 4;
   // in place of rows past the piece its first one, of ranks past the last that one: their sums go nowhere
@@ -168,13 +161,33 @@ __global__ __launch_bounds__(NW * 64) void lora_shrink_kernel(LoraArgs a) {
 #pragma unroll
     for (int i = 0; i < RT; ++i) part[wave][j * 16 + r][i * 4 + o] = acc[j][i];
   __syncthreads();
+}
+// The sum of a row's ranks [c * 4, + 4), after shrink.
+template <int R, int C, int NW>
+__device__ __forceinline__ v4f shrink_sum(const v4f (&part)[NW][R][C], int row, int c) {
+  v4f s = part[0][row][c];
+#pragma unroll
+  for (int v = 1; v < NW; ++v) s += part[v][row][c];
+  return s;
+}
+
+template <class T, int MR, int RT, int NW>
+__global__ __launch_bounds__(NW * 64) void lora_shrink_kernel(LoraArgs a) {
+  constexpr int R = MR * 16, C = RT * 16;
+  __shared__ v4f part[NW][R][C / 4];
+  const GroupPieces pieces(a.g, R);
+  const int split = blockIdx.x % a.parts, tile = blockIdx.x / a.parts % a.tiles, p = blockIdx.x / a.parts / a.tiles;
+  if (p >= pieces.total) return;
+  int e, piece;
+  pieces.find(a.g, p, e, piece);
+  const GroupRows rows = group_rows(a.g, e);
+  const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
+  shrink<T, MR, RT, NW>(a, e, first, here, tile, split, part);
   for (int i = threadIdx.x; i < here * (C / 4); i += NW * 64) {
     const int row = i / (C / 4), c = i % (C / 4);
-    v4f s = part[0][row][c];
-#pragma unroll
-    for (int v = 1; v < NW; ++v) s += part[v][row][c];
     if (tile * C + c * 4 < a.ld_mid)
-      *(v4f*)(a.mid + ((int64_t)split * a.g.rows + first + row) * a.ld_mid + tile * C + c * 4) = s;
+      *(v4f*)(a.mid + ((int64_t)split * a.g.rows + first + row) * a.ld_mid + tile * C + c * 4) =
+          shrink_sum(part, row, c);
   }
 }
 
@@ -225,51 +238,72 @@ constexpr int BF16_PARTS = T::REST ? 1 : 2;
 // ends up with 16 columns in a row, which it reads and writes 16 bytes at a time.
 // Bound by HBM: 8192 tokens x 4096 bf16 read and written in 33 us (4.1 TB/s), gx of as
 // many, written alone, in 24; by latencies at few tokens, one token 5.0 us.
-template <class T, int MR>
-__global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
-  constexpr int R = MR * 16;
-  extern __shared__ v4u lds[];  // [R][ranks of hi, then of lo, in chunks of 8, and one to spread the banks]
-  const GroupPieces pieces(a.g, R);
-  const int tile = blockIdx.x % a.tiles, p = blockIdx.x / a.tiles;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15, o = lane >> 4;
-  const int chunks = (a.len + 63) / 64;
-  if (p >= pieces.total) {
-    // tokens of no adapter: a copy, or zeros
-    const int end = a.g.offsets[a.g.n], begin = end < 0 ? 0 : end;
-    const int64_t row0 = (int64_t)begin + (int64_t)(p - pieces.total) * R;
-    if (row0 >= a.g.rows || a.x == a.out) return;
-    for (int c = tile * 4 + wave; c < chunks; c += a.tiles * 4)
-      for (int j = 0; j < R; j += 8) {
-        const int row = j + lane / 8, col = c * 64 + lane % 8 * 8;
-        if (row0 + row >= a.g.rows || col >= a.len) continue;
-        const int t = token_at(a, (int)row0 + row);
-        if (t < 0) continue;
-        const v4u v = a.x ? load8_first(a.x + t * a.ld_x + col, a.len - col) : v4u{0, 0, 0, 0};
-        uint16_t* to = a.out + t * a.ld_out + col;
-        if (col + 8 <= a.len) {
-          reinterpret_cast<U128*>(to)->v = v;
-        } else {
-          for (int q = 0; col + q < a.len; ++q) to[q] = (uint16_t)(v[q / 2] >> (16 * (q & 1)));
-        }
+// Tokens of no adapter: a copy, or zeros.  Rows [row0, + R) of the order, by `waves`
+// waves, of which this is number `wave` of the columns' (`step` of them).
+template <int R>
+__device__ __forceinline__ void pass_rows(const LoraArgs& a, int64_t number, int first_chunk, int step) {
+  const int lane = threadIdx.x & 63, chunks = (a.len + 63) / 64;
+  const int end = a.g.offsets[a.g.n], begin = end < 0 ? 0 : end;
+  const int64_t row0 = (int64_t)begin + number * R;
+  if (row0 >= a.g.rows || a.x == a.out) return;
+  for (int c = first_chunk; c < chunks; c += step)
+    for (int j = 0; j < R; j += 8) {
+      const int row = j + lane / 8, col = c * 64 + lane % 8 * 8;
+      if (row0 + row >= a.g.rows || col >= a.len) continue;
+      const int t = token_at(a, (int)row0 + row);
+      if (t < 0) continue;
+      const v4u v = a.x ? load8_first(a.x + t * a.ld_x + col, a.len - col) : v4u{0, 0, 0, 0};
+      uint16_t* to = a.out + t * a.ld_out + col;
+      if (col + 8 <= a.len) {
+        reinterpret_cast<U128*>(to)->v = v;
+      } else {
+        for (int q = 0; col + q < a.len; ++q) to[q] = (uint16_t)(v[q / 2] >> (16 * (q & 1)));
       }
-    return;
-  }
-  int e, piece;
-  pieces.find(a.g, p, e, piece);
-  const GroupRows rows = group_rows(a.g, e);
-  const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
-  const int steps = (a.rank + 31) / 32, ld = steps * 8 + 1;  // in chunks
-  int token[MR];
+    }
+}
+
+// mid's values [c, c + 4) of a row of the second product's operand in LDS (zeros past
+// the rank): rows of `steps` * 4 chunks of hi, as many of lo, and one to spread the banks.
+__device__ __forceinline__ void put_mid(v4u* lds, int steps, int row, int c, int rank, v4f s) {
 #pragma unroll
-  for (int j = 0; j < MR; ++j) token[j] = j * 16 + r < here ? token_at(a, first + j * 16 + r) : -1;
-  const uint16_t* wp = a.w.p + e * a.w.step;
+  for (int q = 0; q < 4; ++q)
+    if (c + q >= rank) s[q] = 0.0f;
+  const Two t[4] = {two_parts(s[0]), two_parts(s[1]), two_parts(s[2]), two_parts(s[3])};
+  v2u* to = (v2u*)(lds + row * (steps * 8 + 1)) + c / 4;
+  to[0] = v2u{t[0].hi | (uint32_t)t[1].hi << 16, t[2].hi | (uint32_t)t[3].hi << 16};
+  to[steps * 8] = v2u{t[0].lo | (uint32_t)t[1].lo << 16, t[2].lo | (uint32_t)t[3].lo << 16};
+}
+
+// A wave's columns of a piece: chunks of 64 from `ch` on, every `step`-th.  start()
+// puts the first loads under way, run() needs the operand in LDS.
+template <class T, int MR>
+struct Columns {
+  const LoraArgs& a;
+  int r, o, steps, chunks;
+  const uint16_t *wp, *w_end;
+  int token[MR];
+  v4u y[MR][2], wf[4];
+  float scale;
+
+  __device__ __forceinline__ Columns(const LoraArgs& args, int e, int first, int here) : a(args) {
+    const int lane = threadIdx.x & 63;
+    r = lane & 15;
+    o = lane >> 4;
+    steps = (a.rank + 31) / 32;
+    chunks = (a.len + 63) / 64;
+    wp = a.w.p + e * a.w.step;
+    w_end = a.w.p + a.g.n * a.w.step;
+    scale = a.scale ? a.scale[e] : 1.0f;
+#pragma unroll
+    for (int j = 0; j < MR; ++j) {
+      token[j] = j * 16 + r < here ? token_at(a, first + j * 16 + r) : -1;
+      y[j][0] = y[j][1] = v4u{0, 0, 0, 0};
+    }
+  }
   // Loads are the same for every lane where a chunk of columns exists whole, from a
   // row that exists where the lane has none, so that they can be under way together:
   // those of the next 64 columns (and of the next 32 ranks) while these are multiplied.
-  const uint16_t* w_end = a.w.p + a.g.n * a.w.step;
-  v4u y[MR][2], wf[4];
-  auto load_w = [&](int ch, int k) {
+  __device__ __forceinline__ void load_w(int ch, int k) {
     const int c0 = ch * 64 + (r >> 2) * 16 + (r & 3), at = k * 32 + o * 8;
     if (a.rank % 8 == 0) {
       const bool in = at < a.rank;
@@ -287,8 +321,8 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
         wf[i] = load8_inside(wp + c * a.w.ld + (at < a.rank ? at : 0), a.rank - at, w_end, a.g.n * a.w.step);
       }
     }
-  };
-  auto load_y = [&](int ch) {
+  }
+  __device__ __forceinline__ void load_y(int ch) {
     if (!a.x) return;
     const int c = ch * 64 + o * 16;
 #pragma unroll
@@ -298,16 +332,95 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
         const uint16_t* from = a.x + (token[j] < 0 ? 0 : token[j]) * a.ld_x;
         y[j][h] = ch * 64 + 64 <= a.len ? load8(from + c + h * 8) : load8_end(from + c + h * 8, a.len - c - h * 8, a.len);
       }
-  };
-#pragma unroll
-  for (int j = 0; j < MR; ++j) y[j][0] = y[j][1] = v4u{0, 0, 0, 0};
-  int ch = tile * 4 + wave;
-  if (ch < chunks) {
-    load_w(ch, 0);
-    load_y(ch);
   }
-  const float scale = a.scale ? a.scale[e] : 1.0f;
-  // mid's rows: summed over its parts, zeros past the rank
+  __device__ __forceinline__ void start(int ch) {
+    if (ch < chunks) {
+      load_w(ch, 0);
+      load_y(ch);
+    }
+  }
+  __device__ __forceinline__ void run(const v4u* lds, int ch, int step) {
+    const int ld = steps * 8 + 1;
+    v4f acc[MR][4];
+#pragma unroll
+    for (int j = 0; j < MR; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    v4u base[MR][2];
+    for (int k = 0; ch < chunks;) {
+      v4u w[4][2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) in_bf16<T>(wf[i], w[i]);
+      if (k == 0) {
+#pragma unroll
+        for (int j = 0; j < MR; ++j) base[j][0] = y[j][0], base[j][1] = y[j][1];
+      }
+      const int here_ch = ch, here_k = k;
+      if (++k == steps) {
+        k = 0;
+        ch += step;
+      }
+      if (ch < chunks) {
+        load_w(ch, k);
+        if (k == 0) load_y(ch);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < MR; ++j) {
+        const v4u* s = lds + (j * 16 + r) * ld + here_k * 4 + o;
+        const v4u hi = s[0], lo = s[steps * 4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[j][i] = BF16::mfma(w[i][0], hi, acc[j][i]);
+          acc[j][i] = BF16::mfma(w[i][0], lo, acc[j][i]);
+          if constexpr (BF16_PARTS<T> == 2) acc[j][i] = BF16::mfma(w[i][1], hi, acc[j][i]);
+        }
+      }
+      if (k != 0) continue;
+      const int mine = here_ch * 64 + o * 16;
+#pragma unroll
+      for (int j = 0; j < MR; ++j) {
+        if (token[j] >= 0) {
+          uint16_t* to = a.out + token[j] * a.ld_out + mine;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint16_t v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              v[q] = T::down(fmaf(scale, acc[j][h * 2 + q / 4][q % 4], T::up((uint16_t)(base[j][h][q / 2] >> (16 * (q & 1))))));
+            if (mine + h * 8 + 8 <= a.len) {
+              reinterpret_cast<U128*>(to + h * 8)->v =
+                  v4u{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
+                      v[6] | (uint32_t)v[7] << 16};
+            } else {
+#pragma unroll
+              for (int q = 0; q < 8; ++q)
+                if (mine + h * 8 + q < a.len) to[h * 8 + q] = v[q];
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+  }
+};
+
+template <class T, int MR>
+__global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
+  constexpr int R = MR * 16;
+  extern __shared__ v4u lds[];
+  const GroupPieces pieces(a.g, R);
+  const int tile = blockIdx.x % a.tiles, p = blockIdx.x / a.tiles;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (p >= pieces.total) return pass_rows<R>(a, p - pieces.total, tile * 4 + wave, a.tiles * 4);
+  int e, piece;
+  pieces.find(a.g, p, e, piece);
+  const GroupRows rows = group_rows(a.g, e);
+  const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
+  Columns<T, MR> columns(a, e, first, here);
+  columns.start(tile * 4 + wave);
+  const int steps = columns.steps;
   for (int i = threadIdx.x; i < R * steps * 8; i += 256) {
     const int row = i / (steps * 8), c = i % (steps * 8) * 4;
     v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -316,78 +429,41 @@ __global__ __launch_bounds__(256) void lora_expand_kernel(LoraArgs a) {
       s = *(const v4f*)m;
 #pragma unroll 4
       for (int q = 1; q < a.parts; ++q) s += *(const v4f*)(m + (int64_t)q * a.g.rows * a.ld_mid);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (c + q >= a.rank) s[q] = 0.0f;
     }
-    const Two t[4] = {two_parts(s[0]), two_parts(s[1]), two_parts(s[2]), two_parts(s[3])};
-    v2u* to = (v2u*)(lds + row * ld) + i % (steps * 8);
-    to[0] = v2u{t[0].hi | (uint32_t)t[1].hi << 16, t[2].hi | (uint32_t)t[3].hi << 16};
-    to[steps * 8] = v2u{t[0].lo | (uint32_t)t[1].lo << 16, t[2].lo | (uint32_t)t[3].lo << 16};
+    put_mid(lds, steps, row, c, a.rank, s);
   }
   __syncthreads();
-  v4f acc[MR][4];
-#pragma unroll
-  for (int j = 0; j < MR; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  v4u base[MR][2];
-  for (int k = 0; ch < chunks;) {
-    v4u w[4][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) in_bf16<T>(wf[i], w[i]);
-    if (k == 0) {
-#pragma unroll
-      for (int j = 0; j < MR; ++j) base[j][0] = y[j][0], base[j][1] = y[j][1];
-    }
-    const int here_ch = ch, here_k = k;
-    if (++k == steps) {
-      k = 0;
-      ch += a.tiles * 4;
-    }
-    if (ch < chunks) {
-      load_w(ch, k);
-      if (k == 0) load_y(ch);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int j = 0; j < MR; ++j) {
-      const v4u* s = lds + (j * 16 + r) * ld + here_k * 4 + o;
-      const v4u hi = s[0], lo = s[steps * 4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        acc[j][i] = BF16::mfma(w[i][0], hi, acc[j][i]);
-        acc[j][i] = BF16::mfma(w[i][0], lo, acc[j][i]);
-        if constexpr (BF16_PARTS<T> == 2) acc[j][i] = BF16::mfma(w[i][1], hi, acc[j][i]);
-      }
-    }
-    if (k != 0) continue;
-    const int mine = here_ch * 64 + o * 16;
-#pragma unroll
-    for (int j = 0; j < MR; ++j) {
-      if (token[j] >= 0) {
-        uint16_t* to = a.out + token[j] * a.ld_out + mine;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint16_t v[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            v[q] = T::down(fmaf(scale, acc[j][h * 2 + q / 4][q % 4], T::up((uint16_t)(base[j][h][q / 2] >> (16 * (q & 1))))));
-          if (mine + h * 8 + 8 <= a.len) {
-            reinterpret_cast<U128*>(to + h * 8)->v =
-                v4u{v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
-                    v[6] | (uint32_t)v[7] << 16};
-          } else {
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-              if (mine + h * 8 + q < a.len) to[h * 8 + q] = v[q];
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+  columns.run(lds, tile * 4 + wave, a.tiles * 4);
+}
+
+// Both products of few tokens in one launch: a block sums mid by itself, as every
+// block of the piece's columns does (the adapter's a then comes from L2).  Bound by its
+// latencies: offsets, order, rows, the join of the waves, the second product.
+template <class T, int RT, int NW>
+__global__ __launch_bounds__(NW * 64) void lora_few_kernel(LoraArgs in, LoraArgs a) {
+  constexpr int R = 16, C = RT * 16, STEPS = (RT + 1) / 2;
+  __shared__ v4f part[NW][R][C / 4];
+  __shared__ v4u lds[R * (STEPS * 8 + 1)];
+  const GroupPieces pieces(a.g, R);
+  const int tile = blockIdx.x % a.tiles, p = blockIdx.x / a.tiles;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ch = tile * NW + wave;
+  if (p >= pieces.total) return pass_rows<R>(a, p - pieces.total, ch, a.tiles * NW);
+  int e, piece;
+  pieces.find(a.g, p, e, piece);
+  const GroupRows rows = group_rows(a.g, e);
+  const int first = rows.first + piece * R, here = rows.count - piece * R < R ? rows.count - piece * R : R;
+  Columns<T, 1> columns(a, e, first, here);
+  columns.start(ch);
+  shrink<T, 1, RT, NW>(in, e, first, here, 0, 0, part);
+  for (int i = threadIdx.x; i < R * columns.steps * 8; i += NW * 64) {
+    const int row = i / (columns.steps * 8), c = i % (columns.steps * 8);
+    const bool on = row < here && c * 4 < a.rank;
+    const v4f s = on ? shrink_sum(part, row, c) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    if (on && tile == 0 && in.mid) *(v4f*)(in.mid + (int64_t)(first + row) * in.ld_mid + c * 4) = s;
+    put_mid(lds, columns.steps, row, c * 4, a.rank, s);
   }
+  __syncthreads();
+  columns.run(lds, ch, a.tiles * NW);
 }
 
 // ---------------------------------------------------------------------------
@@ -651,6 +727,31 @@ int run_expand(LoraArgs& a, int rows, hipStream_t s) {
   return hip_status();
 }
 
+// The tokens that one launch serves: sums that are short, or few tokens, for which the
+// second launch costs the host as much (4.5 us) as the kernels differ.  us on the device
+// in one launch and in two (in a graph): 1024 -> 1024 at rank 16 5.6 and 7.9 for one token, 7.2 and
+// 9.3 for 1024 tokens of 40 adapters, at rank 64 10.1 and 11.8, 12.5 and 13.4; 4096 -> 4096 at
+// rank 16 9.0 and 8.5 for one token, 12.2 and 9.9 for 64 of 40, at rank 64 21 and 12.8.
+// Sixteen waves a block instead of eight: 9.9 in place of 9.0.
+constexpr int FEW_BLOCKS = 256;
+bool few_tokens(const qconv_lora_desc& d) {
+  if (d.rank > 64) return false;
+  const int64_t pieces = GroupPieces::most(d.m, d.groups, 16), ranks = d.rank <= 16 ? 1 : d.rank <= 32 ? 2 : 4;
+  return (d.k <= 1024 && pieces <= 128) || (d.k * ranks <= 4096 && pieces <= 16);
+}
+
+template <class T>
+int run_few(LoraArgs& in, LoraArgs& a, hipStream_t s) {
+  const int64_t pieces = a.g.rows / 16 + (a.g.n + 1 < a.g.rows ? a.g.n + 1 : a.g.rows);
+  const int64_t most = ceil_div(a.len, 64 * NW), want = FEW_BLOCKS / pieces;
+  a.tiles = (int)(want < 1 ? 1 : want < most ? want : most);
+  const unsigned blocks = (unsigned)(pieces * a.tiles);
+  if (a.rank <= 16) lora_few_kernel<T, 1, NW><<<blocks, NW * 64, 0, s>>>(in, a);
+  else if (a.rank <= 32) lora_few_kernel<T, 2, NW><<<blocks, NW * 64, 0, s>>>(in, a);
+  else lora_few_kernel<T, 4, NW><<<blocks, NW * 64, 0, s>>>(in, a);
+  return hip_status();
+}
+
 // Tokens of a piece of a weight gradient: as many as make about 1024 blocks (8192
 // tokens x 4096 at rank 32: 27 us and 7.6 of the join; with 600 blocks 34 and 5.7).
 int grad_rows(const LoraArgs& a, int len) {
@@ -709,11 +810,22 @@ template <class T>
 int forward(const qconv_lora_desc& d, LoraArgs a, const void* x, const void* wa, const void* wb, const void* y, void* out,
             float* mid, void* ws, hipStream_t s) {
   const int rows = piece_rows(d);
-  a.parts = shrink_parts(d, d.k);
   a.len = d.k;
   a.x = (const uint16_t*)x;
   a.ld_x = d.ld_x;
   a.w = {(const uint16_t*)wa, d.k, (int64_t)d.rank * d.k};
+  LoraArgs b = a;
+  b.len = d.n;
+  b.x = (const uint16_t*)y;
+  b.ld_x = d.ld_y;
+  b.w = {(const uint16_t*)wb, d.rank, (int64_t)d.n * d.rank};
+  b.out = (uint16_t*)out;
+  b.ld_out = d.ld_out;
+  if (few_tokens(d)) {
+    a.mid = mid;
+    return run_few<T>(a, b, s);
+  }
+  a.parts = shrink_parts(d, d.k);
   a.mid = a.parts == 1 && mid ? mid : (float*)ws;
   int rc = run_shrink<T>(a, rows, s);
   if (rc == QCONV_OK && mid && a.parts > 1) {
@@ -721,13 +833,9 @@ int forward(const qconv_lora_desc& d, LoraArgs a, const void* x, const void* wa,
     a.mid = mid;
     a.parts = 1;
   }
-  a.len = d.n;
-  a.x = (const uint16_t*)y;
-  a.ld_x = d.ld_y;
-  a.w = {(const uint16_t*)wb, d.rank, (int64_t)d.n * d.rank};
-  a.out = (uint16_t*)out;
-  a.ld_out = d.ld_out;
-  return rc ? rc : run_expand<T>(a, rows, s);
+  b.mid = a.mid;
+  b.parts = a.parts;
+  return rc ? rc : run_expand<T>(b, rows, s);
 }
 
 struct BackBytes {
@@ -813,6 +921,7 @@ LoraArgs lora_args(const qconv_lora_desc& d, const int* offsets, const int* orde
 }  // namespace
 
 size_t lora_forward_bytes(const qconv_lora_desc& d, bool keep_mid) {
+  if (few_tokens(d)) return 0;
   const int parts = shrink_parts(d, d.k);
   return keep_mid && parts == 1 ? 0 : parts * mid_bytes(d);
 }

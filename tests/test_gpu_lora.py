@@ -108,6 +108,8 @@ SIZES = [
     (1, 1, 1, 1, 1), (1, 3, 16, 4096, 4096), (2, 2, 3, 5, 7), (15, 4, 4, 127, 63), (16, 1, 8, 128, 64), (17, 5, 15, 129, 65),
     (31, 2, 17, 200, 300), (33, 40, 24, 640, 264), (64, 7, 32, 1000, 1001), (70, 3, 33, 256, 100), (100, 2, 64, 2048, 520),
     (129, 9, 65, 96, 200), (50, 2, 130, 72, 136), (40, 3, 256, 300, 257),
+    # both sides of what one launch takes: 1024 inputs, 128 pieces, rank 64
+    (90, 4, 16, 1025, 72), (20, 3, 33, 1032, 40), (1950, 6, 12, 64, 72), (2100, 6, 12, 64, 72), (30, 20, 20, 2500, 130),
 ]
 
 

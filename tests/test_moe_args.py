@@ -154,11 +154,11 @@ def test_lora_pointers_and_sizes():
             assert L.qconv_lora_forward(_lora(), *a, P, 1 << 40, None) == q.QCONV_EINVAL, (i, v)
     assert L.qconv_lora_forward(_lora(ld_out=25), *ok, P, 1 << 40, None) == q.QCONV_EINVAL  # y itself, by another stride
     assert L.qconv_lora_forward(_lora(ld_out=23), *ok, P, 1 << 40, None) == q.QCONV_EINVAL
-    need = L.qconv_lora_forward_bytes(_lora(), 0)
-    assert need > 0
-    assert L.qconv_lora_forward(_lora(), *ok[:8], None, P, need - 1, None) == q.QCONV_EWORKSPACE
-    assert L.qconv_lora_forward(_lora(), *ok[:8], None, None, need, None) == q.QCONV_EINVAL
-    assert L.qconv_lora_forward(_lora(), *ok[:8], None, P + 8, need, None) == q.QCONV_EINVAL
+    need = L.qconv_lora_forward_bytes(_lora(m=4096), 0)
+    assert need > 0 and L.qconv_lora_forward_bytes(_lora(), 0) == 0
+    assert L.qconv_lora_forward(_lora(m=4096), *ok[:8], None, P, need - 1, None) == q.QCONV_EWORKSPACE
+    assert L.qconv_lora_forward(_lora(m=4096), *ok[:8], None, None, need, None) == q.QCONV_EINVAL
+    assert L.qconv_lora_forward(_lora(m=4096), *ok[:8], None, P + 8, need, None) == q.QCONV_EINVAL
     ok = [P] * 11  # x, a, b, offsets, order, scale, mid, gy, gx, ga, gb
     for i in range(11):
         for v in (None, P + 1):

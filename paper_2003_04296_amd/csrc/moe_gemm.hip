@@ -308,7 +308,9 @@ int run_weights_t(GemmArgs& a, const Groups& g, int64_t step_out, int tile, int 
 
 // The products whose rows are the batch's: tiles of 256 x 256 where there are
 // enough for the 256 compute units and the experts' rows, on average, fill three
-// quarters of one, else 128 x 128.  Few of those are split as in gemm_plan, and until
+// quarters of one, or fewer with long sums, which all count as last ones then (gx of
+// 4096 rows of 8 experts, 4096 -> 1024, with its slopes: 142 us against 208 in small
+// tiles), else 128 x 128.  Few of those are split as in gemm_plan, and until
 // there are two for each unit as long as each part keeps 1024 products: us of the linear
 // forward with a block and with two for each unit, weights from memory: 700 rows of 8
 // experts 4096 -> 1024 42.3 and 31.7, 600 of 3 4096 -> 4096 66.6 and 51.7; with fewer
@@ -318,7 +320,11 @@ GemmPlan plan_rows(const qconv_moe_desc& d, int cols, int64_t products, bool gat
     const int64_t n = GroupPieces::most(d.rows, d.groups, b) * ceil_div(cols, gated ? b / 2 : b);
     return n > 0 ? n : 1;
   };
-  if (aligned && d.rows >= 192 * (int64_t)d.groups && tiles(256) >= 256) return {256, 1, (size_t)256 * TAIL_TILE * 4};
+  // the tiles there will be if half of the experts' last ones are full
+  const int64_t likely = (d.rows / 256 * 2 + (int64_t)d.groups) * ceil_div(cols, gated ? 128 : 256) / 2;
+  const bool long_sums = likely > 0 && likely <= 256 && 256 / likely * likely >= 192 && products / (256 / likely) >= 2048;
+  if (aligned && d.rows >= 192 * (int64_t)d.groups && (tiles(256) >= 256 || long_sums))
+    return {256, 1, (size_t)256 * TAIL_TILE * 4};
   const int64_t small = tiles(128);
   int64_t parts = small >= 192 ? 1 : 256 / small;
   if (parts > products / 512) parts = products / 512;

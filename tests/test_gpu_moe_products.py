@@ -185,3 +185,39 @@ def test_no_rows(dev):
     assert q.moe_linear_forward(x, wg, offsets).shape == (0, 20)
     gx, gw = q.moe_linear_backward(x, wg, offsets, gh)
     assert gx.shape == (0, 33) and not gw.any()
+
+
+@pytest.mark.parametrize("counts,k,f", [
+    ([1500, 1300, 40], 2048, 6000),  # forward and gx: the last large tiles split over idle units
+    ([3400, 0, 2700], 2048, 4096),   # weight gradients: large tiles, the longer expert in pieces
+    ([2400, 300], 520, 1000),        # the same in small tiles
+    ([2, 130, 60], 4100, 120),       # few tiles of long sums
+])
+def test_split_sums(dev, counts, k, f):
+    x, wg, wu, gh, offsets = _problem(dev, counts, 2, k, f, torch.bfloat16)
+    h, pre, grads = _run_gated(x, wg, wu, gh, offsets, q.ACT_SILU)
+    _check_gated(counts, 2, x, wg, wu, gh, h, pre, grads, "silu")
+    y = q.moe_linear_forward(x, wg, offsets, out=torch.full_like(gh, 7.0))
+    gx, gw = q.moe_linear_backward(x, wg, offsets, gh, out=(torch.full_like(x, 7.0), None))
+    for e, i, j in _groups(counts):
+        if i == j:
+            assert not gw[e].any()
+            continue
+        for got, (v, bound), what in zip((y[i:j], gx[i:j], gw[e]), _linear(x[i:j], wg[e], gh[i:j]), ("y", "gx", "gw")):
+            _close(got, v, bound, f"{what} of group {e}")
+    end = sum(counts)
+    assert bool((y[end:] == 7.0).all()) and bool((gx[end:] == 7.0).all())
+
+
+def test_rows_before_the_first_group(dev):
+    """Offsets that do not start at 0: the rows before the first group are no group's, split sums or not."""
+    for counts, k, f in (([20, 200], 96, 72), ([2, 130, 60], 4100, 120), ([5, 3], 2048, 64)):
+        x, wg, wu, gh, offsets = _problem(dev, counts, 9, k, f, torch.float16)
+        offsets = offsets + 6
+        h, pre, grads = _run_gated(x, wg, wu, gh, offsets, q.ACT_RELU)
+        y = q.moe_linear_forward(x, wg, offsets, out=torch.full_like(gh, 7.0))
+        end = 6 + sum(counts)
+        for t in (h, y, grads[0]):
+            assert bool((t[:6] == 7.0).all()) and bool((t[end:] == 7.0).all())
+        fp = (f + 7) // 8 * 8
+        _check_gated(counts, 3, x[6:], wg, wu, gh[6:], h[6:], pre[6 * 2 * fp:], (grads[0][6:], *grads[1:]), "relu")

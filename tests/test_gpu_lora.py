@@ -134,7 +134,7 @@ def test_forward_and_backward(dev, m, groups, rank, k, n, how, dtype):
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
-@pytest.mark.parametrize("m,groups,rank,k,n,how", [(8200, 5, 16, 264, 300, "runs"), (2050, 5, 40, 264, 300, "runs"), (5000, 3, 64, 200, 128, "mixed"),
+@pytest.mark.parametrize("m,groups,rank,k,n,how", [(8200, 5, 16, 264, 300, "runs"), (8200, 5, 24, 264, 300, "mixed"), (2050, 5, 40, 264, 300, "runs"), (5000, 3, 64, 200, 128, "mixed"),
                                                    (1500, 2, 20, 1100, 77, "one"), (513, 2, 8, 64, 72, "one"),
                                                    (4096, 300, 8, 128, 40, "mixed"), (6000, 4096, 4, 40, 24, "mixed")])
 def test_many_tokens(dev, m, groups, rank, k, n, how, dtype):

@@ -140,9 +140,10 @@ def test_many_groups(dev, groups):
 
 @pytest.mark.parametrize("k,f", [(61, 45), (96, 40), (200, 129)])
 @pytest.mark.parametrize("counts", [[40, 7, 150], [800, 400]])
-def test_rows_of_wider_tensors(dev, counts, k, f):
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_rows_of_wider_tensors(dev, counts, k, f, dtype):
     """Row strides past the columns, odd addresses, and NaN beside every row of every operand."""
-    x, wg, wu, gh, offsets = _problem(dev, counts, 2, k, f, torch.float16)
+    x, wg, wu, gh, offsets = _problem(dev, counts, 2, k, f, TYPES[dtype])
 
     def inside(t, off, pad):
         rows = t.reshape(-1, t.shape[-1])
@@ -151,7 +152,7 @@ def test_rows_of_wider_tensors(dev, counts, k, f):
         v.copy_(rows)
         return v if t.dim() == 2 else b.as_strided(t.shape, (t.shape[1] * b.stride(0), b.stride(0), 1), off)
 
-    for off, pad in ((1, 3), (0, 8), (4, 11)):
+    for off, pad in ((1, 3), (0, 8), (4, 11), (4, 8), (3, 16)):
         xs, gs, us, ds = inside(x, off, pad), inside(wg, off, pad), inside(wu, off, pad), inside(gh, off, pad)
         h, pre, grads = _run_gated(xs, gs, us, ds, offsets, q.ACT_GELU)
         _check_gated(counts, 2, x, wg, wu, gh, h, pre, grads, "gelu")
@@ -193,8 +194,9 @@ def test_no_rows(dev):
     ([2400, 300], 520, 1000),        # the same in small tiles
     ([2, 130, 60], 4100, 120),       # few tiles of long sums
 ])
-def test_split_sums(dev, counts, k, f):
-    x, wg, wu, gh, offsets = _problem(dev, counts, 2, k, f, torch.bfloat16)
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_split_sums(dev, counts, k, f, dtype):
+    x, wg, wu, gh, offsets = _problem(dev, counts, 2, k, f, TYPES[dtype])
     h, pre, grads = _run_gated(x, wg, wu, gh, offsets, q.ACT_SILU)
     _check_gated(counts, 2, x, wg, wu, gh, h, pre, grads, "silu")
     y = q.moe_linear_forward(x, wg, offsets, out=torch.full_like(gh, 7.0))

@@ -479,7 +479,8 @@ size_t qconv_lora_mid_floats(int m, int rank);
  * b[groups][n][rank] contiguous, scale[groups] fp32 (NULL for ones).  The tokens of
  * adapter g are order[offsets[g]] .. order[offsets[g + 1] - 1], those after
  * offsets[groups] have none (qconv_moe_sort of each token's adapter, one slot); a
- * token is named once.  out may be y itself (ld_out == ld_y) or overlap no input.
+ * token is named once.  out may be y itself (ld_out == ld_y) or share no value with an
+ * input or mid (QCONV_EINVAL).
  * x a^T stays in fp32 (the leading 16 bits of each value enter the second
  * product); the result is rounded once.  An infinity among the operands may give
  * a NaN in its place.  mid (NULL to leave it out) receives x a^T in order's order

@@ -876,8 +876,8 @@ def lora_forward(y, x, a, b, offsets, order, scale=None, keep_mid: bool = False,
     """Adds to y [m][n], a shared projection's result for x [m][k], each token's
     low-rank adapter: y[t] + scale[g] (x[t] a_g^T) b_g^T with a [adapters][rank][k],
     b [adapters][n][rank], scale fp32 [adapters] (None: ones) -> (out, mid).  In
-    place, or into `out`.  offsets and order are moe_sort's of the tokens' adapters
-    (ids [m]); a token of none keeps its y.  keep_mid (or a buffer `mid` of a former
+    place, or into `out`; neither may share a value with x, a, b or mid.  offsets and
+    order are moe_sort's of the tokens' adapters (ids [m]); a token of none keeps its y.  keep_mid (or a buffer `mid` of a former
     call) keeps what lora_backward needs, else mid is None.  rank is at most 256."""
     m, groups, rank, k, n, d = _lora_args(x, a, b, offsets, order, scale, y, out, "lora_forward", stream)
     L = lib()

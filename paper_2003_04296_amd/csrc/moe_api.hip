@@ -83,6 +83,41 @@ bool lora_inputs(const qconv_lora_desc* d, const void* x, const void* a, const v
          at(offsets, 4) && at(order, 4) && at(scale, 4);
 }
 
+// Where a tensor lies: rows of `len` bytes, `ld` apart.
+struct Span {
+  uintptr_t p;
+  uint64_t rows, ld, len;
+};
+Span rows_at(const void* p, int64_t rows, int64_t ld, int64_t cols, int size) {
+  return {(uintptr_t)p, p ? (uint64_t)rows : 0, (uint64_t)ld * size, (uint64_t)cols * size};
+}
+Span block_at(const void* p, int64_t values, int size) { return rows_at(p, values > 0 ? 1 : 0, values, values, size); }
+// Whether two tensors share a byte.  Those whose rows lie between the other's do not.
+bool cross(Span a, Span b) {
+  if (a.rows == 0 || b.rows == 0) return false;
+  if (b.p < a.p) {
+    const Span t = a;
+    a = b;
+    b = t;
+  }
+  uint64_t d = b.p - a.p;
+  for (uint64_t i = 0; i < b.rows; ++i, d += b.ld) {
+    const uint64_t row = d / a.ld, in = d % a.ld;
+    if (row >= a.rows) return false;
+    if (in < a.len) return true;
+    if (row + 1 == a.rows) return false;
+    if (b.len > a.ld - in) return true;
+    if (b.ld == a.ld) return false;  // the further rows lie as this one
+  }
+  return false;
+}
+template <int N>
+bool cross(const Span& a, const Span (&others)[N]) {
+  for (const Span& b : others)
+    if (cross(a, b)) return true;
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -202,6 +237,13 @@ int qconv_lora_forward(const qconv_lora_desc* d, const void* x, const void* a, c
   const size_t need = lora_forward_bytes(*d, mid != nullptr);
   if (need && !workspace) return QCONV_EINVAL;
   if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  // one launch for few tokens reads a row of x in every block of the result's columns
+  const Span to = rows_at(out, d->m, d->ld_out, d->n, 2);
+  const Span in[] = {rows_at(x, d->m, d->ld_x, d->k, 2), rows_at(out == y ? nullptr : y, d->m, d->ld_y, d->n, 2),
+                     block_at(a, (int64_t)d->groups * d->rank * d->k, 2), block_at(b, (int64_t)d->groups * d->n * d->rank, 2),
+                     block_at(offsets, d->groups + 1, 4), block_at(order, d->m, 4), block_at(scale, d->groups, 4),
+                     block_at(mid, (int64_t)qconv_lora_mid_floats(d->m, d->rank), 4)};
+  if (cross(to, in)) return QCONV_EINVAL;
   return launch_lora_forward(*d, x, a, b, offsets, order, scale, y, out, mid, workspace, (hipStream_t)stream);
 }
 

@@ -390,7 +390,9 @@ int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_co
 /* belong to which weight is known to the device alone: offsets[groups + 1]   */
 /* (device, int32, from 0 on and never falling; rows offsets[g] ..            */
 /* offsets[g + 1] - 1 are group g's).  Nothing synchronises.  Whatever the    */
-/* device arrays hold, no call touches memory outside its tensors.            */
+/* device arrays hold, no call touches memory outside its tensors.  A result   */
+/* that shares a value with another, or with what the call still reads when it */
+/* is written, is refused (QCONV_EINVAL).                                      */
 /* ------------------------------------------------------------------------ */
 
 /* The most groups (experts, adapters). */
@@ -428,7 +430,8 @@ int qconv_moe_combine(const qconv_moe_rows_desc* d, const void* rows, const int3
 /* From gy[tokens][width] (row stride ld_tokens) and the forward's inputs:
  *   grows[place[t][s]] = weights[t][s] gy[t] (row stride ld_grows),
  *   gweights[t][s] = sum over the width of gy[t] rows[place[t][s]] (fp32, 0 where dropped).
- * grows or gweights may be NULL; rows is read for gweights alone. */
+ * grows or gweights may be NULL; rows is read for gweights alone.  grows may be
+ * rows itself (ld_grows == ld_rows), gweights weights itself. */
 int qconv_moe_combine_backward(const qconv_moe_rows_desc* d, const void* gy, const void* rows, const int32_t* place,
                                const float* weights, void* grows, int64_t ld_grows, float* gweights, void* stream);
 

@@ -597,7 +597,8 @@ def q4_gated(x, gate_codes, gate_scales, up_codes, up_scales, act: int = ACT_SIL
 # ---------------------------------------------------------------------------
 # Rows that go to different weights: tokens sorted by expert and back, the
 # experts' products, adapters of many requests.  Which rows belong to which
-# weight stays on the device (offsets); no call waits for it.
+# weight stays on the device (offsets); no call waits for it.  A result over
+# what the call still reads is refused.
 # ---------------------------------------------------------------------------
 
 _ROWS_DESC = struct.Struct("4i2q")
@@ -679,7 +680,7 @@ def _matrix(t, what, stream):
 def moe_gather(x, place, out=None, stream=None):
     """rows [tokens * slots][width] of x [tokens][width] by place (moe_sort):
     rows[place[t][s]] = x[t].  fp32 or 16-bit; rows that no place names are left
-    as they are."""
+    as they are.  out shares no value with x."""
     tokens, width = _matrix(x, "moe_gather", stream)
     slots = _place(place, tokens, x, "moe_gather")
     n = tokens * slots
@@ -693,7 +694,8 @@ def moe_gather(x, place, out=None, stream=None):
 
 def moe_combine(rows, place, weights=None, out=None, stream=None):
     """y [tokens][width] = the rows of each token's slots times weights (fp32 of
-    place's shape; None: ones), summed in fp32 and rounded once."""
+    place's shape; None: ones), summed in fp32 and rounded once.  out shares no
+    value with rows."""
     n, width = _matrix(rows, "moe_combine", stream)
     tokens = place.shape[0] if place.dim() else 0
     slots = _place(place, tokens, rows, "moe_combine")
@@ -718,7 +720,8 @@ def moe_combine_backward(gy, rows, place, weights=None, need_rows: bool = True, 
     """From gy [tokens][width] -> (the gradient of moe_combine's rows, of its
     weights: fp32 of place's shape); None for what need_rows / need_w leave out.
     Gradients of rows that no place names are left as they are.  out: tensors (or
-    None) to write instead of new ones."""
+    None) to write instead of new ones; they may be rows and weights themselves,
+    but share no value with gy."""
     import torch
 
     tokens, width = _matrix(gy, "moe_combine_backward", stream)
@@ -771,7 +774,8 @@ def moe_gated_forward(x, w_gate, w_up, offsets, act: int = ACT_SILU, keep_pre: b
                       workspace=None, stream=None):
     """ffn_forward with the weights [groups][f][k] of each row's group: rows
     offsets[g] .. offsets[g + 1] of x [rows][k] are group g's -> (h [rows][f],
-    pre).  Rows of no group are left as they are."""
+    pre).  Rows of no group are left as they are.  out shares no value with x or
+    the weights."""
     rows, k, groups, f, d = _moe_args(x, (w_gate, w_up), offsets, act, "moe_gated_forward", stream, out)
     L = lib()
     h = _new((rows, f), x.dtype, x, stream) if out is None else out
@@ -789,7 +793,8 @@ def moe_gated_forward(x, w_gate, w_up, offsets, act: int = ACT_SILU, keep_pre: b
 
 
 def moe_linear_forward(x, w, offsets, out=None, workspace=None, stream=None):
-    """y [rows][f] = x w_g^T with the weights [groups][f][k] of each row's group."""
+    """y [rows][f] = x w_g^T with the weights [groups][f][k] of each row's group.
+    out shares no value with x or w."""
     rows, k, groups, f, d = _moe_args(x, (w,), offsets, 0, "moe_linear_forward", stream, out)
     L = lib()
     y = _new((rows, f), x.dtype, x, stream) if out is None else out
@@ -814,7 +819,8 @@ def moe_gated_backward(x, w_gate, w_up, offsets, pre, gh, act: int = ACT_SILU, n
                        out=None, workspace=None, stream=None):
     """From gh [rows][f] and the forward's pre -> (gx [rows][k], gw_gate and
     gw_up [groups][f][k]) in x's type; None for what need_x / need_w leave out.
-    out: contiguous tensors (or None) to write instead of new ones.  Rows of no
+    out: contiguous tensors (or None) to write instead of new ones, which share no
+    value with what is still read: the gradient of x is written first.  Rows of no
     group are left as they are, weights of no row get zeros."""
     rows, k, groups, f, d = _moe_args(x, (w_gate, w_up), offsets, act, "moe_gated_backward", stream, gh)
     _check_pre(pre, rows, f, x, "moe_gated_backward")
@@ -899,7 +905,8 @@ def lora_backward(x, a, b, offsets, order, mid, gy, scale=None, need_x: bool = T
                   workspace=None, stream=None):
     """From gy [m][n] and the forward's mid -> (gx [m][k]: the adapters' part of
     x's gradient, ga, gb) in x's type; None for what need_x / need_w leave out.
-    out: contiguous tensors (or None) to write instead of new ones."""
+    out: contiguous tensors (or None) to write instead of new ones, which share no
+    value with x or gy where ga and gb are wanted."""
     m, groups, rank, k, n, d = _lora_args(x, a, b, offsets, order, scale, gy, None, "lora_backward", stream)
     _check_mid(mid, m, rank, x, "lora_backward")
     gx, ga, gb = _grad_outs(out, ((m, k), (groups, rank, k), (groups, n, rank)), (need_x, need_w, need_w), x,

@@ -1,6 +1,8 @@
 // moe_api.hip -- the C ABI of the operators for rows that go to different
 // weights (include/qconv.h): argument validation only.  Nothing here allocates or
 // synchronises; every launch goes to the caller's stream.
+#include <initializer_list>
+
 #include "dense.h"
 #include "moe.h"
 
@@ -46,43 +48,6 @@ int check_moe(const qconv_moe_desc* d) {
   return QCONV_OK;
 }
 
-// What both forms of the experts' products have in common.
-int check_forward(const qconv_moe_desc* d, bool gated, const void* x, const void* w, const int32_t* offsets,
-                  const void* h, const void* workspace, size_t workspace_bytes) {
-  if (!w || !offsets || (d->rows > 0 && (!x || !h)) || !at(x, 2) || !at(w, 2) || !at(h, 2) || !at(offsets, 4) ||
-      !at(workspace, 16))
-    return QCONV_EINVAL;
-  const size_t need = moe_forward_bytes(*d, gated);
-  if (need && !workspace) return QCONV_EINVAL;
-  return workspace_bytes < need ? QCONV_EWORKSPACE : QCONV_OK;
-}
-int check_backward(const qconv_moe_desc* d, bool gated, const void* x, const void* w, const int32_t* offsets,
-                   const void* gh, const void* gx, const void* gw, const void* workspace, size_t workspace_bytes) {
-  if (!w || !offsets || (d->rows > 0 && (!x || !gh)) || !at(x, 2) || !at(w, 2) || !at(gh, 2) || !at(gx, 2) ||
-      !at(gw, 2) || !at(offsets, 4) || !at(workspace, 16))
-    return QCONV_EINVAL;
-  const size_t need = moe_backward_bytes(*d, gated);
-  if (need && !workspace) return QCONV_EINVAL;
-  return workspace_bytes < need ? QCONV_EWORKSPACE : QCONV_OK;
-}
-
-int check_lora(const qconv_lora_desc* d, bool out) {
-  if (!d || d->m < 0 || d->rank < 1 || d->k < 1 || d->n < 1 || !any_type(d->dtype) || d->ld_x < d->k ||
-      d->ld_y < d->n || (out && d->ld_out < d->n) || d->ld_x > MAX_LD || d->ld_y > MAX_LD || (out && d->ld_out > MAX_LD))
-    return QCONV_EINVAL;
-  const int rc = check_groups(d->groups);
-  if (rc) return rc;
-  if (!half_type(d->dtype) || d->rank > QCONV_LORA_RANK_MOST || d->m > MOST || d->k > MOST || d->n > MOST)
-    return QCONV_EUNSUPPORTED;
-  return QCONV_OK;
-}
-// Adapters, their tokens and scales.
-bool lora_inputs(const qconv_lora_desc* d, const void* x, const void* a, const void* b, const int32_t* offsets,
-                 const int32_t* order, const float* scale, const void* y) {
-  return a && b && offsets && (d->m == 0 || (x && order && y)) && at(x, 2) && at(a, 2) && at(b, 2) && at(y, 2) &&
-         at(offsets, 4) && at(order, 4) && at(scale, 4);
-}
-
 // Where a tensor lies: rows of `len` bytes, `ld` apart.
 struct Span {
   uintptr_t p;
@@ -111,11 +76,63 @@ bool cross(Span a, Span b) {
   }
   return false;
 }
-template <int N>
-bool cross(const Span& a, const Span (&others)[N]) {
+bool cross(const Span& a, std::initializer_list<Span> others) {
   for (const Span& b : others)
     if (cross(a, b)) return true;
   return false;
+}
+Span weights_at(const qconv_moe_desc* d, const void* w) { return rows_at(w, (int64_t)d->groups * d->f, d->ld_w, d->k, 2); }
+Span weight_grads_at(const qconv_moe_desc* d, const void* gw) { return block_at(gw, (int64_t)d->groups * d->f * d->k, 2); }
+
+// What both forms of the experts' products have in common.
+int check_forward(const qconv_moe_desc* d, const void* x, const void* w, const void* w_up, const int32_t* offsets,
+                  const void* h, const float* pre, const void* workspace, size_t workspace_bytes) {
+  if (!w || !offsets || (d->rows > 0 && (!x || !h)) || !at(x, 2) || !at(w, 2) || !at(h, 2) || !at(offsets, 4) ||
+      !at(workspace, 16))
+    return QCONV_EINVAL;
+  const size_t need = moe_forward_bytes(*d, w_up);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  const Span rows = rows_at(x, d->rows, d->ld_x, d->k, 2), from = block_at(offsets, d->groups + 1, 4);
+  const Span to = rows_at(h, d->rows, d->ld_h, d->f, 2);
+  const Span kept = block_at(pre, (int64_t)qconv_ffn_pre_floats(d->rows, d->f), 4);
+  const Span wg = weights_at(d, w), wu = weights_at(d, w_up);
+  return cross(to, {rows, from, wg, wu, kept}) || cross(kept, {rows, from, wg, wu}) ? QCONV_EINVAL : QCONV_OK;
+}
+// The gradient of x is written first, the weights' are next; the gated form is done with
+// gh and pre by then.
+int check_backward(const qconv_moe_desc* d, const void* x, const void* w, const void* w_up, const int32_t* offsets,
+                   const void* gh, const void* gx, const void* gw, const void* gw_up, const void* workspace,
+                   size_t workspace_bytes) {
+  if (!w || !offsets || (d->rows > 0 && (!x || !gh)) || !at(x, 2) || !at(w, 2) || !at(gh, 2) || !at(gx, 2) ||
+      !at(gw, 2) || !at(offsets, 4) || !at(workspace, 16))
+    return QCONV_EINVAL;
+  const size_t need = moe_backward_bytes(*d, w_up);
+  if (need && !workspace) return QCONV_EINVAL;
+  if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  const Span rows = rows_at(gw ? x : nullptr, d->rows, d->ld_x, d->k, 2), from = block_at(offsets, d->groups + 1, 4);
+  const Span grads = rows_at(w_up ? nullptr : gh, d->rows, d->ld_h, d->f, 2);
+  const Span to = block_at(gx, (int64_t)d->rows * d->k, 2);
+  for (const void* g : {gw, gw_up})
+    if (cross(weight_grads_at(d, g), {rows, from, grads, to, weight_grads_at(d, g == gw ? gw_up : nullptr)})) return QCONV_EINVAL;
+  return cross(to, {rows, from, grads, weights_at(d, w), weights_at(d, w_up)}) ? QCONV_EINVAL : QCONV_OK;
+}
+
+int check_lora(const qconv_lora_desc* d, bool out) {
+  if (!d || d->m < 0 || d->rank < 1 || d->k < 1 || d->n < 1 || !any_type(d->dtype) || d->ld_x < d->k ||
+      d->ld_y < d->n || (out && d->ld_out < d->n) || d->ld_x > MAX_LD || d->ld_y > MAX_LD || (out && d->ld_out > MAX_LD))
+    return QCONV_EINVAL;
+  const int rc = check_groups(d->groups);
+  if (rc) return rc;
+  if (!half_type(d->dtype) || d->rank > QCONV_LORA_RANK_MOST || d->m > MOST || d->k > MOST || d->n > MOST)
+    return QCONV_EUNSUPPORTED;
+  return QCONV_OK;
+}
+// Adapters, their tokens and scales.
+bool lora_inputs(const qconv_lora_desc* d, const void* x, const void* a, const void* b, const int32_t* offsets,
+                 const int32_t* order, const float* scale, const void* y) {
+  return a && b && offsets && (d->m == 0 || (x && order && y)) && at(x, 2) && at(a, 2) && at(b, 2) && at(y, 2) &&
+         at(offsets, 4) && at(order, 4) && at(scale, 4);
 }
 
 }  // namespace
@@ -136,6 +153,12 @@ int qconv_moe_sort(const void* ids, int wide, int tokens, int slots, int64_t ld,
   const size_t need = moe_sort_bytes(tokens * slots, groups);
   if (need && !workspace) return QCONV_EINVAL;
   if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  // a value of place is written after the last read of its id
+  const Span from = rows_at(ids, tokens, ld, slots, wide ? 8 : 4);
+  const bool over = place == ids && !wide && ld == slots;
+  if (cross(from, {block_at(offsets, groups + 1, 4), block_at(order, (int64_t)tokens * slots, 4),
+                   block_at(over ? nullptr : place, (int64_t)tokens * slots, 4)}))
+    return QCONV_EINVAL;
   return launch_moe_sort(ids, wide != 0, tokens, slots, ld, groups, offsets, order, place, workspace,
                          (hipStream_t)stream);
 }
@@ -145,6 +168,9 @@ int qconv_moe_gather(const qconv_moe_rows_desc* d, const void* x, const int32_t*
   if (rc) return rc;
   const int a = d->dtype == QCONV_F32 ? 4 : 2;
   if ((d->tokens > 0 && (!x || !place || !rows)) || !at(x, a) || !at(rows, a) || !at(place, 4)) return QCONV_EINVAL;
+  const int64_t n = (int64_t)d->tokens * d->slots;
+  if (cross(rows_at(rows, n, d->ld_rows, d->width, a), {rows_at(x, d->tokens, d->ld_tokens, d->width, a), block_at(place, n, 4)}))
+    return QCONV_EINVAL;
   return launch_moe_gather(*d, x, place, rows, (hipStream_t)stream);
 }
 
@@ -154,6 +180,10 @@ int qconv_moe_combine(const qconv_moe_rows_desc* d, const void* rows, const int3
   if (rc) return rc;
   const int a = d->dtype == QCONV_F32 ? 4 : 2;
   if ((d->tokens > 0 && (!rows || !place || !y)) || !at(rows, a) || !at(y, a) || !at(place, 4) || !at(weights, 4))
+    return QCONV_EINVAL;
+  const int64_t n = (int64_t)d->tokens * d->slots;
+  if (cross(rows_at(y, d->tokens, d->ld_tokens, d->width, a),
+            {rows_at(rows, n, d->ld_rows, d->width, a), block_at(place, n, 4), block_at(weights, n, 4)}))
     return QCONV_EINVAL;
   return launch_moe_combine(*d, rows, place, weights, y, (hipStream_t)stream);
 }
@@ -165,6 +195,14 @@ int qconv_moe_combine_backward(const qconv_moe_rows_desc* d, const void* gy, con
   const int a = d->dtype == QCONV_F32 ? 4 : 2;
   if ((d->tokens > 0 && (!gy || !place || (gweights && !rows))) || (grows && (ld_grows < d->width || ld_grows > MAX_LD)) ||
       !at(gy, a) || !at(rows, a) || !at(grows, a) || !at(place, 4) || !at(weights, 4) || !at(gweights, 4))
+    return QCONV_EINVAL;
+  // a value of rows, and a weight, is read before the gradient in its place is written
+  const int64_t n = (int64_t)d->tokens * d->slots;
+  const Span token = rows_at(gy, d->tokens, d->ld_tokens, d->width, a), places = block_at(place, n, 4);
+  const Span expert = rows_at(gweights ? rows : nullptr, n, d->ld_rows, d->width, a), w = block_at(weights, n, 4);
+  const Span to = rows_at(grows, n, ld_grows, d->width, a), to_w = block_at(gweights, n, 4);
+  if (cross(to, {token, places, w}) || (!(grows == rows && ld_grows == d->ld_rows) && cross(to, expert)) ||
+      cross(to_w, {token, places, expert, to}) || (gweights != weights && cross(to_w, w)))
     return QCONV_EINVAL;
   return launch_moe_combine_back(*d, gy, rows, place, weights, grows, ld_grows, gweights, (hipStream_t)stream);
 }
@@ -179,7 +217,7 @@ int qconv_moe_gated_forward(const qconv_moe_desc* d, const void* x, const void* 
   int rc = check_moe(d);
   if (rc) return rc;
   if (!w_up || !at(w_up, 2) || !at(pre, 16)) return QCONV_EINVAL;
-  rc = check_forward(d, true, x, w_gate, offsets, h, workspace, workspace_bytes);
+  rc = check_forward(d, x, w_gate, w_up, offsets, h, pre, workspace, workspace_bytes);
   return rc ? rc : launch_moe_forward(*d, x, w_gate, w_up, offsets, h, pre, workspace, (hipStream_t)stream);
 }
 
@@ -187,7 +225,7 @@ int qconv_moe_linear_forward(const qconv_moe_desc* d, const void* x, const void*
                              void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_moe(d);
   if (rc) return rc;
-  rc = check_forward(d, false, x, w, offsets, y, workspace, workspace_bytes);
+  rc = check_forward(d, x, w, nullptr, offsets, y, nullptr, workspace, workspace_bytes);
   return rc ? rc : launch_moe_forward(*d, x, w, nullptr, offsets, y, nullptr, workspace, (hipStream_t)stream);
 }
 
@@ -202,7 +240,7 @@ int qconv_moe_gated_backward(const qconv_moe_desc* d, const void* x, const void*
   if (rc) return rc;
   if (!w_up || (d->rows > 0 && !pre) || !gw_gate != !gw_up || !at(w_up, 2) || !at(gw_up, 2) || !at(pre, 16))
     return QCONV_EINVAL;
-  rc = check_backward(d, true, x, w_gate, offsets, gh, gx, gw_gate, workspace, workspace_bytes);
+  rc = check_backward(d, x, w_gate, w_up, offsets, gh, gx, gw_gate, gw_up, workspace, workspace_bytes);
   return rc ? rc : launch_moe_backward(*d, x, w_gate, w_up, offsets, pre, gh, gx, gw_gate, gw_up, workspace,
                                        (hipStream_t)stream);
 }
@@ -212,7 +250,7 @@ int qconv_moe_linear_backward(const qconv_moe_desc* d, const void* x, const void
                               void* stream) {
   int rc = check_moe(d);
   if (rc) return rc;
-  rc = check_backward(d, false, x, w, offsets, gy, gx, gw, workspace, workspace_bytes);
+  rc = check_backward(d, x, w, nullptr, offsets, gy, gx, gw, nullptr, workspace, workspace_bytes);
   return rc ? rc : launch_moe_backward(*d, x, w, nullptr, offsets, nullptr, gy, gx, gw, nullptr, workspace,
                                        (hipStream_t)stream);
 }
@@ -239,11 +277,11 @@ int qconv_lora_forward(const qconv_lora_desc* d, const void* x, const void* a, c
   if (workspace_bytes < need) return QCONV_EWORKSPACE;
   // one launch for few tokens reads a row of x in every block of the result's columns
   const Span to = rows_at(out, d->m, d->ld_out, d->n, 2);
-  const Span in[] = {rows_at(x, d->m, d->ld_x, d->k, 2), rows_at(out == y ? nullptr : y, d->m, d->ld_y, d->n, 2),
-                     block_at(a, (int64_t)d->groups * d->rank * d->k, 2), block_at(b, (int64_t)d->groups * d->n * d->rank, 2),
-                     block_at(offsets, d->groups + 1, 4), block_at(order, d->m, 4), block_at(scale, d->groups, 4),
-                     block_at(mid, (int64_t)qconv_lora_mid_floats(d->m, d->rank), 4)};
-  if (cross(to, in)) return QCONV_EINVAL;
+  if (cross(to, {rows_at(x, d->m, d->ld_x, d->k, 2), rows_at(out == y ? nullptr : y, d->m, d->ld_y, d->n, 2),
+                 block_at(a, (int64_t)d->groups * d->rank * d->k, 2), block_at(b, (int64_t)d->groups * d->n * d->rank, 2),
+                 block_at(offsets, d->groups + 1, 4), block_at(order, d->m, 4), block_at(scale, d->groups, 4),
+                 block_at(mid, (int64_t)qconv_lora_mid_floats(d->m, d->rank), 4)}))
+    return QCONV_EINVAL;
   return launch_lora_forward(*d, x, a, b, offsets, order, scale, y, out, mid, workspace, (hipStream_t)stream);
 }
 
@@ -260,6 +298,15 @@ int qconv_lora_backward(const qconv_lora_desc* d, const void* x, const void* a, 
   const size_t need = lora_backward_bytes(*d);
   if (need && !workspace) return QCONV_EINVAL;
   if (workspace_bytes < need) return QCONV_EWORKSPACE;
+  // gx is written first, then ga, then gb; a and b have been copied by then
+  const Span rows = rows_at(ga ? x : nullptr, d->m, d->ld_x, d->k, 2), grads = rows_at(ga ? gy : nullptr, d->m, d->ld_y, d->n, 2);
+  const Span from = block_at(offsets, d->groups + 1, 4), tokens = block_at(order, d->m, 4), scales = block_at(scale, d->groups, 4);
+  const Span kept = block_at(ga ? mid : nullptr, (int64_t)qconv_lora_mid_floats(d->m, d->rank), 4);
+  const Span to = block_at(gx, (int64_t)d->m * d->k, 2), to_a = block_at(ga, (int64_t)d->groups * d->rank * d->k, 2);
+  const Span to_b = block_at(gb, (int64_t)d->groups * d->n * d->rank, 2);
+  if (cross(to, {rows, grads, from, tokens, scales, kept, to_a, to_b}) ||
+      cross(to_a, {rows, grads, from, tokens, scales, kept, to_b}) || cross(to_b, {grads, from, tokens, scales, kept}))
+    return QCONV_EINVAL;
   return launch_lora_backward(*d, x, a, b, offsets, order, scale, mid, gy, gx, ga, gb, workspace, (hipStream_t)stream);
 }
 

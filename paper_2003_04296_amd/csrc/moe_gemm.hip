@@ -227,13 +227,14 @@ __global__ __launch_bounds__(NW * 64) void moe_rows_kernel(RowsArgs a, Groups g,
   dense_rows_tile<T, Dense16, H, 1, NW>(a, xs, nt, piece);
 }
 
+int64_t few_blocks(int rows, int groups, int outputs) {
+  return round_up(ceil_div(outputs, 16), 8) * GroupPieces::most(rows, groups, 16);
+}
 template <class T, int H>
 int run_few(RowsArgs& a, const Groups& g, int64_t step_w, hipStream_t s) {
   constexpr int NW = 8;
   a.tiles_n = ceil_div(a.n, 16);
-  const int64_t blocks = (int64_t)(a.tiles_n + 7) / 8 * 8 * GroupPieces::most(g.rows, g.n, 16);
-  if (blocks >= (1 << 22)) return QCONV_EUNSUPPORTED;
-  moe_rows_kernel<T, H, NW><<<(unsigned)blocks, NW * 64, 0, s>>>(a, g, step_w);
+  moe_rows_kernel<T, H, NW><<<(unsigned)few_blocks(g.rows, g.n, a.n), NW * 64, 0, s>>>(a, g, step_w);
   return hip_status();
 }
 
@@ -365,7 +366,9 @@ PlanW plan_weights(const qconv_moe_desc& d, bool gated, bool aligned) {
 //   16 experts 2048 -> 4096   99 and 128 at 32 rows, 109 and 132 at 128, 136 and 132 at 256
 //   64 experts 2048 -> 1024   73 and 101 at 64, 106 and 131 at 256, 141 and 134 at 1024
 //   64 experts 512 -> 512     12.4 and 15.5 at 32, 17.4 and 16.6 at 64, 24 and 19 at 256
+// Tiles take more outputs, too, than blocks of 16 outputs may be launched for (2^31 threads).
 bool few_rows(const qconv_moe_desc& d) {
+  if (few_blocks(d.rows, d.groups, d.f) >= (1 << 22)) return false;
   const int many = d.k < 1024 ? 32 : 4 * d.groups;
   return d.rows <= (d.k >= 1024 && many < 64 ? 64 : many);
 }

@@ -444,7 +444,8 @@ typedef struct {
 
 /* The experts' products.  x[rows][k]; weights [groups][f][k], one group's rows
  * right after the other's (row (g, i) at w + (g * f + i) * ld_w).  Rows of no
- * group are not read and their results not written.  Otherwise as
+ * group matter to no result (copies of x and gy into aligned rows, and dg and
+ * du, may read them), and results are not written there.  Otherwise as
  * qconv_ffn_forward and qconv_ffn_backward for each group: pre is
  * [rows][2][fp] (qconv_ffn_pre_floats(rows, f)), gx and the weight gradients
  * [groups][f][k] are contiguous, those of a group without rows zero. */

@@ -392,7 +392,8 @@ int qconv_q4_gated(const qconv_q4_desc* d, const void* x, const uint8_t* gate_co
 /* offsets[g + 1] - 1 are group g's).  Nothing synchronises.  Whatever the    */
 /* device arrays hold, no call touches memory outside its tensors.  A result   */
 /* that shares a value with another, or with what the call still reads when it */
-/* is written, is refused (QCONV_EINVAL).                                      */
+/* is written, is refused (QCONV_EINVAL), as are sizes that would take a launch */
+/* of 2^31 threads (QCONV_EUNSUPPORTED; results are then not to be used).      */
 /* ------------------------------------------------------------------------ */
 
 /* The most groups (experts, adapters). */

@@ -819,6 +819,8 @@ def moe_gated_backward(x, w_gate, w_up, offsets, pre, gh, act: int = ACT_SILU, n
                        out=None, workspace=None, stream=None):
     """From gh [rows][f] and the forward's pre -> (gx [rows][k], gw_gate and
     gw_up [groups][f][k]) in x's type; None for what need_x / need_w leave out.
+    The gradients of both products are rounded to x's type on the way (with fp16
+    infinite past 65504: the loss is scaled as for any gradient).
     out: contiguous tensors (or None) to write instead of new ones, which share no
     value with what is still read: the gradient of x is written first.  Rows of no
     group are left as they are, weights of no row get zeros."""
@@ -883,7 +885,9 @@ def lora_forward(y, x, a, b, offsets, order, scale=None, keep_mid: bool = False,
     low-rank adapter: y[t] + scale[g] (x[t] a_g^T) b_g^T with a [adapters][rank][k],
     b [adapters][n][rank], scale fp32 [adapters] (None: ones) -> (out, mid).  In
     place, or into `out`; neither may share a value with x, a, b or mid.  offsets and
-    order are moe_sort's of the tokens' adapters (ids [m]); a token of none keeps its y.  keep_mid (or a buffer `mid` of a former
+    order are moe_sort's of the tokens' adapters (ids [m]); a token of none keeps its y.
+    An infinity among the operands may give a NaN in its place: the second product
+    takes x a_g^T in two parts.  keep_mid (or a buffer `mid` of a former
     call) keeps what lora_backward needs, else mid is None.  rank is at most 256."""
     m, groups, rank, k, n, d = _lora_args(x, a, b, offsets, order, scale, y, out, "lora_forward", stream)
     L = lib()

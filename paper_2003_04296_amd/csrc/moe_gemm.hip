@@ -7,9 +7,9 @@
 //
 // Bound by the matrix cores at many rows, by reading the weights at few.  Measured in
 // bf16, 16384 rows of 8 experts (half of them one expert's), 2048 <-> 4096, 0.55 TFLOP
-// each: forward 646 us with the 0.54 GB of pre (490 without), gx 482, both weight
-// gradients 520 (850 to 1140 TFLOP/s); 8192 rows of 16 experts, 2048 -> 2048, linear:
-// forward 100, gx 102, weight gradients 115 (600 to 690).  What is lost against one
+// each: forward 652 us with the 0.54 GB of pre (509 without), gx 495, both weight
+// gradients 532 (840 to 1110 TFLOP/s); 8192 rows of 16 experts, 2048 -> 2048, linear:
+// forward 101, gx 102, weight gradients 115 (600 to 680).  What is lost against one
 // weight's products: tiles that an expert's last rows do not fill, the tail of the
 // last tiles, and sums too short to hide a tile's start and end.
 #include "dense_ffn.h"

@@ -1,6 +1,6 @@
 """Workspaces of exactly the stated bytes, full of NaN, for every way that the
 operators for rows that go to different weights use one (run with -m gpu): results are
-those of a call without one, nothing past the workspace is written, one byte group
+those of a call without one, nothing past the workspace is written, one byte
 less is refused."""
 import ctypes
 
